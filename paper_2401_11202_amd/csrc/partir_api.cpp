@@ -28,14 +28,37 @@
 #include <vector>
 
 #include "../../include/partir.h"
-#include "plan.h"
+#include "kernels.h"
 
 namespace partir {
+namespace {
+
+constexpr int kNumCU = 256;           // MI355X compute units: a grid below this underfills
+// Tile-order grouping for L2 reuse: consecutive workgroups walk group_m tile
+// rows before the next tile column; wide grids want shorter groups.
+// Tile-order grouping of the bf16 GEMM: consecutive tiles walk group_m tile
+// rows before moving to the next tile column, so the 32 tiles one XCD runs at
+// a time form a 4 x 8 block of the output, whose operands are 12 row blocks
+// (a 2 x 16 block needs 18): the least L2 -> fabric traffic per k step.
+int group_m_for(int /*tiles_n*/) { return 4; }
+constexpr size_t kWsAlign = 256;
+// Partials the planner may ask for on its own: what the array of
+// partir_loop_matmul_noalloc holds.
+constexpr size_t kMaxPartialBytes = (size_t)64 << 20;
 
 thread_local std::string g_error;
 thread_local std::string g_plan_text;
-thread_local std::function<void()> g_deferred_text;
+thread_local std::function<void()> g_deferred_text;   // builds g_plan_text of the last call, if it is wanted
+
+// Whether the plan being built on this thread needs its text: formatting takes
+// as long as planning, and only partir_last_plan_text reads what a call that
+// executes would leave.
 thread_local bool g_want_text = true;
+
+struct TextScope {
+  explicit TextScope(bool want) { g_want_text = want; }
+  ~TextScope() { g_want_text = true; }
+};
 
 // snprintf into a plan's text; empty when no text is wanted
 void textf(char* buf, size_t n, const char* fmt, ...) {
@@ -57,21 +80,43 @@ int fail(int status, const char* fmt, ...) {
   return status;
 }
 
-namespace {
-
-// Tile-order grouping for L2 reuse: consecutive workgroups walk group_m tile
-// rows before the next tile column; wide grids want shorter groups.
-// Tile-order grouping of the bf16 GEMM: consecutive tiles walk group_m tile
-// rows before moving to the next tile column, so the 32 tiles one XCD runs at
-// a time form a 4 x 8 block of the output, whose operands are 12 row blocks
-// (a 2 x 16 block needs 18): the least L2 -> fabric traffic per k step.
-int group_m_for(int /*tiles_n*/) { return 4; }
-// Partials the planner may ask for on its own: what the array of
-// partir_loop_matmul_noalloc holds.
-constexpr size_t kMaxPartialBytes = (size_t)64 << 20;
-
+size_t align_up(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 int elem_bytes(int dt) { return dt == PARTIR_BF16 ? 2 : 4; }
 bool valid_dtype(int dt) { return dt == PARTIR_F32 || dt == PARTIR_BF16; }
+
+// ---------------------------------------------------------------------------
+// Plans
+// ---------------------------------------------------------------------------
+enum LaunchKind { L_GEMM_BF16, L_GEMM_F32, L_REDUCE, L_ATTN, L_ATTN_COMBINE, L_RMS, L_ACT_BWD, L_COLSUM,
+                  L_GEMM_BF16_PARTS, L_ATTN_BWD, L_RMS_PARTS, L_GEMM_BF16_FIXUP, L_GEMM_BF16_PARTS_FIXUP };
+
+struct Launch {
+  LaunchKind kind;
+  std::string name;
+  std::string text;
+  GemmParams gemm{};
+  GemmF32Params gemm32{};
+  ReduceParams reduce{};
+  AttnParams attn{};
+  RmsParams rms{};
+  ActBwdParams act{};
+  ColSumParams cs{};
+  std::shared_ptr<GemmParts> parts;   // L_GEMM_BF16_PARTS: the device-local arrays
+  std::shared_ptr<RmsParts> rms_parts;   // L_RMS_PARTS
+  AttnBwdParams attn_bwd{};
+};
+
+struct Plan {
+  std::vector<Launch> launches;
+  int n_shards = 1;
+  int n_tile_loops = 0;
+  int n_sum_loops = 0;
+  int n_sum_splitk = 0;
+  size_t ws_bytes = 0;
+  double flops = 0;
+};
 
 // ---------------------------------------------------------------------------
 // Tracing
@@ -445,12 +490,9 @@ hipError_t run_one(const Launch& L, hipStream_t s) {
     case L_GEMM_BF16_PARTS_FIXUP: return launch_gemm_bf16_parts_fixup(L.gemm, *L.parts, s);
     case L_ATTN_BWD: return launch_attention_backward(L.attn_bwd, s);
     case L_RMS_PARTS: return launch_rmsnorm_parts(L.rms, *L.rms_parts, s);
-    case L_CALL: return L.call(s);
   }
   return hipErrorInvalidValue;
 }
-
-}  // namespace
 
 void keep_plan_text(const Plan& plan, const char* what) {
   std::string t = std::string(what) + ": " + std::to_string(plan.n_shards) + " virtual shards, " +
@@ -465,12 +507,50 @@ void keep_plan_text(const Plan& plan, const char* what) {
   if (dump && dump[0] == '1') fputs(t.c_str(), stderr);
 }
 
+// A pointer the plan depends on only by being there: its text is planned again
+// later with a stand-in, so that no caller's pointer outlives the call.
+template <typename T>
+void stand_in(T*& p) {
+  if (p) p = (T*)(uintptr_t)kWsAlign;
+}
+
 int check_ws(const Plan& plan, void* ws, size_t ws_bytes) {
   if (ws_bytes < plan.ws_bytes)
     return fail(PARTIR_E_WORKSPACE, "workspace of %zu bytes, need %zu", ws_bytes, plan.ws_bytes);
   if (plan.ws_bytes > 0 && ws == nullptr) return fail(PARTIR_E_NULL, "workspace pointer is NULL");
   if (plan.ws_bytes > 0 && !aligned16(ws)) return fail(PARTIR_E_LAYOUT, "workspace not 16-byte aligned");
   return PARTIR_OK;
+}
+
+int execute(const Plan& plan, void* stream);
+
+// A call that executes: plans it once (with its workspace), runs it, and
+// leaves the text to partir_last_plan_text.
+template <typename Args>
+int run_plan(const char* what, const Args& a, void (*planner)(const Args&, void*, Plan&), void* ws, size_t ws_bytes,
+             void* stream) {
+  const char* dump = getenv("PARTIR_DUMP_PLAN");
+  const bool now = dump && dump[0] == '1';
+  Plan plan;
+  plan.launches.reserve(12);
+  {
+    TextScope scope(now);
+    planner(a, ws, plan);
+  }
+  const int st = check_ws(plan, ws, ws_bytes);
+  if (st) return st;
+  if (now) {
+    keep_plan_text(plan, what);
+  } else {
+    Args sizes = a;
+    sizes.drop_pointers();
+    g_deferred_text = [what, sizes, planner] {
+      Plan again;
+      planner(sizes, nullptr, again);
+      keep_plan_text(again, what);
+    };
+  }
+  return execute(plan, stream);
 }
 
 int execute(const Plan& plan, void* stream) {
@@ -501,8 +581,6 @@ int execute(const Plan& plan, void* stream) {
   }
   return PARTIR_OK;
 }
-
-namespace {
 
 // ---------------------------------------------------------------------------
 // partir_loop_matmul
@@ -1390,8 +1468,6 @@ void plan_mlp_bwd(const MlpBwdArgs& a, void* ws, Plan& plan) {
   plan.ws_bytes = off + gws;
 }
 
-}  // namespace
-
 void fill_info(const Plan& plan, partir_plan_info* info) {
   if (!info) return;
   info->n_virtual_shards = plan.n_shards;
@@ -1403,6 +1479,8 @@ void fill_info(const Plan& plan, partir_plan_info* info) {
   info->workspace_bytes = plan.ws_bytes;
   info->flops = plan.flops;
 }
+
+}  // namespace
 
 void set_last_error(const std::string& msg) { g_error = msg; }
 
