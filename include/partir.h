@@ -482,6 +482,104 @@ size_t partir_decoder_layer_workspace(int64_t B, int64_t S, int64_t D, int64_t n
                                       int64_t d_head, int64_t F, int R_batch, int R_model);
 
 /* ------------------------------------------------------------------------ */
+/* Operators beside the nests: positions, norms of queries and keys,           */
+/* attention to another sequence, the norm of the gradients.                   */
+/* ------------------------------------------------------------------------ */
+/* These take their leading dimensions as arguments, so that queries, keys and
+ * values can be column blocks of one fused projection.  The conventions above
+ * hold; partir_trace_* and partir_last_plan_text do not cover them.  `stream`
+ * must belong to the current device. */
+
+/* How partir_rotary_frequencies stretches the positions of a model to longer
+ * contexts. */
+typedef enum partir_rotary_scaling {
+  PARTIR_ROTARY_PLAIN = 0,   /* f_i = base^(-2 i / rotary_dim)                            */
+  PARTIR_ROTARY_LINEAR = 1,  /* f_i / factor                                              */
+  PARTIR_ROTARY_BASE = 2,    /* base * factor^(rotary_dim / (rotary_dim - 2)): the last
+                                pair as with LINEAR, the first unchanged                  */
+  PARTIR_ROTARY_PARTS = 3    /* by the turns a pair makes in original_length positions:
+                                f_i / factor up to slow_turns, f_i from fast_turns on, a
+                                linear blend between                                      */
+} partir_rotary_scaling;
+
+/* Radians per position of the rotary_dim / 2 pairs into the HOST array freqs;
+ * partir_rotary and its kin read them from device memory.  rotary_dim even, at
+ * most 256; base > 1; factor >= 1 (not read by PLAIN); the last three
+ * arguments are read by PARTS only.
+ * Errors: E_NULL, E_SHAPE, E_UNSUPPORTED. */
+int partir_rotary_frequencies(int64_t rotary_dim, double base, int scaling, double factor, int64_t original_length,
+                              double slow_turns, double fast_turns, double* freqs);
+
+/* Rotary positions: the first rotary_dim values of each head are rotary_dim / 2
+ * pairs (a, b), turned by theta = position * freqs[i] and multiplied by
+ * magnitude:  (a, b) -> magnitude (a cos - b sin, a sin + b cos);
+ * the other values are kept.  inverse != 0 applies the transposed map (sin
+ * negated): the gradient of the call without it.
+ * Q: [T, n_heads * d_head], K: [T, n_kv_heads * d_head] (either head count may
+ * be 0), dtype F32 or BF16, leading dims ldq, ldk; Qo, Ko of the same shapes
+ * and type.  An output is its input (pointer and leading dim alike), or apart
+ * from every input and output.
+ * interleaved: pairs are (x[2i], x[2i+1]), else (x[i], x[i + rotary_dim / 2]).
+ * freqs: [rotary_dim / 2] float64 on the device.  positions: [T] int32, or
+ * int64 with positions64 != 0; NULL: row t stands at t mod S (S >= 1).
+ * Positions may be of any size: angles are formed in float64.
+ * d_head: a multiple of 8 up to 256; rotary_dim even, 0..d_head.
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_LAYOUT, E_UNSUPPORTED, E_HIP. */
+int partir_rotary(const void* Q, const void* K, void* Qo, void* Ko, const double* freqs, const void* positions,
+                  int positions64, int64_t T, int64_t S, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
+                  int64_t rotary_dim, int64_t ldq, int64_t ldk, int64_t ldqo, int64_t ldko, int dtype, int interleaved,
+                  int inverse, float magnitude, void* stream);
+
+/* RMS norm of every head of Q and K over its d_head values with a gain shared
+ * by the heads, then the rotation of partir_rotary, in one pass:
+ *   n = g * x / sqrt(mean(x^2) + eps),  y = rotary(n).
+ * gq, gk: [d_head] float32, or NULL for gains of 1.  rotary_dim = 0 is the
+ * norms alone (freqs may be NULL).  Otherwise as partir_rotary. */
+int partir_qk_norm_rotary(const void* Q, const void* K, const float* gq, const float* gk, void* Qo, void* Ko,
+                          const double* freqs, const void* positions, int positions64, int64_t T, int64_t S,
+                          int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t rotary_dim, int64_t ldq,
+                          int64_t ldk, int64_t ldqo, int64_t ldko, int dtype, int interleaved, float magnitude, float eps,
+                          void* stream);
+
+/* Gradients of partir_qk_norm_rotary for the cotangents dQo, dKo of its
+ * outputs, from its inputs Q, K (nothing is kept by the forward call):
+ *   dn = rotary^T(dy);  r = 1 / sqrt(mean(x^2) + eps);
+ *   dx = r (g dn - x r^2 mean(x g dn));   dg = sum over tokens and heads of dn x r.
+ * dQ, dK as Q, K (either may be its cotangent's array, pointer and leading dim
+ * alike); dgq, dgk: [d_head] float32, either may be NULL: not stored.  The sums of dg are
+ * taken in float32 in a fixed order.  With T = 0 or no heads dg is 0.
+ * Workspace: the partial gain gradients. */
+int partir_qk_norm_rotary_backward(const void* Q, const void* K, const void* dQo, const void* dKo, const float* gq,
+                                   const float* gk, void* dQ, void* dK, float* dgq, float* dgk, const double* freqs,
+                                   const void* positions, int positions64, int64_t T, int64_t S, int64_t n_heads,
+                                   int64_t n_kv_heads, int64_t d_head, int64_t rotary_dim, int64_t ldq, int64_t ldk,
+                                   int64_t lddqo, int64_t lddko, int64_t lddq, int64_t lddk, int dtype, int interleaved,
+                                   float magnitude, float eps, void* ws, size_t ws_bytes, void* stream);
+size_t partir_qk_norm_rotary_backward_workspace(int64_t T, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
+                                                int64_t rotary_dim, int dtype);
+
+/* Global norm of n tensors, sqrt of the sum of every element's square, into
+ * norm[0] (device, float32).  tensors, numel, dtypes: HOST arrays of device
+ * pointers, element counts and partir_dtypes (F32 and BF16 may be mixed); a
+ * tensor is dense and aligned to its element type only, so it may be a view
+ * into a flat bucket.  Squares are summed in float64, in a fixed order.  No
+ * tensors, or empty ones: 0.
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_LAYOUT, E_WORKSPACE, E_HIP. */
+int partir_grad_norm(const void* const* tensors, const int64_t* numel, const int* dtypes, int n, float* norm, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* partir_grad_norm, then out[i] = tensors[i] * (norm > max_norm ? max_norm /
+ * norm : 1), each value rounded once to its type.  out: HOST array of device
+ * pointers; out[i] = tensors[i] scales in place (nothing is written where the
+ * norm is within max_norm).  Where an element is infinite or NaN, so is the
+ * norm, and nothing is scaled: the tensors are copied as they are.  Outputs must be apart from
+ * each other and from other tensors' inputs (E_LAYOUT).  max_norm >= 0
+ * (E_UNSUPPORTED otherwise). */
+int partir_clip_grad_norm(const void* const* tensors, void* const* out, const int64_t* numel, const int* dtypes, int n,
+                          double max_norm, float* norm, void* ws, size_t ws_bytes, void* stream);
+size_t partir_grad_norm_workspace(int n);
+
+/* ------------------------------------------------------------------------ */
 /* Plans: what a call will do, without doing it (host only, no GPU needed).  */
 /* ------------------------------------------------------------------------ */
 typedef struct partir_plan_info {

@@ -39,7 +39,9 @@ EXPORTS = ("partir_loop_matmul", "partir_loop_matmul_workspace", "partir_mlp_blo
            "partir_attn_block_saved_bytes", "partir_attn_block_backward", "partir_attn_block_backward_workspace",
            "partir_plan_attn_block_backward", "partir_decoder_layer_sharded",
            "partir_decoder_layer_sharded_workspace", "partir_plan_decoder_layer_sharded",
-           "partir_loop_matmul_noalloc")
+           "partir_loop_matmul_noalloc", "partir_rotary_frequencies", "partir_rotary", "partir_qk_norm_rotary",
+           "partir_qk_norm_rotary_backward", "partir_qk_norm_rotary_backward_workspace", "partir_grad_norm",
+           "partir_clip_grad_norm", "partir_grad_norm_workspace")
 
 
 class PartirError(RuntimeError):
@@ -66,7 +68,10 @@ _lib = None
 _TILE = {None: AXIS_NONE, "M": AXIS_M, "N": AXIS_N, "K": AXIS_K}
 _SUM_IMPL = {"auto": SUM_AUTO, "fused": SUM_FUSED, "splitk": SUM_SPLITK}
 I64, I32, P, SZ, F = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
+D = ctypes.c_double
 PP = ctypes.POINTER(ctypes.c_void_p)   # a host array of device pointers
+PI64, PI32 = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int)
+ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 
 def lib():
@@ -126,6 +131,17 @@ def lib():
         "partir_attn_block_backward_workspace": (SZ, [I64, I64, I64, I64, I64, I32, I32]),
         "partir_plan_attn_block_backward": (I32, [I64, I64, I64, I64, I64, I32, I32, I32,
                                                   ctypes.POINTER(PlanInfo)]),
+        "partir_rotary_frequencies": (I32, [I64, D, I32, D, I64, D, D, P]),
+        "partir_rotary": (I32, [P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64, I64, I64, I64, I64, I32, I32, I32,
+                                F, P]),
+        "partir_qk_norm_rotary": (I32, [P, P, P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64, I64, I64, I64, I64,
+                                        I32, I32, F, F, P]),
+        "partir_qk_norm_rotary_backward": (I32, [P, P, P, P, P, P, P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64,
+                                                 I64, I64, I64, I64, I64, I64, I32, I32, F, F, P, SZ, P]),
+        "partir_qk_norm_rotary_backward_workspace": (SZ, [I64, I64, I64, I64, I64, I32]),
+        "partir_grad_norm": (I32, [PP, PI64, PI32, I32, P, P, SZ, P]),
+        "partir_clip_grad_norm": (I32, [PP, PP, PI64, PI32, I32, D, P, P, SZ, P]),
+        "partir_grad_norm_workspace": (SZ, [I32]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -788,6 +804,252 @@ def decoder_layer(x, g1, g2, Wq, Wk, Wv, Wo, W1, W2, *, B: int, S: int, n_heads:
                                       _ptr(Wo), _ptr(W1), _ptr(W2), B, S, D, n_heads, d_head, F,
                                       R_batch, R_model, _ptr(ws), wsb, _stream(stream)))
     return x
+
+
+# ---------------------------------------------------------------------------
+# Operators beside the nests: rotary positions, norms of queries and keys,
+# the global norm of gradients
+# ---------------------------------------------------------------------------
+def _launch(dev, fn, *args, stream):
+    """fn(*args, stream) with `dev` current (a call runs where its tensors are)."""
+    torch = _th()
+    if dev.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(dev):
+            _check(fn(*args, _stream(stream)))
+
+
+def _matrix(t, name, rows, cols, dtype):
+    """The leading dim of a row-major [rows, cols] tensor, a view perhaps."""
+    if not isinstance(t, _th().Tensor):
+        _bad("PARTIR_E_NULL", f"{name} must be a tensor")
+    if t.dtype != dtype:
+        _bad("PARTIR_E_DTYPE", f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != (rows, cols):
+        _bad("PARTIR_E_SHAPE", f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
+    if rows == 0 or cols == 0:
+        return cols
+    if t.stride(1) != 1 and cols > 1:
+        _bad("PARTIR_E_LAYOUT", f"{name} must be row-major")
+    return t.stride(0) if rows > 1 else cols     # one row: its stride is never used
+
+
+def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       original_length: int = 0, slow_turns: float = 1.0, fast_turns: float = 32.0, device="cuda"):
+    """Radians per position of each pair, float64 [rotary_dim / 2] on `device`
+    (laid out once, for every call of rotary and qk_norm_rotary).  scaling for
+    contexts `factor` times longer: None, 'linear' (f / factor), 'base' (the
+    base raised so that the slowest pair is as with 'linear') or 'parts' (by the
+    turns a pair makes in original_length positions: f / factor up to
+    slow_turns, f from fast_turns on, a linear blend between)."""
+    torch = _th()
+    if scaling not in ROTARY_SCALING:
+        _bad("PARTIR_E_UNSUPPORTED", f"scaling {scaling!r}")
+    host = torch.empty(max(0, rotary_dim // 2), dtype=torch.float64)
+    _check(lib().partir_rotary_frequencies(rotary_dim, base, ROTARY_SCALING[scaling], factor, original_length,
+                                           slow_turns, fast_turns, _ptr(host)))
+    return host.to(device)
+
+
+def _rotary_args(Q, K, freqs, d_head, positions, S):
+    """Checked sizes of a rotary call: (T, Hq, Hk, rotary_dim, S, ldq, ldk)."""
+    torch = _th()
+    if not isinstance(Q, torch.Tensor) or Q.dim() != 2 or (K is not None and (not isinstance(K, torch.Tensor) or K.dim() != 2)):
+        _bad("PARTIR_E_SHAPE", "Q and K must be 2-D tensors")
+    if d_head < 1:
+        _bad("PARTIR_E_SHAPE", f"d_head = {d_head}")
+    T, cq = Q.shape
+    ck = 0 if K is None else K.shape[1]
+    if cq % d_head or ck % d_head:
+        _bad("PARTIR_E_SHAPE", f"rows of {cq} and {ck} values do not hold whole heads of {d_head}")
+    _dt(Q)
+    ldq = _matrix(Q, "Q", T, cq, Q.dtype)
+    ldk = 0 if K is None else _matrix(K, "K", T, ck, Q.dtype)
+    rd = 0
+    if freqs is not None:
+        if freqs.dim() != 1:
+            _bad("PARTIR_E_SHAPE", "freqs must be 1-D")
+        rd = 2 * _req(freqs, "freqs", (freqs.shape[0],), torch.float64).shape[0]
+    if positions is not None:
+        if positions.dtype not in (torch.int32, torch.int64):
+            _bad("PARTIR_E_DTYPE", f"positions has dtype {positions.dtype}, expected int32 or int64")
+        _req(positions, "positions", (T,), positions.dtype)
+    return T, cq // d_head, ck // d_head, rd, (T if S is None else S) or 1, ldq, ldk
+
+
+def _rotary_out(out, names, Q, K, T):
+    """The outputs of a rotary call and their leading dims: the caller's pair, or new ones."""
+    if out is None:
+        torch = _th()
+        out = (torch.empty((T, Q.shape[1]), dtype=Q.dtype, device=Q.device),
+               None if K is None else torch.empty((T, K.shape[1]), dtype=Q.dtype, device=Q.device))
+        return out, Q.shape[1], 0 if K is None else K.shape[1]
+    if not isinstance(out, (tuple, list)) or len(out) != 2 or (out[1] is None) != (K is None):
+        _bad("PARTIR_E_SHAPE", f"out must hold ({names[0]}, {names[1]}), the second None without K")
+    return (tuple(out), _matrix(out[0], names[0], T, Q.shape[1], Q.dtype),
+            0 if K is None else _matrix(out[1], names[1], T, K.shape[1], Q.dtype))
+
+
+def rotary(Q, K, freqs, *, d_head: int, positions=None, S: Optional[int] = None, interleaved: bool = False,
+           magnitude: float = 1.0, inverse: bool = False, out=None, stream=None):
+    """Q and K with the first 2 * len(freqs) values of each head turned by
+    position * freqs.  Q [T, n_heads * d_head], K [T, n_kv_heads * d_head] or
+    None, bf16 or f32, views with a leading dim allowed; positions [T] int32 or
+    int64, or None: row t stands at t mod S (S None: at t).  interleaved: pairs
+    of neighbours, else of halves.  inverse: the gradient of the call without
+    it.  out: (Q', K') to write into, the inputs themselves allowed.  Returns
+    (Q', K')."""
+    T, Hq, Hk, rd, S, ldq, ldk = _rotary_args(Q, K, freqs, d_head, positions, S)
+    fresh = out is None
+    if not fresh:
+        out, ldqo, ldko = _rotary_out(out, ("Q'", "K'"), Q, K, T)
+    dev = _gpu_all(Q=Q, K=K, freqs=freqs, positions=positions, out=None if fresh else out)
+    if fresh:
+        out, ldqo, ldko = _rotary_out(None, None, Q, K, T)
+        _on_stream(stream, *out)
+    _launch(dev, lib().partir_rotary, _ptr(Q), _ptr(K), _ptr(out[0]), _ptr(out[1]), _ptr(freqs), _ptr(positions),
+            int(positions is not None and positions.dtype == _th().int64), T, S, Hq, Hk, d_head, rd, ldq, ldk, ldqo, ldko,
+            _dt(Q), int(interleaved), int(inverse), float(magnitude), stream=stream)
+    return out
+
+
+def qk_norm_rotary(Q, K, gq, gk, freqs, *, d_head: int, positions=None, S: Optional[int] = None,
+                   interleaved: bool = False, magnitude: float = 1.0, eps: float = 1e-6, out=None, stream=None):
+    """rotary of Q and K after an RMS norm of each head, g x / sqrt(mean(x^2) +
+    eps), in one pass.  gq, gk: gains [d_head] f32, or None for 1.  freqs None:
+    the norms alone.  Otherwise as rotary."""
+    T, Hq, Hk, rd, S, ldq, ldk = _rotary_args(Q, K, freqs, d_head, positions, S)
+    _opt(gq, "gq", (d_head,), _f32())
+    _opt(gk, "gk", (d_head,), _f32())
+    fresh = out is None
+    if not fresh:
+        out, ldqo, ldko = _rotary_out(out, ("Q'", "K'"), Q, K, T)
+    dev = _gpu_all(Q=Q, K=K, gq=gq, gk=gk, freqs=freqs, positions=positions, out=None if fresh else out)
+    if fresh:
+        out, ldqo, ldko = _rotary_out(None, None, Q, K, T)
+        _on_stream(stream, *out)
+    _launch(dev, lib().partir_qk_norm_rotary, _ptr(Q), _ptr(K), _ptr(gq), _ptr(gk), _ptr(out[0]), _ptr(out[1]),
+            _ptr(freqs), _ptr(positions), int(positions is not None and positions.dtype == _th().int64), T, S, Hq, Hk,
+            d_head, rd, ldq, ldk, ldqo, ldko, _dt(Q), int(interleaved), float(magnitude), float(eps), stream=stream)
+    return out
+
+
+def qk_norm_rotary_backward(Q, K, dQo, dKo, gq, gk, freqs, *, d_head: int, positions=None, S: Optional[int] = None,
+                            interleaved: bool = False, magnitude: float = 1.0, eps: float = 1e-6, out=None,
+                            gain_out=None, workspace=None, stream=None):
+    """Gradients (dQ, dK, dgq, dgk) of qk_norm_rotary for the cotangents dQo,
+    dKo of its outputs, from its inputs.  out: (dQ, dK) to write into (the
+    cotangents themselves allowed); gain_out: (dgq, dgk), f32 [d_head]."""
+    torch = _th()
+    T, Hq, Hk, rd, S, ldq, ldk = _rotary_args(Q, K, freqs, d_head, positions, S)
+    lddqo = _matrix(dQo, "dQo", T, Q.shape[1], Q.dtype)
+    if (dKo is None) != (K is None):
+        _bad("PARTIR_E_NULL", "dKo must be given exactly where K is")
+    lddko = 0 if K is None else _matrix(dKo, "dKo", T, K.shape[1], Q.dtype)
+    _opt(gq, "gq", (d_head,), _f32())
+    _opt(gk, "gk", (d_head,), _f32())
+    fresh, fresh_g = out is None, gain_out is None
+    if not fresh:
+        out, lddq, lddk = _rotary_out(out, ("dQ", "dK"), Q, K, T)
+    if not fresh_g:
+        if len(gain_out) != 2:
+            _bad("PARTIR_E_SHAPE", "gain_out must hold (dgq, dgk)")
+        _opt(gain_out[0], "dgq", (d_head,), _f32())
+        _opt(gain_out[1], "dgk", (d_head,), _f32())
+    dev = _gpu_all(Q=Q, K=K, dQo=dQo, dKo=dKo, gq=gq, gk=gk, freqs=freqs, positions=positions, out=None if fresh else out,
+                   gain_out=gain_out)
+    if fresh:
+        out, lddq, lddk = _rotary_out(None, None, Q, K, T)
+    if fresh_g:
+        gain_out = (torch.empty(d_head, dtype=torch.float32, device=dev),
+                    None if K is None else torch.empty(d_head, dtype=torch.float32, device=dev))
+    ws, wsb = _workspace(dev, workspace, lib().partir_qk_norm_rotary_backward_workspace, T, Hq, Hk, d_head, rd, _dt(Q))
+    _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()), *(gain_out if fresh_g else ()))
+    _launch(dev, lib().partir_qk_norm_rotary_backward, _ptr(Q), _ptr(K), _ptr(dQo), _ptr(dKo), _ptr(gq), _ptr(gk),
+            _ptr(out[0]), _ptr(out[1]), _ptr(gain_out[0]), _ptr(gain_out[1]), _ptr(freqs), _ptr(positions),
+            int(positions is not None and positions.dtype == torch.int64), T, S, Hq, Hk, d_head, rd, ldq, ldk, lddqo,
+            lddko, lddq, lddk, _dt(Q), int(interleaved), float(magnitude), float(eps), _ptr(ws), wsb, stream=stream)
+    return (*out, *gain_out)
+
+
+def _grad_arrays(tensors, name):
+    """Host arrays (pointers, counts, dtypes) of a list of dense tensors, and their device."""
+    torch = _th()
+    bf, f32 = torch.bfloat16, torch.float32
+    n = len(tensors)
+    ptrs, numel, dts = (ctypes.c_void_p * n)(), (I64 * n)(), (I32 * n)()
+    dev = None
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor):
+            _bad("PARTIR_E_NULL", f"{name}[{i}] must be a tensor")
+        dt = t.dtype
+        if dt is f32:
+            dts[i] = F32
+        elif dt is bf:
+            dts[i] = BF16
+        else:
+            _bad("PARTIR_E_DTYPE", f"{name}[{i}] has dtype {dt}, expected float32 or bfloat16")
+        if not t.is_contiguous():
+            _bad("PARTIR_E_LAYOUT", f"{name}[{i}] must be dense (contiguous)")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            _bad("PARTIR_E_LAYOUT", f"{name}[{i}] is on {t.device}, expected {dev}")
+        numel[i] = t.numel()
+        ptrs[i] = t.data_ptr()
+    return ptrs, numel, dts, dev
+
+
+def _grad_call(fn, tensors, norm, workspace, stream, outs=None, max_norm=None):
+    torch = _th()
+    tensors = list(tensors)
+    ptrs, numel, dts, dev = _grad_arrays(tensors, "tensors")
+    optrs = ptrs
+    if outs is not None:
+        outs = list(outs)
+        if len(outs) != len(tensors):
+            _bad("PARTIR_E_SHAPE", f"out must hold {len(tensors)} tensors")
+        optrs, onumel, odts, odev = _grad_arrays(outs, "out")
+        for i, (t, o) in enumerate(zip(tensors, outs)):
+            if t.shape != o.shape:
+                _bad("PARTIR_E_SHAPE", f"out[{i}] has shape {tuple(o.shape)}, expected {tuple(t.shape)}")
+            if dts[i] != odts[i]:
+                _bad("PARTIR_E_DTYPE", f"out[{i}] has dtype {o.dtype}, expected {t.dtype}")
+        if odev != dev:
+            _bad("PARTIR_E_LAYOUT", f"out is on {odev}, expected {dev}")
+    if norm is not None:
+        _req(norm, "norm", (), torch.float32, dev)
+        dev = norm.device
+    if dev is None:
+        dev = torch.device("cuda", torch.cuda.current_device())
+    if dev.type != "cuda":
+        _bad("PARTIR_E_LAYOUT", f"tensors must be on a GPU (got {dev})")
+    fresh = norm is None
+    if fresh:
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+    n = len(tensors)
+    ws, wsb = _workspace(dev, workspace, lib().partir_grad_norm_workspace, n)
+    _on_stream(stream, ws if workspace is None else None, norm if fresh else None)
+    if max_norm is None:
+        _launch(dev, fn, ptrs, numel, dts, n, _ptr(norm), _ptr(ws), wsb, stream=stream)
+    else:
+        _launch(dev, fn, ptrs, optrs, numel, dts, n, float(max_norm), _ptr(norm), _ptr(ws), wsb, stream=stream)
+    return norm
+
+
+def grad_norm(tensors, *, norm=None, workspace=None, stream=None):
+    """sqrt of the sum of all elements' squares over a list of dense f32 / bf16
+    tensors (views into flat buckets too), a 0-dim f32 tensor.  norm: where to
+    write it."""
+    return _grad_call(lib().partir_grad_norm, tensors, norm, workspace, stream)
+
+
+def clip_grad_norm(tensors, max_norm: float, *, out=None, norm=None, workspace=None, stream=None):
+    """Scales a list of gradients by max_norm / norm where their global norm
+    exceeds max_norm, in place or into the list `out`, and returns the norm (a
+    0-dim f32 tensor).  With an infinite or NaN element nothing is scaled."""
+    return _grad_call(lib().partir_clip_grad_norm, tensors, norm, workspace, stream, out, max_norm)
 
 
 # ---------------------------------------------------------------------------

@@ -1,0 +1,237 @@
+"""Refusals of the operators beside the nests (no GPU needed): the C ABI's
+checks, with pointers that are never dereferenced, and the binding's, with CPU
+tensors; and the frequencies of rotary positions, which the host computes."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators_oracle as OO
+from paper_2401_11202_amd import partir as P
+
+A, ODD, NULL = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10004), None
+bf, f32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _never_launch(monkeypatch):
+    monkeypatch.setenv("PARTIR_FAIL_LAUNCH", "1")
+
+
+def name(st):
+    return P.STATUS[st]
+
+
+def status(fn):
+    with pytest.raises(P.PartirError) as e:
+        fn()
+    return P.STATUS[e.value.status]
+
+
+# ---------------------------------------------------------------------------
+# rotary and norms
+# ---------------------------------------------------------------------------
+ROT = dict(Q=A, K=A, Qo=A, Ko=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128, ldqo=256,
+           ldko=128, dt=P.BF16, inter=0, inv=0, mag=1.0)
+
+
+def rotary(**kw):
+    a = dict(ROT, **kw)
+    return name(P.lib().partir_rotary(*(a[k] for k in ROT), None))
+
+
+BAD_ROT = [
+    (dict(Q=NULL), "PARTIR_E_NULL"), (dict(Ko=NULL), "PARTIR_E_NULL"), (dict(f=NULL), "PARTIR_E_NULL"),
+    (dict(T=-1), "PARTIR_E_SHAPE"), (dict(T=2 ** 31), "PARTIR_E_SHAPE"), (dict(S=0), "PARTIR_E_SHAPE"),
+    (dict(dh=60), "PARTIR_E_SHAPE"), (dict(dh=0), "PARTIR_E_SHAPE"), (dict(dh=264, rd=8), "PARTIR_E_SHAPE"),
+    (dict(rd=63), "PARTIR_E_SHAPE"), (dict(rd=66), "PARTIR_E_SHAPE"), (dict(rd=-2), "PARTIR_E_SHAPE"),
+    (dict(Hq=-1), "PARTIR_E_SHAPE"), (dict(Hq=2 ** 40), "PARTIR_E_SHAPE"), (dict(dt=7), "PARTIR_E_DTYPE"),
+    (dict(ldq=248), "PARTIR_E_LAYOUT"), (dict(ldq=260), "PARTIR_E_LAYOUT"), (dict(ldk=2 ** 25), "PARTIR_E_SHAPE"),
+    (dict(Q=ODD), "PARTIR_E_LAYOUT"), (dict(Ko=ODD), "PARTIR_E_LAYOUT"), (dict(f=ODD), "PARTIR_E_LAYOUT"),
+    (dict(pos=ODD, p64=1), "PARTIR_E_LAYOUT"), (dict(mag=float("nan")), "PARTIR_E_UNSUPPORTED"),
+    (dict(mag=float("inf")), "PARTIR_E_UNSUPPORTED"),
+]
+GOOD_ROT = [dict(), dict(pos=A, p64=1, S=0), dict(pos=ODD), dict(Hk=0, K=NULL, Ko=NULL, ldk=0, ldko=0), dict(rd=0, f=NULL),
+            dict(rd=2), dict(dt=P.F32), dict(ldq=264, ldko=2 ** 24)]
+
+
+@pytest.mark.parametrize("kw,want", BAD_ROT)
+def test_rotary_refusals(kw, want):
+    assert rotary(**kw) == want
+    assert P.lib().partir_last_error().decode().startswith(want)
+
+
+@pytest.mark.parametrize("kw", GOOD_ROT)
+def test_rotary_accepts(kw):
+    assert rotary(**kw) == "PARTIR_E_HIP"          # reached the launch, which is forced to fail
+
+
+def test_nothing_to_do_launches_nothing():
+    assert rotary(T=0, Q=NULL, K=NULL, Qo=NULL, Ko=NULL, f=NULL) == "PARTIR_OK"
+    assert rotary(Hq=0, Hk=0, Q=NULL, K=NULL, Qo=NULL, Ko=NULL) == "PARTIR_OK"
+
+
+NORM = dict(Q=A, K=A, gq=A, gk=A, Qo=A, Ko=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128,
+            ldqo=256, ldko=128, dt=P.BF16, inter=0, mag=1.0, eps=1e-6)
+BWD = dict(Q=A, K=A, dQo=A, dKo=A, gq=A, gk=A, dQ=A, dK=A, dgq=A, dgk=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64,
+           rd=64, ldq=256, ldk=128, lddqo=256, lddko=128, lddq=256, lddk=128, dt=P.BF16, inter=0, mag=1.0, eps=1e-6, ws=A,
+           wsb=1 << 24)
+
+
+def norm(**kw):
+    a = dict(NORM, **kw)
+    return name(P.lib().partir_qk_norm_rotary(*(a[k] for k in NORM), None))
+
+
+def bwd(**kw):
+    a = dict(BWD, **kw)
+    return name(P.lib().partir_qk_norm_rotary_backward(*(a[k] for k in BWD), None))
+
+
+def test_qk_norm_refusals():
+    for kw, want in BAD_ROT:
+        assert norm(**kw) == want, kw
+    assert norm(gq=ODD) == "PARTIR_E_LAYOUT" and norm(eps=-1.0) == "PARTIR_E_UNSUPPORTED"
+    assert norm(eps=float("nan")) == "PARTIR_E_UNSUPPORTED"
+    for kw in ({}, dict(gq=NULL, gk=NULL), dict(eps=0.0), dict(rd=0, f=NULL)):
+        assert norm(**kw) == "PARTIR_E_HIP", kw
+
+
+def test_qk_norm_backward_refusals():
+    need = P.lib().partir_qk_norm_rotary_backward_workspace(16, 4, 2, 64, 64, P.BF16)
+    assert 0 < need <= 1 << 24
+    for kw, want in ((dict(dQo=NULL), "PARTIR_E_NULL"), (dict(dK=NULL), "PARTIR_E_NULL"), (dict(lddqo=8), "PARTIR_E_LAYOUT"),
+                     (dict(lddqo=-8), "PARTIR_E_LAYOUT"), (dict(dQo=ODD), "PARTIR_E_LAYOUT"), (dict(lddk=130), "PARTIR_E_LAYOUT"),
+                     (dict(wsb=need - 1), "PARTIR_E_WORKSPACE"), (dict(ws=NULL), "PARTIR_E_NULL"), (dict(ws=ODD), "PARTIR_E_LAYOUT"),
+                     (dict(dgq=ctypes.c_void_p(0x10002)), "PARTIR_E_LAYOUT"), (dict(eps=-1e-9), "PARTIR_E_UNSUPPORTED"),
+                     (dict(wsb=need), "PARTIR_E_HIP"), (dict(dgq=NULL, dgk=NULL), "PARTIR_E_HIP"),
+                     (dict(T=0, ws=NULL, wsb=0, dgq=NULL, dgk=NULL), "PARTIR_OK"), (dict(T=0, ws=NULL, wsb=0), "PARTIR_E_HIP")):
+        assert bwd(**kw) == want, kw
+    bad = ctypes.c_size_t(-1).value
+    for a in ((-1, 4, 2, 64, 64, P.BF16), (16, 4, 2, 60, 60, P.BF16), (16, 4, 2, 64, 66, P.BF16), (16, -4, 2, 64, 64, P.BF16),
+              (16, 4, 2, 64, 64, 9)):
+        assert P.lib().partir_qk_norm_rotary_backward_workspace(*a) == bad
+    assert P.lib().partir_qk_norm_rotary_backward_workspace(0, 4, 2, 64, 64, P.BF16) == 0
+
+
+@pytest.mark.parametrize("T,Hq,Hk,dh,rd", [(1, 1, 0, 8, 8), (100000, 64, 64, 256, 2), (2 ** 30, 1, 1, 64, 64), (7, 2 ** 16, 1, 128, 128)])
+def test_qk_norm_backward_workspace_is_what_the_call_needs(T, Hq, Hk, dh, rd):
+    for dt in (P.BF16, P.F32):
+        need = P.lib().partir_qk_norm_rotary_backward_workspace(T, Hq, Hk, dh, rd, dt)
+        a = dict(T=T, Hq=Hq, Hk=Hk, dh=dh, rd=rd, ldq=Hq * dh, ldk=Hk * dh, lddqo=Hq * dh, lddko=Hk * dh, lddq=Hq * dh,
+                 lddk=Hk * dh, dt=dt)
+        assert bwd(wsb=need, **a) == "PARTIR_E_HIP" and bwd(wsb=need - 1, **a) == "PARTIR_E_WORKSPACE"
+        assert need <= 1024 * 2 * 256 * 4
+
+
+@pytest.mark.parametrize("scaling,kw", [(None, {}), ("linear", dict(factor=4.0)), ("base", dict(factor=8.0)),
+                                        ("parts", dict(factor=16.0, original_length=4096)),
+                                        ("parts", dict(factor=2.0, original_length=64, slow_turns=0.25, fast_turns=3.0))])
+@pytest.mark.parametrize("rd", [2, 20, 64, 128, 256])
+def test_rotary_frequencies(scaling, kw, rd):
+    if scaling == "base" and rd == 2:
+        assert status(lambda: P.rotary_frequencies(rd, scaling=scaling, device="cpu", **kw)) == "PARTIR_E_UNSUPPORTED"
+        return
+    got = P.rotary_frequencies(rd, base=50000.0, scaling=scaling, device="cpu", **kw).numpy()
+    o = {"slow_turns": "slow", "fast_turns": "fast"}
+    ref = OO.frequencies(rd, 50000.0, scaling, **{o.get(k, k): v for k, v in kw.items()})
+    assert got.dtype == np.float64 and np.abs(got - ref).max() <= 1e-15 * 8
+    if scaling == "base":       # the slowest pair is as with linear scaling, the fastest unchanged
+        lin = OO.frequencies(rd, 50000.0, "linear", kw["factor"])
+        assert got[0] == 1.0 and abs(got[-1] / lin[-1] - 1) < 1e-12
+    if scaling == "parts":      # between the two, fast pairs kept and slow ones divided
+        plain = OO.frequencies(rd, 50000.0)
+        assert (got <= plain * (1 + 1e-15)).all() and (got >= plain / kw["factor"] * (1 - 1e-15)).all()
+
+
+def test_rotary_frequencies_refusals():
+    for kw in (dict(base=1.0), dict(base=float("inf")), dict(scaling="linear", factor=0.5), dict(scaling="nope"),
+               dict(scaling="parts", factor=2.0), dict(scaling="parts", factor=2.0, original_length=9, slow_turns=2.0, fast_turns=1.0)):
+        assert status(lambda: P.rotary_frequencies(64, device="cpu", **kw)) == "PARTIR_E_UNSUPPORTED", kw
+    for rd in (63, 258):
+        assert status(lambda: P.rotary_frequencies(rd, device="cpu")) == "PARTIR_E_SHAPE"
+
+
+def test_rotary_binding_checks():
+    q, k, f = torch.zeros(16, 256, dtype=bf), torch.zeros(16, 128, dtype=bf), torch.zeros(32, dtype=torch.float64)
+    call = lambda *a, **kw: status(lambda: P.rotary(*a, **{**dict(d_head=64), **kw}))  # noqa: E731
+    assert call(q, k, f) == "PARTIR_E_LAYOUT"                                   # all correct, but on the CPU
+    assert call(q, k, f, d_head=48) == "PARTIR_E_SHAPE"
+    assert call(q, k, f, d_head=0) == "PARTIR_E_SHAPE"
+    assert call(q, k[:8], f) == "PARTIR_E_SHAPE"
+    assert call(q, k.float(), f) == "PARTIR_E_DTYPE"
+    assert call(q.half(), None, f) == "PARTIR_E_DTYPE"
+    assert call(q, k, f.float()) == "PARTIR_E_DTYPE"
+    assert call(q.t(), None, f, d_head=8) == "PARTIR_E_LAYOUT"
+    assert call(q, k, f, positions=torch.zeros(15, dtype=torch.int64)) == "PARTIR_E_SHAPE"
+    assert call(q, k, f, positions=torch.zeros(16)) == "PARTIR_E_DTYPE"
+    assert call(q, k, f, out=(q, None)) == "PARTIR_E_SHAPE"
+    assert call(q, k, f, out=(q, q)) == "PARTIR_E_SHAPE"
+    assert call(q, k, f, out=(q, k.float())) == "PARTIR_E_DTYPE"
+    g = torch.zeros(64)
+    assert status(lambda: P.qk_norm_rotary(q, k, g[:32], g, f, d_head=64)) == "PARTIR_E_SHAPE"
+    assert status(lambda: P.qk_norm_rotary(q, k, g, g.to(bf), f, d_head=64)) == "PARTIR_E_DTYPE"
+    assert status(lambda: P.qk_norm_rotary(q, k, g, g, f, d_head=64)) == "PARTIR_E_LAYOUT"
+    b = lambda *a, **kw: status(lambda: P.qk_norm_rotary_backward(*a, **{**dict(d_head=64), **kw}))  # noqa: E731
+    assert b(q, k, q, None, g, g, f) == "PARTIR_E_NULL"
+    assert b(q, k, q, q, g, g, f) == "PARTIR_E_SHAPE"
+    assert b(q, k, q, k, g, g, f, gain_out=(g, g.to(bf))) == "PARTIR_E_DTYPE"
+    assert b(q, k, q, k, g, g, f) == "PARTIR_E_LAYOUT"
+
+
+# ---------------------------------------------------------------------------
+# norm of gradients
+# ---------------------------------------------------------------------------
+def clip(ptrs, numel, dts, out=None, max_norm=1.0, norm=A, ws=A, wsb=1 << 24, n=None):
+    k = len(ptrs)
+    return name(P.lib().partir_clip_grad_norm((ctypes.c_void_p * k)(*ptrs), (ctypes.c_void_p * k)(*(out or ptrs)),
+                                              (ctypes.c_int64 * k)(*numel), (ctypes.c_int * k)(*dts), k if n is None else n,
+                                              max_norm, norm, ws, wsb, None))
+
+
+def test_clip_refusals():
+    one = ([0x20000], [100], [P.F32])
+    assert clip(*one) == "PARTIR_E_HIP"
+    assert clip([0x20002], [100], [P.F32]) == "PARTIR_E_LAYOUT"
+    assert clip([0x20002], [100], [P.BF16]) == "PARTIR_E_HIP"
+    assert clip([0x20001], [100], [P.BF16]) == "PARTIR_E_LAYOUT"
+    assert clip([None], [100], [P.F32]) == "PARTIR_E_NULL"
+    assert clip([None], [0], [P.F32]) == "PARTIR_E_HIP"                         # empty: the norm 0 is written
+    assert clip([0x20000], [-1], [P.F32]) == "PARTIR_E_SHAPE"
+    assert clip([0x20000], [1 << 41], [P.F32]) == "PARTIR_E_SHAPE"
+    assert clip([0x20000], [100], [3]) == "PARTIR_E_DTYPE"
+    assert clip(*one, max_norm=-1.0) == "PARTIR_E_UNSUPPORTED"
+    assert clip(*one, max_norm=float("nan")) == "PARTIR_E_UNSUPPORTED"
+    assert clip(*one, max_norm=float("inf")) == "PARTIR_E_HIP"
+    assert clip(*one, norm=NULL) == "PARTIR_E_NULL"
+    assert clip(*one, n=-1) == "PARTIR_E_SHAPE"
+    need = P.lib().partir_grad_norm_workspace(1)
+    assert clip(*one, wsb=need) == "PARTIR_E_HIP" and clip(*one, wsb=need - 1) == "PARTIR_E_WORKSPACE"
+    assert clip(*one, ws=ODD) == "PARTIR_E_LAYOUT" and clip(*one, ws=NULL) == "PARTIR_E_NULL"
+    assert P.lib().partir_grad_norm_workspace(-1) == ctypes.c_size_t(-1).value
+    assert P.lib().partir_grad_norm_workspace(0) == 0
+
+
+def test_overlapping_outputs_are_refused():
+    two = [P.F32, P.F32]
+    assert clip([0x20000, 0x20000], [100, 100], two) == "PARTIR_E_LAYOUT"       # the same tensor twice
+    assert clip([0x20190, 0x20000], [100, 101], two) == "PARTIR_E_LAYOUT"       # one value shared, in either order
+    assert clip([0x20000, 0x20190], [101, 100], two) == "PARTIR_E_LAYOUT"
+    assert clip([0x20190, 0x20000], [100, 100], two) == "PARTIR_E_HIP"          # neighbours
+    assert clip([0x20000, 0x20000], [100, 100], two, out=[0x30000, 0x40000]) == "PARTIR_E_HIP"   # read twice, written apart
+    assert clip([0x20000, 0x30000], [100, 100], two, out=[0x30000, 0x40000]) == "PARTIR_E_LAYOUT"
+    assert clip([0x20000], [100], [P.F32], out=[0x20004]) == "PARTIR_E_LAYOUT"  # its own input, shifted
+    assert clip([0x20000, 0x20000], [100, 0], two) == "PARTIR_E_HIP"
+
+
+def test_clip_binding_checks():
+    t = torch.zeros(8)
+    assert status(lambda: P.grad_norm([t])) == "PARTIR_E_LAYOUT"                # on the CPU
+    assert status(lambda: P.grad_norm([t, None])) == "PARTIR_E_NULL"
+    assert status(lambda: P.grad_norm([t.half()])) == "PARTIR_E_DTYPE"
+    assert status(lambda: P.grad_norm([torch.zeros(4, 4).t()[:2]])) == "PARTIR_E_LAYOUT"
+    assert status(lambda: P.clip_grad_norm([t], 1.0, out=[])) == "PARTIR_E_SHAPE"
+    assert status(lambda: P.clip_grad_norm([t], 1.0, out=[t[:4]])) == "PARTIR_E_SHAPE"
+    assert status(lambda: P.clip_grad_norm([t], 1.0, out=[t.to(bf)])) == "PARTIR_E_DTYPE"
+    assert status(lambda: P.clip_grad_norm([t], 1.0, norm=torch.zeros(1))) == "PARTIR_E_SHAPE"
