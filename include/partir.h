@@ -558,6 +558,48 @@ int partir_qk_norm_rotary_backward(const void* Q, const void* K, const void* dQo
 size_t partir_qk_norm_rotary_backward_workspace(int64_t T, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
                                                 int64_t rotary_dim, int dtype);
 
+/* Attention to another sequence: O = softmax(scale Q K^T) V for Sq queries and
+ * Sk keys of each of B sequences, no causal mask.
+ * Q, O: [B*Sq, n_heads * d_head] and K, V: [B*Sk, n_kv_heads * d_head] bf16,
+ * sequence-major, leading dims ldq, ldo, ldk, ldv; n_kv_heads divides n_heads
+ * and query head h reads key head h / (n_heads / n_kv_heads).  Sq and Sk may be
+ * any size, 1 and 0 among them.
+ * k_lens: [B] int32 on the device, the valid keys of each sequence (clamped to
+ * 0..Sk), or NULL: Sk.  Keys behind them are not read, whatever they hold.  A
+ * query without keys gets 0.
+ * scale <= 0 selects 1/sqrt(d_head).  d_head == 128.
+ * With few queries the keys are evaluated in parts that are joined in order by
+ * the combiner of partir_attention; the parts are the workspace (0 without).
+ * Errors: E_NULL, E_SHAPE, E_DIVISIBILITY (n_kv_heads does not divide n_heads),
+ * E_LAYOUT, E_WORKSPACE, E_UNSUPPORTED (scale), E_HIP. */
+int partir_cross_attention(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t Sq, int64_t Sk,
+                           int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk, int64_t ldv,
+                           int64_t ldo, const int32_t* k_lens, float scale, void* ws, size_t ws_bytes, void* stream);
+size_t partir_cross_attention_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                        int64_t d_head);
+
+/* The forward of a training step: also the base-2 log-sum-exp of every query's
+ * scaled scores, lse [B*Sq, n_heads] fp32 (as partir_attention_train; -inf for
+ * a query without keys).  Same workspace. */
+int partir_cross_attention_train(const void* Q, const void* K, const void* V, void* O, float* lse, int64_t B, int64_t Sq,
+                                 int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                 int64_t ldv, int64_t ldo, const int32_t* k_lens, float scale, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* Gradients of partir_cross_attention for the cotangent dO of O, from the
+ * forward's O and lse (formulas as partir_attention_backward).  dQ as Q; dK and
+ * dV as K and V, summed over the query heads of a key head; keys behind
+ * k_lens get zeros.  Every gradient is summed in a fixed order, without
+ * atomics.  Workspace: the rowsums of dO * O and, where the queries or keys are
+ * few, fp32 parts of the gradients. */
+int partir_cross_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                                    const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
+                                    int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                    int64_t ldv, int64_t ldo, int64_t lddo, int64_t lddq, int64_t lddk, int64_t lddv,
+                                    const int32_t* k_lens, float scale, void* ws, size_t ws_bytes, void* stream);
+size_t partir_cross_attention_backward_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                                 int64_t d_head);
+
 /* Global norm of n tensors, sqrt of the sum of every element's square, into
  * norm[0] (device, float32).  tensors, numel, dtypes: HOST arrays of device
  * pointers, element counts and partir_dtypes (F32 and BF16 may be mixed); a
@@ -616,6 +658,12 @@ int partir_plan_decoder_layer_sharded(int64_t B, int64_t S, int64_t D, int64_t n
 int partir_plan_decoder_layer(int64_t B, int64_t S, int64_t D, int64_t n_heads,
                               int64_t d_head, int64_t F, int R_batch, int R_model,
                               partir_plan_info* info);
+/* n_virtual_shards: the parts of the key axis (backward: the larger count of
+ * parts of its two axes).  flops: with every key valid.  No plan text. */
+int partir_plan_cross_attention(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
+                                partir_plan_info* info);
+int partir_plan_cross_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                         int64_t d_head, partir_plan_info* info);
 
 /* Human-readable shard table of the last plan built on this thread
  * (views, offsets, tile grid and #sum realisation per launch).  The string is

@@ -40,6 +40,71 @@ hipError_t launch_qk_norm_backward(const RotaryParams& p, bool bf16, bool interl
 // dg[i][d] = sum over the parts, in order (a NULL dg[i] is skipped)
 hipError_t launch_gain_reduce(const float* dgpart, int parts, int dh, float* dgq, float* dgk, hipStream_t s);
 
+// ---- attention to another sequence (cross_attention.hip) --------------------
+// d_head = 128, bf16.  Query head h reads key head h / G, G = Hq / Hk.  The
+// G Sq query rows of a (sequence, key head) are numbered i = s G + g (position
+// s, head kvh G + g) and tiled together, so that a single token's shared heads
+// fill one tile.
+struct CrossParams {
+  const uint16_t* Q;
+  const uint16_t* K;
+  const uint16_t* V;
+  uint16_t* O;
+  float* lse;              // [B Sq][Hq] base-2 log-sum-exp of the scaled scores, or NULL
+  const int32_t* lens;     // [B] valid keys of each sequence, or NULL: Sk
+  int64_t ldq, ldk, ldv, ldo;
+  int B, Sq, Sk, Hq, Hk, G;
+  float scale_log2;        // scale * log2(e)
+  // key axis in nsplit parts (see cross_range): unnormalised outputs and
+  // softmax statistics of the parts, joined by the combine launch
+  int nsplit;
+  float* Opart;            // [nsplit][B Sq Hq][128]
+  float2* MLpart;          // [nsplit][B Sq Hq] (m, l)
+};
+// The kernel of a launch: waves over queries and key groups of a workgroup,
+// keys of a block, parts of the key axis.
+struct CrossChoice {
+  int qw, kg, block, nsplit;
+};
+CrossChoice cross_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
+hipError_t launch_cross_attention(const CrossParams& p, const CrossChoice& c, hipStream_t s);
+hipError_t launch_cross_combine(const CrossParams& p, hipStream_t s);
+
+// Keys of part `split` of nsplit of a sequence with len keys: whole blocks of
+// 64, shared out evenly; parts behind the last block are empty.
+struct CrossRange {
+  int begin, end, parts;   // [begin, end), and how many parts hold keys
+};
+__host__ __device__ __forceinline__ CrossRange cross_range(int len, int nsplit, int split) {
+  const int nblk = (len + 63) / 64, per = (nblk + nsplit - 1) / nsplit;
+  CrossRange r;
+  r.parts = per ? (nblk + per - 1) / per : 0;
+  const long long b = (long long)split * per * 64, e = b + (long long)per * 64;
+  r.begin = (int)(b < len ? b : len);
+  r.end = (int)(e < len ? e : len);
+  return r;
+}
+
+// Gradients (cross_attention_bwd.hip).  The dq pass takes the key axis in
+// q_parts parts, the dk / dv passes the query axis in k_parts; more than one
+// part means fp32 partials for an ordered reduction.
+struct CrossBwdParams {
+  const uint16_t *Q, *K, *V, *O, *dO;
+  const float* lse;
+  float* Dstat;            // [B Sq][Hq] rowsums of dO * O, from the dq pass for the dk pass
+  uint16_t *dQ, *dK, *dV;
+  float *dQpart, *dKpart, *dVpart;   // [parts][rows][heads * 128]
+  const int32_t* lens;
+  int64_t ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv;
+  int B, Sq, Sk, Hq, Hk, G;
+  int q_parts, k_parts;
+  float scale, scale_log2;
+};
+// (q_parts, k_parts)
+void cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, int* q_parts, int* k_parts);
+enum CrossBwdPass { CROSS_DQ, CROSS_DV, CROSS_DK };
+hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s);
+
 // ---- global norm of many tensors (grad_norm.hip) ----------------------------
 constexpr int kGradTensors = 112;             // tensors of one launch's table
 constexpr int kGradChunkBytes = 32768;        // bytes of one step of a workgroup

@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "../../include/partir.h"
+#include "kernels.h"
 #include "operators.h"
 
 namespace partir {
@@ -269,6 +270,128 @@ int run_grads(const void* const* in, void* const* out, const int64_t* numel, con
   return PARTIR_OK;
 }
 
+// ---------------------------------------------------------------------------
+// attention to another sequence
+// ---------------------------------------------------------------------------
+struct CrossSizes {
+  int64_t B, Sq, Sk, Hq, Hk, dh;
+};
+
+int validate_cross(const CrossSizes& z) {
+  if (z.B < 0 || z.Sq < 0 || z.Sk < 0 || z.B > kMaxSize || z.Sq > kMaxSize || z.Sk > kMaxSize)
+    return fail(PARTIR_E_SHAPE, "B = %lld, Sq = %lld, Sk = %lld", (long long)z.B, (long long)z.Sq, (long long)z.Sk);
+  if (z.dh != 128) return fail(PARTIR_E_SHAPE, "d_head = %lld, only 128 is provided", (long long)z.dh);
+  if (z.Hq < 1 || z.Hk < 1 || z.Hq * z.dh > kMaxLd || z.Hk > z.Hq)
+    return fail(PARTIR_E_SHAPE, "n_heads = %lld, n_kv_heads = %lld", (long long)z.Hq, (long long)z.Hk);
+  if (z.Hq % z.Hk)
+    return fail(PARTIR_E_DIVISIBILITY, "n_kv_heads = %lld does not divide n_heads = %lld", (long long)z.Hk, (long long)z.Hq);
+  const int64_t G = z.Hq / z.Hk;
+  if (z.Sq * G > kMaxSize || z.B * z.Sq > kMaxSize || z.B * z.Sk > kMaxSize)
+    return fail(PARTIR_E_SHAPE, "more than 2^30 query rows of a key head, queries or keys");
+  // workgroups of any launch (parts are asked for only below one a CU), and the threads of the join
+  if (z.B * z.Hk * std::max(cdiv(z.Sq * G, 32), cdiv(z.Sk, 128)) > ((int64_t)1 << 30) || z.B * z.Sq * z.Hq > ((int64_t)1 << 33))
+    return fail(PARTIR_E_SHAPE, "more than 2^30 workgroups");
+  return PARTIR_OK;
+}
+
+int check_lens(const void* lens) {
+  return aligned(lens, 4) ? PARTIR_OK : fail(PARTIR_E_LAYOUT, "k_lens must be 4-byte aligned");
+}
+
+// scale <= 0 selects 1 / sqrt(d_head)
+int resolve_scale(float& scale, int64_t dh) {
+  if (std::isnan(scale)) return fail(PARTIR_E_UNSUPPORTED, "scale is NaN");
+  if (scale <= 0.0f) scale = 1.0f / std::sqrt((float)dh);
+  if (scale < 1e-30f || scale > 1e30f) return fail(PARTIR_E_UNSUPPORTED, "scale outside 1e-30 .. 1e30");
+  return PARTIR_OK;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct CrossPlan {
+  CrossChoice c;
+  size_t o_bytes = 0, ml_bytes = 0;
+  size_t ws() const { return o_bytes + ml_bytes; }
+};
+CrossPlan plan_cross(const CrossSizes& z) {
+  CrossPlan p;
+  p.c = cross_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk);
+  if (p.c.nsplit > 1) {
+    const size_t rows = (size_t)p.c.nsplit * z.B * z.Sq * z.Hq;
+    p.o_bytes = align_up(rows * z.dh * 4);
+    p.ml_bytes = align_up(rows * 8);
+  }
+  return p;
+}
+
+int run_cross(const void* Q, const void* K, const void* V, void* O, float* lse, const CrossSizes& z, int64_t ldq, int64_t ldk,
+              int64_t ldv, int64_t ldo, const int32_t* lens, float scale, void* ws, size_t ws_bytes, void* stream) {
+  if (int st = validate_cross(z)) return st;
+  if (int st = resolve_scale(scale, z.dh)) return st;
+  const int64_t Tq = z.B * z.Sq, Tk = z.B * z.Sk;
+  if (int st = check_matrix("Q", Q, Tq, z.Hq * z.dh, ldq, 2)) return st;
+  if (int st = check_matrix("K", K, Tq ? Tk : 0, z.Hk * z.dh, ldk, 2)) return st;
+  if (int st = check_matrix("V", V, Tq ? Tk : 0, z.Hk * z.dh, ldv, 2)) return st;
+  if (int st = check_matrix("O", O, Tq, z.Hq * z.dh, ldo, 2)) return st;
+  if (int st = check_lens(lens)) return st;
+  if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
+  if (Tq == 0) return PARTIR_OK;
+  const CrossPlan plan = plan_cross(z);
+  if (int st = check_ws(plan.ws(), ws, ws_bytes)) return st;
+  CrossParams p{};
+  p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)K; p.V = (const uint16_t*)V; p.O = (uint16_t*)O;
+  p.lse = lse; p.lens = lens;
+  p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo;
+  p.B = (int)z.B; p.Sq = (int)z.Sq; p.Sk = (int)z.Sk; p.Hq = (int)z.Hq; p.Hk = (int)z.Hk; p.G = (int)(z.Hq / z.Hk);
+  p.scale_log2 = scale * kLog2e;
+  p.nsplit = plan.c.nsplit;
+  if (p.nsplit > 1) {
+    p.Opart = (float*)ws;
+    p.MLpart = (float2*)((char*)ws + plan.o_bytes);
+  }
+  if (int st = begin_launches()) return st;
+  if (int st = launched(launch_cross_attention(p, plan.c, (hipStream_t)stream), "cross_attention")) return st;
+  if (p.nsplit == 1) return PARTIR_OK;
+  return launched(launch_cross_combine(p, (hipStream_t)stream), "cross_combine");
+}
+
+struct CrossBwdPlan {
+  int q_parts = 1, k_parts = 1;
+  size_t d_bytes = 0, q_bytes = 0, k_bytes = 0;   // k_bytes: of dK's and of dV's partials each
+  size_t ws() const { return d_bytes + q_bytes + 2 * k_bytes; }
+};
+CrossBwdPlan plan_cross_bwd(const CrossSizes& z) {
+  CrossBwdPlan p;
+  if (z.B == 0) return p;
+  cross_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk, &p.q_parts, &p.k_parts);
+  p.d_bytes = align_up((size_t)z.B * z.Sq * z.Hq * 4);
+  if (p.q_parts > 1) p.q_bytes = align_up((size_t)p.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
+  if (p.k_parts > 1) p.k_bytes = align_up((size_t)p.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
+  return p;
+}
+
+// out (bf16) = sum over the parts, in order
+hipError_t reduce_parts(const float* partial, int parts, int64_t rows, int64_t cols, void* out, int64_t ld, hipStream_t s) {
+  ReduceParams r{};
+  r.partial = partial;
+  r.part_ld = cols;
+  r.part_stride = rows * cols;
+  r.R = parts; r.M = (int)rows; r.N = (int)cols;
+  r.C = out; r.ldc = ld;
+  r.out_bf16 = 1;
+  return launch_splitk_reduce(r, s);
+}
+
+void fill_info(partir_plan_info* info, int shards, int launches, size_t ws, double flops) {
+  info->n_virtual_shards = shards;
+  info->n_tile_loops = 1;                       // the heads
+  info->n_sum_loops = info->n_sum_splitk = shards > 1;
+  info->n_launches = launches;
+  info->reserved = 0;
+  info->workspace_bytes = ws;
+  info->flops = flops;
+}
+
 }  // namespace
 }  // namespace partir
 
@@ -380,6 +503,119 @@ int partir_qk_norm_rotary_backward(const void* Q, const void* K, const void* dQo
       if (int st = launched(launch_qk_norm_backward(p, dtype == PARTIR_BF16, interleaved != 0, s), "qk_norm_backward")) return st;
     if (!dgq && !dgk) return PARTIR_OK;
     return launched(launch_gain_reduce(p.dgpart, empty ? 0 : p.grid, p.dh, dgq, dgk, s), "gain_reduce");
+  });
+}
+
+// ---- attention to another sequence ------------------------------------------------
+size_t partir_cross_attention_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                        int64_t d_head) {
+  const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+  if (guarded([&]() -> int { return validate_cross(z); })) return (size_t)-1;
+  return plan_cross(z).ws();
+}
+
+int partir_plan_cross_attention(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
+                                partir_plan_info* info) {
+  return guarded([&]() -> int {
+    const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+    if (int st = validate_cross(z)) return st;
+    if (!info) return fail(PARTIR_E_NULL, "info must be non-NULL");
+    const CrossPlan p = plan_cross(z);
+    fill_info(info, p.c.nsplit, B * Sq == 0 ? 0 : p.c.nsplit > 1 ? 2 : 1, p.ws(),
+              4.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
+    return PARTIR_OK;
+  });
+}
+
+int partir_cross_attention(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t Sq, int64_t Sk,
+                           int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk, int64_t ldv,
+                           int64_t ldo, const int32_t* k_lens, float scale, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    return run_cross(Q, K, V, O, nullptr, {B, Sq, Sk, n_heads, n_kv_heads, d_head}, ldq, ldk, ldv, ldo, k_lens, scale, ws,
+                     ws_bytes, stream);
+  });
+}
+
+int partir_cross_attention_train(const void* Q, const void* K, const void* V, void* O, float* lse, int64_t B, int64_t Sq,
+                                 int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                 int64_t ldv, int64_t ldo, const int32_t* k_lens, float scale, void* ws, size_t ws_bytes,
+                                 void* stream) {
+  return guarded([&]() -> int {
+    if (B > 0 && Sq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
+    return run_cross(Q, K, V, O, lse, {B, Sq, Sk, n_heads, n_kv_heads, d_head}, ldq, ldk, ldv, ldo, k_lens, scale, ws,
+                     ws_bytes, stream);
+  });
+}
+
+size_t partir_cross_attention_backward_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                                 int64_t d_head) {
+  const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+  if (guarded([&]() -> int { return validate_cross(z); })) return (size_t)-1;
+  return plan_cross_bwd(z).ws();
+}
+
+int partir_plan_cross_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                         int64_t d_head, partir_plan_info* info) {
+  return guarded([&]() -> int {
+    const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+    if (int st = validate_cross(z)) return st;
+    if (!info) return fail(PARTIR_E_NULL, "info must be non-NULL");
+    const CrossBwdPlan p = plan_cross_bwd(z);
+    const int nq = B * Sq ? 1 + (p.q_parts > 1) : 0, nk = B * Sk ? 2 * (1 + (p.k_parts > 1)) : 0;
+    fill_info(info, std::max(p.q_parts, p.k_parts), nq + nk, p.ws(),
+              10.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
+    return PARTIR_OK;
+  });
+}
+
+int partir_cross_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                                    const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
+                                    int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                    int64_t ldv, int64_t ldo, int64_t lddo, int64_t lddq, int64_t lddk, int64_t lddv,
+                                    const int32_t* k_lens, float scale, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+    if (int st = validate_cross(z)) return st;
+    if (int st = resolve_scale(scale, d_head)) return st;
+    const int64_t Tq = B * Sq, Tk = B * Sk, cq = n_heads * d_head, ck = n_kv_heads * d_head;
+    const struct { const char* name; const void* p; int64_t rows, cols, ld; } all[] = {
+        {"Q", Q, Tq, cq, ldq}, {"K", K, Tk, ck, ldk}, {"V", V, Tk, ck, ldv}, {"O", O, Tq, cq, ldo}, {"dO", dO, Tq, cq, lddo},
+        {"dQ", dQ, Tq, cq, lddq}, {"dK", dK, Tk, ck, lddk}, {"dV", dV, Tk, ck, lddv}};
+    for (const auto& m : all)
+      if (int st = check_matrix(m.name, m.p, m.rows, m.cols, m.ld, 2)) return st;
+    if (int st = check_lens(k_lens)) return st;
+    if (Tq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
+    if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
+    if (Tq == 0 && Tk == 0) return PARTIR_OK;
+    const CrossBwdPlan plan = plan_cross_bwd(z);
+    if (int st = check_ws(plan.ws(), ws, ws_bytes)) return st;
+    CrossBwdParams p{};
+    p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)K; p.V = (const uint16_t*)V; p.O = (const uint16_t*)O;
+    p.dO = (const uint16_t*)dO; p.lse = lse; p.lens = k_lens;
+    p.dQ = (uint16_t*)dQ; p.dK = (uint16_t*)dK; p.dV = (uint16_t*)dV;
+    char* base = (char*)ws;
+    p.Dstat = (float*)base;
+    p.dQpart = (float*)(base + plan.d_bytes);
+    p.dKpart = (float*)(base + plan.d_bytes + plan.q_bytes);
+    p.dVpart = (float*)(base + plan.d_bytes + plan.q_bytes + plan.k_bytes);
+    p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.ldg = lddo; p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
+    p.B = (int)B; p.Sq = (int)Sq; p.Sk = (int)Sk; p.Hq = (int)n_heads; p.Hk = (int)n_kv_heads; p.G = (int)(n_heads / n_kv_heads);
+    p.q_parts = plan.q_parts; p.k_parts = plan.k_parts;
+    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    if (int st = begin_launches()) return st;
+    hipStream_t s = (hipStream_t)stream;
+    if (Tq > 0) {
+      if (int st = launched(launch_cross_backward(p, CROSS_DQ, s), "cross_bwd_dq")) return st;
+      if (p.q_parts > 1)
+        if (int st = launched(reduce_parts(p.dQpart, p.q_parts, Tq, cq, dQ, lddq, s), "cross_bwd_dq.reduce")) return st;
+    }
+    if (Tk == 0) return PARTIR_OK;
+    if (int st = launched(launch_cross_backward(p, CROSS_DV, s), "cross_bwd_dv")) return st;
+    if (int st = launched(launch_cross_backward(p, CROSS_DK, s), "cross_bwd_dk")) return st;
+    if (p.k_parts == 1) return PARTIR_OK;
+    if (int st = launched(reduce_parts(p.dVpart, p.k_parts, Tk, ck, dV, lddv, s), "cross_bwd_dv.reduce")) return st;
+    return launched(reduce_parts(p.dKpart, p.k_parts, Tk, ck, dK, lddk, s), "cross_bwd_dk.reduce");
   });
 }
 

@@ -41,7 +41,10 @@ EXPORTS = ("partir_loop_matmul", "partir_loop_matmul_workspace", "partir_mlp_blo
            "partir_decoder_layer_sharded_workspace", "partir_plan_decoder_layer_sharded",
            "partir_loop_matmul_noalloc", "partir_rotary_frequencies", "partir_rotary", "partir_qk_norm_rotary",
            "partir_qk_norm_rotary_backward", "partir_qk_norm_rotary_backward_workspace", "partir_grad_norm",
-           "partir_clip_grad_norm", "partir_grad_norm_workspace")
+           "partir_clip_grad_norm", "partir_grad_norm_workspace", "partir_cross_attention",
+           "partir_cross_attention_workspace", "partir_cross_attention_train", "partir_cross_attention_backward",
+           "partir_cross_attention_backward_workspace", "partir_plan_cross_attention",
+           "partir_plan_cross_attention_backward")
 
 
 class PartirError(RuntimeError):
@@ -142,6 +145,15 @@ def lib():
         "partir_grad_norm": (I32, [PP, PI64, PI32, I32, P, P, SZ, P]),
         "partir_clip_grad_norm": (I32, [PP, PP, PI64, PI32, I32, D, P, P, SZ, P]),
         "partir_grad_norm_workspace": (SZ, [I32]),
+        "partir_cross_attention": (I32, [P, P, P, P, I64, I64, I64, I64, I64, I64, I64, I64, I64, I64, P, F, P, SZ, P]),
+        "partir_cross_attention_train": (I32, [P, P, P, P, P, I64, I64, I64, I64, I64, I64, I64, I64, I64, I64, P, F, P,
+                                               SZ, P]),
+        "partir_cross_attention_workspace": (SZ, [I64] * 6),
+        "partir_cross_attention_backward": (I32, [P, P, P, P, P, P, P, P, P, I64, I64, I64, I64, I64, I64, I64, I64, I64,
+                                                  I64, I64, I64, I64, I64, P, F, P, SZ, P]),
+        "partir_cross_attention_backward_workspace": (SZ, [I64] * 6),
+        "partir_plan_cross_attention": (I32, [I64] * 6 + [ctypes.POINTER(PlanInfo)]),
+        "partir_plan_cross_attention_backward": (I32, [I64] * 6 + [ctypes.POINTER(PlanInfo)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -808,7 +820,7 @@ def decoder_layer(x, g1, g2, Wq, Wk, Wv, Wo, W1, W2, *, B: int, S: int, n_heads:
 
 # ---------------------------------------------------------------------------
 # Operators beside the nests: rotary positions, norms of queries and keys,
-# the global norm of gradients
+# attention to another sequence, the global norm of gradients
 # ---------------------------------------------------------------------------
 def _launch(dev, fn, *args, stream):
     """fn(*args, stream) with `dev` current (a call runs where its tensors are)."""
@@ -971,6 +983,108 @@ def qk_norm_rotary_backward(Q, K, dQo, dKo, gq, gk, freqs, *, d_head: int, posit
             int(positions is not None and positions.dtype == torch.int64), T, S, Hq, Hk, d_head, rd, ldq, ldk, lddqo,
             lddko, lddq, lddk, _dt(Q), int(interleaved), float(magnitude), float(eps), _ptr(ws), wsb, stream=stream)
     return (*out, *gain_out)
+
+
+def _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens):
+    """Checked sizes of a cross attention call: (n_kv_heads, Tq, Tk, ldq, ldk, ldv)."""
+    Hk = n_heads if n_kv_heads is None else n_kv_heads
+    if B < 0 or Sq < 0 or Sk < 0:
+        _bad("PARTIR_E_SHAPE", f"B = {B}, Sq = {Sq}, Sk = {Sk}")
+    bf = _bf16()
+    ldq = _matrix(Q, "Q", B * Sq, n_heads * d_head, bf)
+    ldk = _matrix(K, "K", B * Sk, Hk * d_head, bf)
+    ldv = _matrix(V, "V", B * Sk, Hk * d_head, bf)
+    _opt(k_lens, "k_lens", (B,), _th().int32)
+    return Hk, B * Sq, B * Sk, ldq, ldk, ldv
+
+
+def cross_attention(Q, K, V, *, B: int, Sq: int, Sk: int, n_heads: int, n_kv_heads: Optional[int] = None,
+                    d_head: int = 128, k_lens=None, scale: float = 0.0, out=None, workspace=None, stream=None):
+    """O = softmax(scale Q K^T) V of Sq queries over Sk keys of another
+    sequence, per head.  Q [B*Sq, n_heads * d_head], K, V [B*Sk, n_kv_heads *
+    d_head] bf16 (views with a leading dim allowed), n_kv_heads dividing n_heads;
+    k_lens [B] int32: the valid keys of each sequence (None: Sk); a query
+    without keys gets 0."""
+    return _cross_forward(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens, scale, out, None, False, workspace,
+                          stream)
+
+
+def cross_attention_train(Q, K, V, *, B: int, Sq: int, Sk: int, n_heads: int, n_kv_heads: Optional[int] = None,
+                          d_head: int = 128, k_lens=None, scale: float = 0.0, out=None, lse=None, workspace=None,
+                          stream=None):
+    """cross_attention that also returns the base-2 log-sum-exp [B*Sq, n_heads]
+    f32 for cross_attention_backward.  Returns (O, lse)."""
+    return _cross_forward(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens, scale, out, lse, True, workspace,
+                          stream)
+
+
+def _cross_forward(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens, scale, out, lse, train, workspace, stream):
+    torch = _th()
+    Hk, Tq, Tk, ldq, ldk, ldv = _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens)
+    ldo = n_heads * d_head
+    fresh_o, fresh_l = out is None, train and lse is None
+    if not fresh_o:
+        ldo = _matrix(out, "out", Tq, n_heads * d_head, torch.bfloat16)
+    _opt(lse, "lse", (Tq, n_heads), torch.float32)
+    dev = _gpu_all(Q=Q, K=K, V=V, k_lens=k_lens, out=out, lse=lse)
+    if fresh_o:
+        out = torch.empty((Tq, n_heads * d_head), dtype=torch.bfloat16, device=dev)
+    if fresh_l:
+        lse = torch.empty((Tq, n_heads), dtype=torch.float32, device=dev)
+    ws, wsb = _workspace(dev, workspace, lib().partir_cross_attention_workspace, B, Sq, Sk, n_heads, Hk, d_head)
+    _on_stream(stream, ws if workspace is None else None, out if fresh_o else None, lse if fresh_l else None)
+    if train:
+        _launch(dev, lib().partir_cross_attention_train, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(lse), B, Sq, Sk,
+                n_heads, Hk, d_head, ldq, ldk, ldv, ldo, _ptr(k_lens), float(scale), _ptr(ws), wsb, stream=stream)
+        return out, lse
+    _launch(dev, lib().partir_cross_attention, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), B, Sq, Sk, n_heads, Hk, d_head, ldq,
+            ldk, ldv, ldo, _ptr(k_lens), float(scale), _ptr(ws), wsb, stream=stream)
+    return out
+
+
+def cross_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, n_heads: int,
+                             n_kv_heads: Optional[int] = None, d_head: int = 128, k_lens=None, scale: float = 0.0,
+                             out=None, workspace=None, stream=None):
+    """Gradients (dQ, dK, dV) of cross_attention for the cotangent dO of O, from
+    the forward's O and lse; dK and dV are summed over the query heads of a key
+    head, and are 0 behind k_lens.  out: (dQ, dK, dV) to write into."""
+    torch = _th()
+    bf = torch.bfloat16
+    Hk, Tq, Tk, ldq, ldk, ldv = _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens)
+    cq, ck = n_heads * d_head, Hk * d_head
+    ldo, lddo = _matrix(O, "O", Tq, cq, bf), _matrix(dO, "dO", Tq, cq, bf)
+    _req(lse, "lse", (Tq, n_heads), torch.float32)
+    lds = (cq, ck, ck)
+    fresh = out is None
+    if not fresh:
+        if len(out) != 3:
+            _bad("PARTIR_E_SHAPE", "out must hold (dQ, dK, dV)")
+        lds = (_matrix(out[0], "dQ", Tq, cq, bf), _matrix(out[1], "dK", Tk, ck, bf), _matrix(out[2], "dV", Tk, ck, bf))
+    dev = _gpu_all(Q=Q, K=K, V=V, O=O, dO=dO, lse=lse, k_lens=k_lens, out=out)
+    if fresh:
+        out = (torch.empty((Tq, cq), dtype=bf, device=dev), torch.empty((Tk, ck), dtype=bf, device=dev),
+               torch.empty((Tk, ck), dtype=bf, device=dev))
+    ws, wsb = _workspace(dev, workspace, lib().partir_cross_attention_backward_workspace, B, Sq, Sk, n_heads, Hk, d_head)
+    _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()))
+    _launch(dev, lib().partir_cross_attention_backward, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(lse),
+            _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), B, Sq, Sk, n_heads, Hk, d_head, ldq, ldk, ldv, ldo, lddo, *lds,
+            _ptr(k_lens), float(scale), _ptr(ws), wsb, stream=stream)
+    return out
+
+
+def plan_cross_attention(B, Sq, Sk, n_heads, n_kv_heads=None, d_head=128):
+    return _plan_sizes(lib().partir_plan_cross_attention, B, Sq, Sk, n_heads, n_kv_heads or n_heads, d_head)
+
+
+def plan_cross_attention_backward(B, Sq, Sk, n_heads, n_kv_heads=None, d_head=128):
+    return _plan_sizes(lib().partir_plan_cross_attention_backward, B, Sq, Sk, n_heads, n_kv_heads or n_heads, d_head)
+
+
+def _plan_sizes(fn, *args):
+    """A plan without a text."""
+    info = PlanInfo()
+    _check(fn(*args, ctypes.byref(info)))
+    return info.as_dict()
 
 
 def _grad_arrays(tensors, name):

@@ -235,3 +235,149 @@ def test_clip_binding_checks():
     assert status(lambda: P.clip_grad_norm([t], 1.0, out=[t[:4]])) == "PARTIR_E_SHAPE"
     assert status(lambda: P.clip_grad_norm([t], 1.0, out=[t.to(bf)])) == "PARTIR_E_DTYPE"
     assert status(lambda: P.clip_grad_norm([t], 1.0, norm=torch.zeros(1))) == "PARTIR_E_SHAPE"
+
+
+# ---------------------------------------------------------------------------
+# cross attention
+# ---------------------------------------------------------------------------
+CROSS = dict(Q=A, K=A, V=A, O=A, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256, ldv=256, ldo=512, lens=NULL, scale=0.0,
+             ws=NULL, wsb=0)
+CROSS_BWD = dict(Q=A, K=A, V=A, O=A, dO=A, lse=A, dQ=A, dK=A, dV=A, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256,
+                 ldv=256, ldo=512, lddo=512, lddq=512, lddk=256, lddv=256, lens=NULL, scale=0.0, ws=A, wsb=1 << 30)
+
+
+def cross(**kw):
+    a = dict(CROSS, **kw)
+    return name(P.lib().partir_cross_attention(*(a[k] for k in CROSS), None))
+
+
+def cross_bwd(**kw):
+    a = dict(CROSS_BWD, **kw)
+    return name(P.lib().partir_cross_attention_backward(*(a[k] for k in CROSS_BWD), None))
+
+
+BAD_CROSS = [
+    (dict(Q=NULL), "PARTIR_E_NULL"), (dict(K=NULL), "PARTIR_E_NULL"), (dict(V=NULL), "PARTIR_E_NULL"),
+    (dict(O=NULL), "PARTIR_E_NULL"), (dict(Q=ODD), "PARTIR_E_LAYOUT"), (dict(V=ODD), "PARTIR_E_LAYOUT"),
+    (dict(B=-1), "PARTIR_E_SHAPE"), (dict(Sq=-1), "PARTIR_E_SHAPE"), (dict(Sk=2 ** 31), "PARTIR_E_SHAPE"),
+    (dict(B=2 ** 20, Sk=2 ** 20), "PARTIR_E_SHAPE"), (dict(B=2 ** 16, Sq=2 ** 15, Sk=0), "PARTIR_E_SHAPE"),
+    (dict(dh=64, ldq=512), "PARTIR_E_SHAPE"), (dict(Hq=0), "PARTIR_E_SHAPE"), (dict(Hk=0), "PARTIR_E_SHAPE"),
+    (dict(Hk=8), "PARTIR_E_SHAPE"), (dict(Hk=3), "PARTIR_E_DIVISIBILITY"), (dict(Hq=2 ** 18, Hk=2 ** 18), "PARTIR_E_SHAPE"),
+    (dict(ldq=504), "PARTIR_E_LAYOUT"), (dict(ldk=260), "PARTIR_E_LAYOUT"), (dict(ldv=2 ** 24 + 8), "PARTIR_E_SHAPE"),
+    (dict(ldo=0), "PARTIR_E_LAYOUT"), (dict(lens=ctypes.c_void_p(0x10002)), "PARTIR_E_LAYOUT"),
+    (dict(scale=float("nan")), "PARTIR_E_UNSUPPORTED"), (dict(scale=float("inf")), "PARTIR_E_UNSUPPORTED"),
+    (dict(scale=1e-38), "PARTIR_E_UNSUPPORTED"),
+]
+
+
+@pytest.mark.parametrize("kw,want", BAD_CROSS)
+def test_cross_attention_refusals(kw, want):
+    assert cross(**kw) == want
+    if "O" not in kw or kw["O"]:
+        assert cross_bwd(**kw) == want
+
+
+def test_cross_attention_accepts():
+    for kw in ({}, dict(lens=ODD), dict(ldk=512, ldv=2 ** 24), dict(Sk=0, K=NULL, V=NULL), dict(Hk=4, ldk=512, ldv=512)):
+        assert cross(**kw) == "PARTIR_E_HIP", kw
+        assert cross_bwd(**dict(kw, lddk=512, lddv=512, **({"dK": NULL, "dV": NULL} if "Sk" in kw else {}))) == "PARTIR_E_HIP", kw
+    assert cross(B=0, Q=NULL, K=NULL, V=NULL, O=NULL) == "PARTIR_OK"
+    assert cross(Sq=0, Q=NULL, K=NULL, V=NULL, O=NULL) == "PARTIR_OK"      # no query reads a key
+    assert cross_bwd(Sq=0, Q=NULL, O=NULL, dO=NULL, lse=NULL, dQ=NULL) == "PARTIR_E_HIP"    # dK, dV: zeros
+    assert cross_bwd(Sq=0, Sk=0, Q=NULL, K=NULL, V=NULL, O=NULL, dO=NULL, lse=NULL, dQ=NULL, dK=NULL, dV=NULL) == "PARTIR_OK"
+    for kw in (dict(lse=NULL), dict(dO=NULL), dict(dQ=NULL), dict(dK=NULL), dict(dV=NULL)):
+        assert cross_bwd(**kw) == "PARTIR_E_NULL", kw
+    for kw in (dict(lse=ctypes.c_void_p(0x10002)), dict(lddo=500), dict(lddq=8), dict(lddk=248), dict(dV=ODD)):
+        assert cross_bwd(**kw) == "PARTIR_E_LAYOUT", kw
+
+
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk", [(2, 3, 50, 4, 2), (1, 1, 131072, 32, 8), (4, 4096, 2048, 32, 8), (2, 4096, 77, 8, 8),
+                                           (1, 2 ** 20, 2 ** 20, 1, 1), (1, 1, 2 ** 30, 1, 1), (1, 2 ** 29, 1, 2, 1),
+                                           (64, 1, 4097, 8, 1), (1, 700, 33, 3, 1)])
+def test_cross_attention_workspace_is_what_the_call_needs(B, Sq, Sk, Hq, Hk):
+    z = (B, Sq, Sk, Hq, Hk, 128)
+    need, plan = P.lib().partir_cross_attention_workspace(*z), P.plan_cross_attention(B, Sq, Sk, Hq, Hk)
+    assert need == plan["workspace_bytes"] and (need > 0) == (plan["n_virtual_shards"] > 1) == (plan["n_launches"] == 2)
+    a = dict(B=B, Sq=Sq, Sk=Sk, Hq=Hq, Hk=Hk, ldq=Hq * 128, ldo=Hq * 128, ldk=Hk * 128, ldv=Hk * 128, ws=A)
+    assert cross(wsb=need, **a) == "PARTIR_E_HIP"
+    if need:
+        assert cross(wsb=need - 1, **a) == "PARTIR_E_WORKSPACE" and cross(**dict(a, wsb=need, ws=NULL)) == "PARTIR_E_NULL"
+    a.update(lddo=Hq * 128, lddq=Hq * 128, lddk=Hk * 128, lddv=Hk * 128)
+    need = P.lib().partir_cross_attention_backward_workspace(*z)
+    assert need == P.plan_cross_attention_backward(B, Sq, Sk, Hq, Hk)["workspace_bytes"] >= B * Sq * Hq * 4
+    assert cross_bwd(wsb=need, **a) == "PARTIR_E_HIP" and cross_bwd(wsb=need - 1, **a) == "PARTIR_E_WORKSPACE"
+    assert cross_bwd(**dict(a, wsb=need, ws=ODD)) == "PARTIR_E_LAYOUT"
+
+
+def test_cross_attention_queries_refuse_what_the_call_refuses():
+    bad = ctypes.c_size_t(-1).value
+    for z in ((-1, 1, 1, 1, 1, 128), (1, 1, 1, 3, 2, 128), (1, 1, 1, 2, 2, 64), (2 ** 20, 2 ** 20, 1, 1, 1, 128)):
+        assert P.lib().partir_cross_attention_workspace(*z) == bad
+        assert P.lib().partir_cross_attention_backward_workspace(*z) == bad
+        assert P.lib().partir_plan_cross_attention(*z, ctypes.byref(P.PlanInfo())) != 0
+    assert name(P.lib().partir_plan_cross_attention(1, 1, 1, 1, 1, 128, None)) == "PARTIR_E_NULL"
+
+
+def test_cross_attention_binding_checks():
+    q, kv = torch.zeros(6, 512, dtype=bf), torch.zeros(100, 512, dtype=bf)
+    k, v = kv[:, :256], kv[:, 256:]
+    kw = dict(B=2, Sq=3, Sk=50, n_heads=4, n_kv_heads=2)
+    call = lambda *a, **o: status(lambda: P.cross_attention(*a, **{**kw, **o}))  # noqa: E731
+    assert call(q, k, v) == "PARTIR_E_LAYOUT"                                   # correct, but on the CPU
+    assert call(q, kv, v) == "PARTIR_E_SHAPE"
+    assert call(q, k, v, Sk=49) == "PARTIR_E_SHAPE"
+    assert call(q, k, v, Sk=-50) == "PARTIR_E_SHAPE"
+    assert call(q.float(), k, v) == "PARTIR_E_DTYPE"
+    assert call(q, k, v.t().contiguous().t()) == "PARTIR_E_LAYOUT"
+    assert call(q, k, v, k_lens=torch.zeros(2, dtype=torch.int64)) == "PARTIR_E_DTYPE"
+    assert call(q, k, v, k_lens=torch.zeros(3, dtype=torch.int32)) == "PARTIR_E_SHAPE"
+    assert call(q, k, v, out=q[:, :256]) == "PARTIR_E_SHAPE"
+    lse = torch.zeros(6, 4)
+    b = lambda *a, **o: status(lambda: P.cross_attention_backward(*a, **{**kw, **o}))  # noqa: E731
+    assert b(q, k, v, q, q, lse) == "PARTIR_E_LAYOUT"
+    assert b(q, k, v, q, q, lse[:, :2]) == "PARTIR_E_SHAPE"
+    assert b(q, k, v, q, q.float(), lse) == "PARTIR_E_DTYPE"
+    assert b(q, k, v, q, q, lse, out=(q, k)) == "PARTIR_E_SHAPE"
+    assert b(q, k, v, q, q, lse, out=(q, k, q)) == "PARTIR_E_SHAPE"
+    assert status(lambda: P.cross_attention_train(q, k, v, lse=lse.to(bf), **kw)) == "PARTIR_E_DTYPE"
+
+
+# ---------------------------------------------------------------------------
+# the oracle against torch's own routines in fp64
+# ---------------------------------------------------------------------------
+def test_oracle_against_autograd():
+    g = torch.Generator().manual_seed(1)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)  # noqa: E731
+    B, Sq, Sk, Hq, Hk, lens = 2, 3, 7, 4, 2, [7, 4]
+    q, k, v = r(B * Sq, Hq * 128), r(B * Sk, Hk * 128), r(B * Sk, Hk * 128)
+    do = r(B * Sq, Hq * 128)
+    leaf = [x.clone().requires_grad_() for x in (q, k, v)]
+    o = []
+    for b in range(B):
+        qq = leaf[0][b * Sq:(b + 1) * Sq].reshape(Sq, Hq, 128).transpose(0, 1)
+        kk, vv = (x[b * Sk:b * Sk + lens[b]].reshape(-1, Hk, 128).transpose(0, 1).repeat_interleave(Hq // Hk, 0) for x in leaf[1:])
+        o.append(torch.nn.functional.scaled_dot_product_attention(qq, kk, vv).transpose(0, 1).reshape(Sq, -1))
+    o = torch.cat(o)
+    grads = torch.autograd.grad(o, leaf, do)
+    ref, _ = OO.cross_attention(q.numpy(), k.numpy(), v.numpy(), B, Sq, Sk, Hq, Hk, lens)
+    assert np.abs(ref - o.detach().numpy()).max() < 1e-12
+    for a, b in zip(OO.cross_attention_backward(q.numpy(), k.numpy(), v.numpy(), do.numpy(), B, Sq, Sk, Hq, Hk, lens), grads):
+        assert np.abs(a - b.numpy()).max() < 1e-12
+    # rotary as a complex product, the norm by autograd
+    T, H, dh, rd = 5, 3, 16, 12
+    x, gain, dy = r(T, H * dh), r(dh), r(T, H * dh)
+    pos, f = np.arange(T) * 1000, OO.frequencies(rd)
+    w = torch.polar(torch.full((T, 1, rd // 2), 1.5, dtype=torch.float64), torch.from_numpy(pos[:, None] * f)[:, None])
+    for inter in (False, True):
+        xl, gl = x.clone().requires_grad_(), gain.clone().requires_grad_()
+        h = xl.reshape(T, H, dh)
+        n = torch.nn.functional.rms_norm(h, (dh,), gl, 1e-4)
+        a, b = (n[..., 0:rd:2], n[..., 1:rd:2]) if inter else (n[..., :rd // 2], n[..., rd // 2:rd])
+        z = torch.complex(a, b) * w
+        rot = torch.stack((z.real, z.imag), -1).flatten(-2) if inter else torch.cat((z.real, z.imag), -1)
+        y = torch.cat((rot, n[..., rd:]), -1).reshape(T, -1)
+        kw = dict(interleaved=inter, magnitude=1.5)
+        assert np.abs(OO.qk_norm_rotary(x.numpy(), gain.numpy(), pos, f, dh, 1e-4, **kw) - y.detach().numpy()).max() < 1e-11
+        dx, dg = torch.autograd.grad(y, (xl, gl), dy)
+        got = OO.qk_norm_rotary_backward(x.numpy(), gain.numpy(), dy.numpy(), pos, f, dh, 1e-4, **kw)
+        assert np.abs(got[0] - dx.numpy()).max() < 1e-11 and np.abs(got[1] - dg.numpy()).max() < 1e-11
