@@ -238,25 +238,40 @@ __global__ __launch_bounds__(64 * QW * KG) void cross_attention_kernel(CrossPara
                  (__bf16)(oacc[d][4 * g + 2] * inv), (__bf16)(oacc[d][4 * g + 3] * inv)};
 }
 
-// O = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - M), M = max m_s, the parts
-// in order; 32 threads a row of 128.
+// O = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - M), M = max m_s.  A row of
+// 128 takes 32 threads, 4 columns each, in each of 8 groups that share the
+// parts (s = group, group + 8, ..); the groups are added in order.  The parts'
+// rows are read once, all groups' loads in flight together: 32 parts of 32 rows
+// 22 us with one group, 5 with eight.
 __global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams p) {
-  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
-  const int c4 = threadIdx.x & 31;
-  const int64_t rows = (int64_t)p.B * p.Sq * p.Hq;
-  if (row >= rows) return;
+  __shared__ f32x4 acc_s[8][32];
+  __shared__ float l_s[8];
+  const int64_t row = blockIdx.x, rows = (int64_t)p.B * p.Sq * p.Hq;
+  const int grp = threadIdx.x >> 5, c4 = threadIdx.x & 31;
   const int64_t tq = row / p.Hq;
   const int head = (int)(row - tq * p.Hq), b = (int)(tq / p.Sq);
   const int parts = cross_range(key_count(p, b), p.nsplit, 0).parts;
   float M = -3.0e38f;
-  for (int s = 0; s < parts; ++s) M = fmaxf(M, p.MLpart[s * rows + row].x);
+  for (int s = c4; s < parts; s += 32) M = fmaxf(M, p.MLpart[s * rows + row].x);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
   float L = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < parts; ++s) {
+#pragma unroll 4
+  for (int s = grp; s < parts; s += 8) {
     const float2 ml = p.MLpart[s * rows + row];
     const float f = __builtin_amdgcn_exp2f(ml.x - M);
     L += f * ml.y;
     acc += f * *(const f32x4*)(p.Opart + (s * rows + row) * DH + 4 * c4);
+  }
+  acc_s[grp][c4] = acc;
+  if (c4 == 0) l_s[grp] = L;
+  __syncthreads();
+  if (grp > 0) return;
+#pragma unroll
+  for (int g = 1; g < 8; ++g) {
+    acc += acc_s[g][c4];
+    L += l_s[g];
   }
   if (p.lse && c4 == 0) p.lse[row] = parts ? M + __builtin_amdgcn_logf(L) : -__builtin_inff();
   const float inv = parts ? 1.0f / L : 0.0f;
@@ -308,7 +323,7 @@ hipError_t launch_cross_attention(const CrossParams& p, const CrossChoice& c, hi
 
 hipError_t launch_cross_combine(const CrossParams& p, hipStream_t s) {
   const int64_t rows = (int64_t)p.B * p.Sq * p.Hq;
-  hipLaunchKernelGGL(cross_combine_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL(cross_combine_kernel, dim3((unsigned)rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -298,21 +298,23 @@ __global__ __launch_bounds__(NT) void qk_norm_backward_kernel(RotaryParams p) {
   }
 }
 
-// 32 columns and 8 row groups a workgroup; the parts of a group in order, then
-// the groups in order.
+// 8 columns and 32 groups of parts a workgroup: the parts of a group in order
+// (i = group, group + 32, ..), then the groups in order.  With 1024 parts every
+// thread adds 32 values whose loads are in flight together.
 __global__ __launch_bounds__(256) void gain_reduce_kernel(const float* part, int parts, int dh, float* dgq, float* dgk) {
-  __shared__ float red[8][32];
-  const int w = blockIdx.y, col = threadIdx.x & 31, grp = threadIdx.x >> 5;
-  const int d = blockIdx.x * 32 + col;
+  __shared__ float red[32][9];
+  const int w = blockIdx.y, col = threadIdx.x & 7, grp = threadIdx.x >> 3;
+  const int d = blockIdx.x * 8 + col;   // dh is a multiple of 8
   float* out = w ? dgk : dgq;
+  if (!out) return;
   float s = 0.0f;
-  if (d < dh && out)
-    for (int i = grp; i < parts; i += 8) s += part[((int64_t)i * 2 + w) * dh + d];
+#pragma unroll 8
+  for (int i = grp; i < parts; i += 32) s += part[((int64_t)i * 2 + w) * dh + d];
   red[grp][col] = s;
   __syncthreads();
-  if (grp == 0 && d < dh && out) {
+  if (grp == 0) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += red[i][col];
+    for (int i = 1; i < 32; ++i) s += red[i][col];
     out[d] = s;
   }
 }
@@ -385,8 +387,7 @@ hipError_t launch_qk_norm_backward(const RotaryParams& p, bool bf16, bool interl
 }
 
 hipError_t launch_gain_reduce(const float* dgpart, int parts, int dh, float* dgq, float* dgk, hipStream_t s) {
-  hipLaunchKernelGGL(gain_reduce_kernel, dim3((unsigned)((dh + 31) / 32), 2), dim3(256), 0, s, dgpart, parts, dh, dgq,
-                     dgk);
+  hipLaunchKernelGGL(gain_reduce_kernel, dim3((unsigned)(dh / 8), 2), dim3(256), 0, s, dgpart, parts, dh, dgq, dgk);
   return hipGetLastError();
 }
 

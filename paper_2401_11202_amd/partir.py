@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -73,7 +74,6 @@ _SUM_IMPL = {"auto": SUM_AUTO, "fused": SUM_FUSED, "splitk": SUM_SPLITK}
 I64, I32, P, SZ, F = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
 D = ctypes.c_double
 PP = ctypes.POINTER(ctypes.c_void_p)   # a host array of device pointers
-PI64, PI32 = ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int)
 ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 
@@ -142,8 +142,8 @@ def lib():
         "partir_qk_norm_rotary_backward": (I32, [P, P, P, P, P, P, P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64,
                                                  I64, I64, I64, I64, I64, I64, I32, I32, F, F, P, SZ, P]),
         "partir_qk_norm_rotary_backward_workspace": (SZ, [I64, I64, I64, I64, I64, I32]),
-        "partir_grad_norm": (I32, [PP, PI64, PI32, I32, P, P, SZ, P]),
-        "partir_clip_grad_norm": (I32, [PP, PP, PI64, PI32, I32, D, P, P, SZ, P]),
+        "partir_grad_norm": (I32, [P, P, P, I32, P, P, SZ, P]),   # three host arrays
+        "partir_clip_grad_norm": (I32, [P, P, P, P, I32, D, P, P, SZ, P]),   # four host arrays
         "partir_grad_norm_workspace": (SZ, [I32]),
         "partir_cross_attention": (I32, [P, P, P, P, I64, I64, I64, I64, I64, I64, I64, I64, I64, I64, P, F, P, SZ, P]),
         "partir_cross_attention_train": (I32, [P, P, P, P, P, I64, I64, I64, I64, I64, I64, I64, I64, I64, I64, P, F, P,
@@ -825,26 +825,37 @@ def decoder_layer(x, g1, g2, Wq, Wk, Wv, Wo, W1, W2, *, B: int, S: int, n_heads:
 def _launch(dev, fn, *args, stream):
     """fn(*args, stream) with `dev` current (a call runs where its tensors are)."""
     torch = _th()
-    if dev.index == torch.cuda.current_device():
+    if dev.index == torch._C._cuda_getDevice():
         _check(fn(*args, _stream(stream)))
     else:
         with torch.cuda.device(dev):
             _check(fn(*args, _stream(stream)))
 
 
+def _one_gpu(*ts):
+    """Whether the tensors (None left out) are all on one GPU.  Where they are
+    not, _gpu_all names the one that is not."""
+    d = ts[0].get_device()
+    for t in ts:
+        if t is not None and t.get_device() != d:
+            return False
+    return d >= 0
+
+
 def _matrix(t, name, rows, cols, dtype):
     """The leading dim of a row-major [rows, cols] tensor, a view perhaps."""
-    if not isinstance(t, _th().Tensor):
+    if not isinstance(t, _torch.Tensor):
         _bad("PARTIR_E_NULL", f"{name} must be a tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         _bad("PARTIR_E_DTYPE", f"{name} has dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         _bad("PARTIR_E_SHAPE", f"{name} has shape {tuple(t.shape)}, expected {(rows, cols)}")
     if rows == 0 or cols == 0:
         return cols
-    if t.stride(1) != 1 and cols > 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         _bad("PARTIR_E_LAYOUT", f"{name} must be row-major")
-    return t.stride(0) if rows > 1 else cols     # one row: its stride is never used
+    return ld if rows > 1 else cols     # one row: its stride is never used
 
 
 def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
@@ -865,7 +876,7 @@ def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, scaling: Optio
 
 
 def _rotary_args(Q, K, freqs, d_head, positions, S):
-    """Checked sizes of a rotary call: (T, Hq, Hk, rotary_dim, S, ldq, ldk)."""
+    """Checked sizes of a rotary call: (T, Hq, Hk, rotary_dim, S, ldq, ldk, dtype, positions are 64-bit)."""
     torch = _th()
     if not isinstance(Q, torch.Tensor) or Q.dim() != 2 or (K is not None and (not isinstance(K, torch.Tensor) or K.dim() != 2)):
         _bad("PARTIR_E_SHAPE", "Q and K must be 2-D tensors")
@@ -875,28 +886,37 @@ def _rotary_args(Q, K, freqs, d_head, positions, S):
     ck = 0 if K is None else K.shape[1]
     if cq % d_head or ck % d_head:
         _bad("PARTIR_E_SHAPE", f"rows of {cq} and {ck} values do not hold whole heads of {d_head}")
-    _dt(Q)
-    ldq = _matrix(Q, "Q", T, cq, Q.dtype)
-    ldk = 0 if K is None else _matrix(K, "K", T, ck, Q.dtype)
-    rd = 0
+    dt = Q.dtype
+    code = _dt(Q)
+    ldq = _matrix(Q, "Q", T, cq, dt)
+    ldk = 0 if K is None else _matrix(K, "K", T, ck, dt)
+    rd = p64 = 0
     if freqs is not None:
-        if freqs.dim() != 1:
-            _bad("PARTIR_E_SHAPE", "freqs must be 1-D")
-        rd = 2 * _req(freqs, "freqs", (freqs.shape[0],), torch.float64).shape[0]
+        if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+            _bad("PARTIR_E_DTYPE", "freqs must be a dense 1-D float64 tensor")
+        rd = 2 * freqs.shape[0]
     if positions is not None:
-        if positions.dtype not in (torch.int32, torch.int64):
+        if positions.dtype is torch.int64:
+            p64 = 1
+        elif positions.dtype is not torch.int32:
             _bad("PARTIR_E_DTYPE", f"positions has dtype {positions.dtype}, expected int32 or int64")
-        _req(positions, "positions", (T,), positions.dtype)
-    return T, cq // d_head, ck // d_head, rd, (T if S is None else S) or 1, ldq, ldk
+        if positions.shape != (T,):
+            _bad("PARTIR_E_SHAPE", f"positions has shape {tuple(positions.shape)}, expected {(T,)}")
+        if not positions.is_contiguous():
+            _bad("PARTIR_E_LAYOUT", "positions must be contiguous")
+    return T, cq // d_head, ck // d_head, rd, (T if S is None else S) or 1, ldq, ldk, code, p64
 
 
-def _rotary_out(out, names, Q, K, T):
-    """The outputs of a rotary call and their leading dims: the caller's pair, or new ones."""
-    if out is None:
-        torch = _th()
-        out = (torch.empty((T, Q.shape[1]), dtype=Q.dtype, device=Q.device),
-               None if K is None else torch.empty((T, K.shape[1]), dtype=Q.dtype, device=Q.device))
-        return out, Q.shape[1], 0 if K is None else K.shape[1]
+def _rotary_new(Q, K, T):
+    """New outputs of a rotary call and their leading dims."""
+    q = _torch.empty((T, Q.shape[1]), dtype=Q.dtype, device=Q.device)
+    if K is None:
+        return (q, None), Q.shape[1], 0
+    return (q, _torch.empty((T, K.shape[1]), dtype=Q.dtype, device=Q.device)), Q.shape[1], K.shape[1]
+
+
+def _rotary_given(out, names, Q, K, T):
+    """The caller's outputs and their leading dims."""
     if not isinstance(out, (tuple, list)) or len(out) != 2 or (out[1] is None) != (K is None):
         _bad("PARTIR_E_SHAPE", f"out must hold ({names[0]}, {names[1]}), the second None without K")
     return (tuple(out), _matrix(out[0], names[0], T, Q.shape[1], Q.dtype),
@@ -912,17 +932,17 @@ def rotary(Q, K, freqs, *, d_head: int, positions=None, S: Optional[int] = None,
     of neighbours, else of halves.  inverse: the gradient of the call without
     it.  out: (Q', K') to write into, the inputs themselves allowed.  Returns
     (Q', K')."""
-    T, Hq, Hk, rd, S, ldq, ldk = _rotary_args(Q, K, freqs, d_head, positions, S)
+    T, Hq, Hk, rd, S, ldq, ldk, dt, p64 = _rotary_args(Q, K, freqs, d_head, positions, S)
     fresh = out is None
     if not fresh:
-        out, ldqo, ldko = _rotary_out(out, ("Q'", "K'"), Q, K, T)
-    dev = _gpu_all(Q=Q, K=K, freqs=freqs, positions=positions, out=None if fresh else out)
+        out, ldqo, ldko = _rotary_given(out, ("Q'", "K'"), Q, K, T)
+    if not _one_gpu(Q, K, freqs, positions, *(() if fresh else out)):
+        _gpu_all(Q=Q, K=K, freqs=freqs, positions=positions, out=out)
     if fresh:
-        out, ldqo, ldko = _rotary_out(None, None, Q, K, T)
+        out, ldqo, ldko = _rotary_new(Q, K, T)
         _on_stream(stream, *out)
-    _launch(dev, lib().partir_rotary, _ptr(Q), _ptr(K), _ptr(out[0]), _ptr(out[1]), _ptr(freqs), _ptr(positions),
-            int(positions is not None and positions.dtype == _th().int64), T, S, Hq, Hk, d_head, rd, ldq, ldk, ldqo, ldko,
-            _dt(Q), int(interleaved), int(inverse), float(magnitude), stream=stream)
+    _launch(Q.device, lib().partir_rotary, _ptr(Q), _ptr(K), _ptr(out[0]), _ptr(out[1]), _ptr(freqs), _ptr(positions), p64,
+            T, S, Hq, Hk, d_head, rd, ldq, ldk, ldqo, ldko, dt, interleaved, inverse, magnitude, stream=stream)
     return out
 
 
@@ -931,19 +951,20 @@ def qk_norm_rotary(Q, K, gq, gk, freqs, *, d_head: int, positions=None, S: Optio
     """rotary of Q and K after an RMS norm of each head, g x / sqrt(mean(x^2) +
     eps), in one pass.  gq, gk: gains [d_head] f32, or None for 1.  freqs None:
     the norms alone.  Otherwise as rotary."""
-    T, Hq, Hk, rd, S, ldq, ldk = _rotary_args(Q, K, freqs, d_head, positions, S)
+    T, Hq, Hk, rd, S, ldq, ldk, dt, p64 = _rotary_args(Q, K, freqs, d_head, positions, S)
     _opt(gq, "gq", (d_head,), _f32())
     _opt(gk, "gk", (d_head,), _f32())
     fresh = out is None
     if not fresh:
-        out, ldqo, ldko = _rotary_out(out, ("Q'", "K'"), Q, K, T)
-    dev = _gpu_all(Q=Q, K=K, gq=gq, gk=gk, freqs=freqs, positions=positions, out=None if fresh else out)
+        out, ldqo, ldko = _rotary_given(out, ("Q'", "K'"), Q, K, T)
+    if not _one_gpu(Q, K, gq, gk, freqs, positions, *(() if fresh else out)):
+        _gpu_all(Q=Q, K=K, gq=gq, gk=gk, freqs=freqs, positions=positions, out=out)
     if fresh:
-        out, ldqo, ldko = _rotary_out(None, None, Q, K, T)
+        out, ldqo, ldko = _rotary_new(Q, K, T)
         _on_stream(stream, *out)
-    _launch(dev, lib().partir_qk_norm_rotary, _ptr(Q), _ptr(K), _ptr(gq), _ptr(gk), _ptr(out[0]), _ptr(out[1]),
-            _ptr(freqs), _ptr(positions), int(positions is not None and positions.dtype == _th().int64), T, S, Hq, Hk,
-            d_head, rd, ldq, ldk, ldqo, ldko, _dt(Q), int(interleaved), float(magnitude), float(eps), stream=stream)
+    _launch(Q.device, lib().partir_qk_norm_rotary, _ptr(Q), _ptr(K), _ptr(gq), _ptr(gk), _ptr(out[0]), _ptr(out[1]),
+            _ptr(freqs), _ptr(positions), p64, T, S, Hq, Hk, d_head, rd, ldq, ldk, ldqo, ldko, dt, interleaved, magnitude,
+            eps, stream=stream)
     return out
 
 
@@ -953,8 +974,8 @@ def qk_norm_rotary_backward(Q, K, dQo, dKo, gq, gk, freqs, *, d_head: int, posit
     """Gradients (dQ, dK, dgq, dgk) of qk_norm_rotary for the cotangents dQo,
     dKo of its outputs, from its inputs.  out: (dQ, dK) to write into (the
     cotangents themselves allowed); gain_out: (dgq, dgk), f32 [d_head]."""
-    torch = _th()
-    T, Hq, Hk, rd, S, ldq, ldk = _rotary_args(Q, K, freqs, d_head, positions, S)
+    T, Hq, Hk, rd, S, ldq, ldk, dt, p64 = _rotary_args(Q, K, freqs, d_head, positions, S)
+    torch = _torch
     lddqo = _matrix(dQo, "dQo", T, Q.shape[1], Q.dtype)
     if (dKo is None) != (K is None):
         _bad("PARTIR_E_NULL", "dKo must be given exactly where K is")
@@ -963,25 +984,26 @@ def qk_norm_rotary_backward(Q, K, dQo, dKo, gq, gk, freqs, *, d_head: int, posit
     _opt(gk, "gk", (d_head,), _f32())
     fresh, fresh_g = out is None, gain_out is None
     if not fresh:
-        out, lddq, lddk = _rotary_out(out, ("dQ", "dK"), Q, K, T)
+        out, lddq, lddk = _rotary_given(out, ("dQ", "dK"), Q, K, T)
     if not fresh_g:
         if len(gain_out) != 2:
             _bad("PARTIR_E_SHAPE", "gain_out must hold (dgq, dgk)")
         _opt(gain_out[0], "dgq", (d_head,), _f32())
         _opt(gain_out[1], "dgk", (d_head,), _f32())
-    dev = _gpu_all(Q=Q, K=K, dQo=dQo, dKo=dKo, gq=gq, gk=gk, freqs=freqs, positions=positions, out=None if fresh else out,
-                   gain_out=gain_out)
+    if not _one_gpu(Q, K, dQo, dKo, gq, gk, freqs, positions, *(() if fresh else out), *(() if fresh_g else gain_out)):
+        _gpu_all(Q=Q, K=K, dQo=dQo, dKo=dKo, gq=gq, gk=gk, freqs=freqs, positions=positions, out=out, gain_out=gain_out)
+    dev = Q.device
     if fresh:
-        out, lddq, lddk = _rotary_out(None, None, Q, K, T)
+        out, lddq, lddk = _rotary_new(Q, K, T)
     if fresh_g:
         gain_out = (torch.empty(d_head, dtype=torch.float32, device=dev),
                     None if K is None else torch.empty(d_head, dtype=torch.float32, device=dev))
-    ws, wsb = _workspace(dev, workspace, lib().partir_qk_norm_rotary_backward_workspace, T, Hq, Hk, d_head, rd, _dt(Q))
+    ws, wsb = _workspace(dev, workspace, lib().partir_qk_norm_rotary_backward_workspace, T, Hq, Hk, d_head, rd, dt)
     _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()), *(gain_out if fresh_g else ()))
     _launch(dev, lib().partir_qk_norm_rotary_backward, _ptr(Q), _ptr(K), _ptr(dQo), _ptr(dKo), _ptr(gq), _ptr(gk),
-            _ptr(out[0]), _ptr(out[1]), _ptr(gain_out[0]), _ptr(gain_out[1]), _ptr(freqs), _ptr(positions),
-            int(positions is not None and positions.dtype == torch.int64), T, S, Hq, Hk, d_head, rd, ldq, ldk, lddqo,
-            lddko, lddq, lddk, _dt(Q), int(interleaved), float(magnitude), float(eps), _ptr(ws), wsb, stream=stream)
+            _ptr(out[0]), _ptr(out[1]), _ptr(gain_out[0]), _ptr(gain_out[1]), _ptr(freqs), _ptr(positions), p64, T, S, Hq,
+            Hk, d_head, rd, ldq, ldk, lddqo, lddko, lddq, lddk, dt, interleaved, magnitude, eps, _ptr(ws), wsb,
+            stream=stream)
     return (*out, *gain_out)
 
 
@@ -990,7 +1012,7 @@ def _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens):
     Hk = n_heads if n_kv_heads is None else n_kv_heads
     if B < 0 or Sq < 0 or Sk < 0:
         _bad("PARTIR_E_SHAPE", f"B = {B}, Sq = {Sq}, Sk = {Sk}")
-    bf = _bf16()
+    bf = _th().bfloat16
     ldq = _matrix(Q, "Q", B * Sq, n_heads * d_head, bf)
     ldk = _matrix(K, "K", B * Sk, Hk * d_head, bf)
     ldv = _matrix(V, "V", B * Sk, Hk * d_head, bf)
@@ -1026,7 +1048,9 @@ def _cross_forward(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens, scal
     if not fresh_o:
         ldo = _matrix(out, "out", Tq, n_heads * d_head, torch.bfloat16)
     _opt(lse, "lse", (Tq, n_heads), torch.float32)
-    dev = _gpu_all(Q=Q, K=K, V=V, k_lens=k_lens, out=out, lse=lse)
+    if not _one_gpu(Q, K, V, k_lens, out, lse):
+        _gpu_all(Q=Q, K=K, V=V, k_lens=k_lens, out=out, lse=lse)
+    dev = Q.device
     if fresh_o:
         out = torch.empty((Tq, n_heads * d_head), dtype=torch.bfloat16, device=dev)
     if fresh_l:
@@ -1060,7 +1084,9 @@ def cross_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, n
         if len(out) != 3:
             _bad("PARTIR_E_SHAPE", "out must hold (dQ, dK, dV)")
         lds = (_matrix(out[0], "dQ", Tq, cq, bf), _matrix(out[1], "dK", Tk, ck, bf), _matrix(out[2], "dV", Tk, ck, bf))
-    dev = _gpu_all(Q=Q, K=K, V=V, O=O, dO=dO, lse=lse, k_lens=k_lens, out=out)
+    if not _one_gpu(Q, K, V, O, dO, lse, k_lens, *(() if fresh else out)):
+        _gpu_all(Q=Q, K=K, V=V, O=O, dO=dO, lse=lse, k_lens=k_lens, out=out)
+    dev = Q.device
     if fresh:
         out = (torch.empty((Tq, cq), dtype=bf, device=dev), torch.empty((Tk, ck), dtype=bf, device=dev),
                torch.empty((Tk, ck), dtype=bf, device=dev))
@@ -1088,67 +1114,64 @@ def _plan_sizes(fn, *args):
 
 
 def _grad_arrays(tensors, name):
-    """Host arrays (pointers, counts, dtypes) of a list of dense tensors, and their device."""
+    """Host arrays (addresses, counts, dtypes) of a list of dense tensors, and
+    the set of their GPUs' indexes (-1: the CPU).  Read by maps over the whole list,
+    which cost a third of a loop over hundreds of tensors."""
     torch = _th()
-    bf, f32 = torch.bfloat16, torch.float32
-    n = len(tensors)
-    ptrs, numel, dts = (ctypes.c_void_p * n)(), (I64 * n)(), (I32 * n)()
-    dev = None
-    for i, t in enumerate(tensors):
-        if not isinstance(t, torch.Tensor):
-            _bad("PARTIR_E_NULL", f"{name}[{i}] must be a tensor")
-        dt = t.dtype
-        if dt is f32:
-            dts[i] = F32
-        elif dt is bf:
-            dts[i] = BF16
-        else:
-            _bad("PARTIR_E_DTYPE", f"{name}[{i}] has dtype {dt}, expected float32 or bfloat16")
-        if not t.is_contiguous():
-            _bad("PARTIR_E_LAYOUT", f"{name}[{i}] must be dense (contiguous)")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            _bad("PARTIR_E_LAYOUT", f"{name}[{i}] is on {t.device}, expected {dev}")
-        numel[i] = t.numel()
-        ptrs[i] = t.data_ptr()
-    return ptrs, numel, dts, dev
+    T = torch.Tensor
+    try:
+        dtypes = list(map(T.dtype.__get__, tensors))
+        dense = all(map(T.is_contiguous, tensors))
+        devs = set(map(T.get_device, tensors))
+        ptrs, numel = array("Q", map(T.data_ptr, tensors)), array("q", map(T.numel, tensors))
+    except TypeError:
+        i = next(i for i, t in enumerate(tensors) if not isinstance(t, T))
+        _bad("PARTIR_E_NULL", f"{name}[{i}] must be a tensor")
+    codes = {torch.float32: F32, torch.bfloat16: BF16}
+    try:
+        dts = array("i", map(codes.__getitem__, dtypes))
+    except KeyError:
+        i = next(i for i, d in enumerate(dtypes) if d not in codes)
+        _bad("PARTIR_E_DTYPE", f"{name}[{i}] has dtype {dtypes[i]}, expected float32 or bfloat16")
+    if not dense:
+        i = next(i for i, t in enumerate(tensors) if not t.is_contiguous())
+        _bad("PARTIR_E_LAYOUT", f"{name}[{i}] must be dense (contiguous)")
+    return ptrs, numel, dts, devs
 
 
 def _grad_call(fn, tensors, norm, workspace, stream, outs=None, max_norm=None):
     torch = _th()
     tensors = list(tensors)
-    ptrs, numel, dts, dev = _grad_arrays(tensors, "tensors")
+    ptrs, numel, dts, devs = _grad_arrays(tensors, "tensors")
     optrs = ptrs
     if outs is not None:
         outs = list(outs)
         if len(outs) != len(tensors):
             _bad("PARTIR_E_SHAPE", f"out must hold {len(tensors)} tensors")
-        optrs, onumel, odts, odev = _grad_arrays(outs, "out")
-        for i, (t, o) in enumerate(zip(tensors, outs)):
-            if t.shape != o.shape:
-                _bad("PARTIR_E_SHAPE", f"out[{i}] has shape {tuple(o.shape)}, expected {tuple(t.shape)}")
-            if dts[i] != odts[i]:
-                _bad("PARTIR_E_DTYPE", f"out[{i}] has dtype {o.dtype}, expected {t.dtype}")
-        if odev != dev:
-            _bad("PARTIR_E_LAYOUT", f"out is on {odev}, expected {dev}")
+        optrs, onumel, odts, odevs = _grad_arrays(outs, "out")
+        devs |= odevs
+        if onumel != numel:
+            i = next(i for i in range(len(outs)) if onumel[i] != numel[i])
+            _bad("PARTIR_E_SHAPE", f"out[{i}] has {onumel[i]} elements, expected {numel[i]}")
+        if odts != dts:
+            i = next(i for i in range(len(outs)) if odts[i] != dts[i])
+            _bad("PARTIR_E_DTYPE", f"out[{i}] has dtype {outs[i].dtype}, expected {tensors[i].dtype}")
     if norm is not None:
-        _req(norm, "norm", (), torch.float32, dev)
-        dev = norm.device
-    if dev is None:
-        dev = torch.device("cuda", torch.cuda.current_device())
-    if dev.type != "cuda":
-        _bad("PARTIR_E_LAYOUT", f"tensors must be on a GPU (got {dev})")
+        devs.add(_req(norm, "norm", (), torch.float32).get_device())
+    if len(devs) > 1 or -1 in devs:
+        _gpu_all(tensors=tensors, out=outs, norm=norm)
+    dev = torch.device("cuda", devs.pop() if devs else torch.cuda.current_device())
     fresh = norm is None
     if fresh:
         norm = torch.empty((), dtype=torch.float32, device=dev)
     n = len(tensors)
     ws, wsb = _workspace(dev, workspace, lib().partir_grad_norm_workspace, n)
     _on_stream(stream, ws if workspace is None else None, norm if fresh else None)
+    host = [a.buffer_info()[0] for a in (ptrs, optrs, numel, dts)]     # the arrays outlive the call
     if max_norm is None:
-        _launch(dev, fn, ptrs, numel, dts, n, _ptr(norm), _ptr(ws), wsb, stream=stream)
+        _launch(dev, fn, host[0], host[2], host[3], n, _ptr(norm), _ptr(ws), wsb, stream=stream)
     else:
-        _launch(dev, fn, ptrs, optrs, numel, dts, n, float(max_norm), _ptr(norm), _ptr(ws), wsb, stream=stream)
+        _launch(dev, fn, *host, n, float(max_norm), _ptr(norm), _ptr(ws), wsb, stream=stream)
     return norm
 
 
