@@ -66,6 +66,20 @@ __device__ __forceinline__ void tile_load(const uint16_t* base, int64_t ld, int 
   }
 }
 
+// An LDS write through a restrict pointer, for lds_read's reason: a plain one
+// waits for every LDS DMA in flight first.
+template <typename T>
+__device__ __forceinline__ void lds_write(char* __restrict__ p, T v) { *(T*)p = v; }
+
+// A workgroup barrier that waits for this wave's LDS reads and writes but not
+// for its loads in flight, as __syncthreads would.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  WAIT_LGKMCNT(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // two fp32 values rounded to bf16 into elements i, i + 1 of x
 __device__ __forceinline__ void put2(bf16x8& x, int i, float a, float b) {
   const f32x2 f = {a, b};
@@ -81,6 +95,38 @@ __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
 __device__ __forceinline__ void zero(f32x16& a) {
 #pragma unroll
   for (int v = 0; v < 16; ++v) a[v] = 0.0f;
+}
+
+// Stores a wave's results, 32 rows of ND blocks of 32 columns held as a 32x32
+// MFMA leaves them (lane: row lane & 31; element v of block d: column 32 d + 8
+// (v / 4) + 4 h + v % 4), times f, as T (bf16: the one rounding).  A lane's own
+// values are 8- or 16-byte pieces of a row, and stores of such pieces, 64 rows
+// apart, held the attention kernels up for 4 us at their end; so the rows pass
+// through `area` in LDS (the wave's own, row_area bytes, 16-byte aligned) and
+// leave whole, 16 bytes a lane.  off: where this lane's row starts in out, in
+// values (both lanes of a row alike); rows from `rows` on are not stored.
+template <int ND, typename T>
+__host__ __device__ constexpr int row_area() { return 32 * (ND * 32 * (int)sizeof(T) + 16); }
+template <int ND, typename T>
+__device__ __forceinline__ void store_rows(char* area, T* out, int64_t off, int rows, const f32x16* a, float f, int lane) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  constexpr int PITCH = ND * 32 * sizeof(T) + 16, CPR = ND * 32 * sizeof(T) / 16, RPI = 64 / CPR;
+  const int h = lane >> 5, col = lane & 31;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(vec4*)(area + col * PITCH + (32 * d + 8 * g + 4 * h) * sizeof(T)) =
+          vec4{(T)(a[d][4 * g + 0] * f), (T)(a[d][4 * g + 1] * f), (T)(a[d][4 * g + 2] * f), (T)(a[d][4 * g + 3] * f)};
+  const int r0 = lane / CPR, c = lane % CPR;
+  const int lo = (int)(uint32_t)off, hi = (int)(off >> 32);
+#pragma unroll
+  for (int j = 0; j < 32 / RPI; ++j) {
+    const int r = j * RPI + r0;
+    const f32x4 v = *(const f32x4*)(area + r * PITCH + c * 16);
+    const int64_t o = ((int64_t)__shfl(hi, r) << 32) | (uint32_t)__shfl(lo, r);
+    if (r < rows) *(f32x4*)((char*)(out + o) + c * 16) = v;
+  }
 }
 
 }  // namespace partir

@@ -4,7 +4,7 @@
 //
 // A workgroup takes 32 QW rows of the G Sq query rows of one (sequence, key
 // head); its QW x KG waves hold 32 rows each, and the KG key groups take every
-// KG-th block of BKV keys through double-buffered LDS stages of their own.  A
+// KG-th block of BKV keys through a ring of LDS stages of their own.  A
 // wave computes
 //     S^T[BKV keys x 32 rows] = K_blk Q^T      (v_mfma_f32_32x32x16_bf16)
 // so that a lane owns one row: maximum and sum of the running softmax are lane
@@ -30,54 +30,55 @@ __device__ __forceinline__ int key_count(const CrossParams& p, int b) {
   return p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
 }
 
-template <int QW, int KG, int BKV>
-__global__ __launch_bounds__(64 * QW * KG) void cross_attention_kernel(CrossParams p) {
+template <int QW, int KG, int BKV, int NS, int OCC>
+__global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(CrossParams p) {
   constexpr int NSUB = BKV / 32;
+  constexpr int LPB = 2 * BKV / (4 * QW);                       // tile loads of a wave per block
   constexpr int T_BYTES = BKV * ROWB, STAGE = 2 * T_BYTES;      // K tile, then V tile
-  constexpr int MERGE = (KG - 1) * QW * 64 * 66 * 4;            // O, m and l of the other key groups
-  constexpr int LDS = KG * 2 * STAGE > MERGE ? KG * 2 * STAGE : MERGE;
-  __shared__ __attribute__((aligned(1024))) char smem[LDS];
+  constexpr int ND = 4 / KG, PER = QW * 64;                     // 32-wide blocks of O that a key group finishes
+  constexpr int MERGE = KG * (KG - 1) * ND * PER * 64, ML = KG * PER * 8;
+  static_assert(KG * NS * STAGE >= MERGE + ML && KG * NS * STAGE >= QW * KG * row_area<ND, __bf16>() &&
+                (KG == 1 || KG * NS * STAGE >= QW * KG * row_area<ND, float>()), "the stages are reused");
+  __shared__ __attribute__((aligned(1024))) char smem[KG * NS * STAGE];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int w = wave % QW, kg = wave / QW;
   const int h = lane >> 5, col = lane & 31;
 
-  const int R = p.G * p.Sq, nqb = (R + 32 * QW - 1) / (32 * QW), nbh = p.B * p.Hk;
-  int qb, bh, split;
-  if (p.nsplit == 1 && (nbh & 7) == 0) {
+  const int R = p.G * p.Sq;
+  int qb, bh, split = 0;
+  if (p.nsplit == 1 && (p.by_nbh.d & 7) == 0) {
     // Workgroup i runs on XCD i mod 8: an XCD takes one (sequence, key head)
     // after the other, whose K and V stay in its L2.
-    const int j = blockIdx.x >> 3;
-    const int n = j / nqb;
+    const int j = blockIdx.x >> 3, n = p.by_nqb.quot(j);
     bh = n * 8 + (blockIdx.x & 7);
-    qb = j - n * nqb;
-    split = 0;
+    qb = p.by_nqb.rem(j, n);
   } else {
-    bh = blockIdx.x % nbh;
-    const int r = blockIdx.x / nbh;
-    split = r % p.nsplit;
-    qb = r / p.nsplit;
+    const int r = p.by_nbh.quot(blockIdx.x);
+    bh = p.by_nbh.rem(blockIdx.x, r);
+    qb = p.by_split.quot(r);
+    split = p.by_split.rem(r, qb);
   }
-  const int b = bh / p.Hk, kvh = bh - b * p.Hk;
-  const CrossRange range = cross_range(key_count(p, b), p.nsplit, split);
-  if (p.nsplit > 1 && split >= range.parts) return;   // the combine does not read it
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
 
   // this lane's row: queries (B operand of S^T) in registers
   const int i = qb * 32 * QW + 32 * w + col;
-  const int ic = min(i, R - 1), sq = ic / p.G;
+  const int ic = min(i, R - 1), sq = p.by_g.quot(ic);
   const int64_t tq = (int64_t)b * p.Sq + sq;
-  const int head = kvh * p.G + ic - sq * p.G;
+  const int head = kvh * p.G + p.by_g.rem(ic, sq);
   bf16x8 qf[8];
   {
     const uint16_t* qrow = p.Q + tq * p.ldq + head * DH + 8 * h;
 #pragma unroll
     for (int ds = 0; ds < 8; ++ds) qf[ds] = *(const bf16x8*)(qrow + 16 * ds);
   }
+  const CrossRange range = cross_range(key_count(p, b), p.by_split, split);
+  if (p.nsplit > 1 && split >= range.parts) return;   // the combine does not read it
 
   const uint16_t* kbase = p.K + (int64_t)b * p.Sk * p.ldk + kvh * DH;
   const uint16_t* vbase = p.V + (int64_t)b * p.Sk * p.ldv + kvh * DH;
-  char* const stages = smem + kg * 2 * STAGE;
+  char* const stages = smem + kg * NS * STAGE;
   // key block kb of the part; the addresses are 64-bit, so a part may hold any
   // number of bytes
   auto gload = [&](int kb, int buf) {
@@ -96,14 +97,18 @@ __global__ __launch_bounds__(64 * QW * KG) void cross_attention_kernel(CrossPara
   const int nkb = (range.end - range.begin + BKV - 1) / BKV;
   const float sl2 = p.scale_log2;
 
-  if (kg < nkb) gload(kg, 0);
-  WAIT_VMCNT(0);
-  __syncthreads();
-  // Two blocks a trip, so that a block's stage is a constant and folds into
-  // the reads' offsets.
+  // A ring of NS stages: loads run NS - 1 blocks ahead.  Blocks behind the last
+  // are loaded too (no row of them is read: zeros), which keeps the counts of
+  // loads in flight constant.
+#pragma unroll
+  for (int n = 0; n < NS - 1; ++n) gload(n * KG + kg, n);
   auto block = [&](auto stage_c, int kb) {
     constexpr int cur = decltype(stage_c)::value;
-    if (kb + KG < nkb) gload(kb + KG, cur ^ 1);
+    __builtin_amdgcn_sched_barrier(0);
+    WAIT_VMCNT(LPB * (NS - 2));          // this wave's loads of the block have landed
+    asm volatile("s_barrier" ::: "memory");   // everyone's have, and the stage loaded next is done with
+    __builtin_amdgcn_sched_barrier(0);
+    gload(kb + KG * (NS - 1), (cur + NS - 1) % NS);
     if (KG == 1 || kb < nkb) {
       const char* ks = stages + cur * STAGE;
       const char* vs = ks + T_BYTES;
@@ -168,74 +173,96 @@ __global__ __launch_bounds__(64 * QW * KG) void cross_attention_kernel(CrossPara
 #pragma unroll
         for (int d = 0; d < 4; ++d) oacc[d] = mfma(tr.read(vs, u, d), pf[u], oacc[d]);
     }
-    WAIT_VMCNT(0);   // this wave's loads of the next tiles have landed
-    __syncthreads();
   };
-  // every barrier is the workgroup's: the trip count does not depend on the group
-  for (int kb = 0; kb < nkb; kb += 2 * KG) {
+  // NS blocks a trip, so that a block's stage is a constant and folds into the
+  // reads' offsets.  Every barrier is the workgroup's: the trip count does not
+  // depend on the group.
+  for (int kb = 0; kb < nkb; kb += NS * KG) {
     block(std::integral_constant<int, 0>{}, kb + kg);
     if (kb + KG < nkb) block(std::integral_constant<int, 1>{}, kb + KG + kg);
+    if constexpr (NS > 2) {
+      if (kb + 2 * KG < nkb) block(std::integral_constant<int, 2>{}, kb + 2 * KG + kg);
+    }
   }
+  WAIT_VMCNT(0);   // no LDS write is in flight behind the loop
+  __syncthreads();
 
   float l_tot = l_run + __shfl_xor(l_run, 32);
   if constexpr (KG > 1) {
-    // the groups' (m, l, O) into group 0's, in order; the stages are free (the
-    // loop ended on a barrier with no load in flight)
-    constexpr int PER = QW * 64;
-    auto area = [&](int g) { return smem + (g - 1) * PER * 66 * 4; };
-    if (kg > 0) {
-      f32x4* mo = (f32x4*)area(kg) + (w * 64 + lane);
+    // The groups' (m, l, O) together, in order.  Group g finishes the ND blocks
+    // of O from g ND on: it hands the others theirs and takes what they hold of
+    // its own.
+    auto box = [&](int to, int from, int d) {   // from != to
+      return (f32x4*)(smem + (((to * (KG - 1) + (from < to ? from : from - 1)) * ND + d) * PER + w * 64 + lane) * 16);
+    };
+    constexpr int STEP = KG * (KG - 1) * ND * PER;   // between the four quarters of a block
+    float2* const ml = (float2*)(smem + MERGE) + w * 64 + lane;
+    ml[kg * PER] = make_float2(m_run, l_tot);
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+    for (int g = 0; g < KG; ++g)
+      if (g != kg) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-          mo[(4 * d + g) * PER] = f32x4{oacc[d][4 * g + 0], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]};
-      ((float2*)(area(kg) + PER * 64 * 4))[w * 64 + lane] = make_float2(m_run, l_tot);
-    }
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            box(g, kg, d)[q * STEP] = f32x4{oacc[g * ND + d][4 * q + 0], oacc[g * ND + d][4 * q + 1],
+                                            oacc[g * ND + d][4 * q + 2], oacc[g * ND + d][4 * q + 3]};
+      }
     __syncthreads();
-    if (kg > 0) return;
+    float2 st[KG];
+    m_run = -1e30f;
 #pragma unroll
-    for (int g2 = 1; g2 < KG; ++g2) {
-      const f32x4* mo = (const f32x4*)area(g2) + (w * 64 + lane);
-      const float2 o = ((const float2*)(area(g2) + PER * 64 * 4))[w * 64 + lane];
-      const float m_new = fmaxf(m_run, o.x);   // a group without keys holds (-1e30, 0, 0)
-      const float a0 = __builtin_amdgcn_exp2f(m_run - m_new), a1 = __builtin_amdgcn_exp2f(o.x - m_new);
-      l_tot = a0 * l_tot + a1 * o.y;
-      m_run = m_new;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 v = mo[(4 * d + g) * PER];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) oacc[d][4 * g + e] = a0 * oacc[d][4 * g + e] + a1 * v[e];
-        }
+    for (int g = 0; g < KG; ++g) {
+      st[g] = ml[g * PER];
+      m_run = fmaxf(m_run, st[g].x);   // a group without keys holds (-1e30, 0, 0)
     }
+    f32x16 own[ND];
+#pragma unroll
+    for (int g = 0; g < KG; ++g)       // this group's own blocks (a constant index for every g)
+      if (g == kg) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d) own[d] = oacc[g * ND + d];
+      }
+    f32x16 sum[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) zero(sum[d]);
+    l_tot = 0.0f;
+#pragma unroll
+    for (int g = 0; g < KG; ++g) {
+      const float a = __builtin_amdgcn_exp2f(st[g].x - m_run);
+      l_tot += a * st[g].y;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        f32x16 v = own[d];
+        if (g != kg) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 x = box(kg, g, d)[q * STEP];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+          }
+        }
+        sum[d] += a * v;
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) oacc[d] = sum[d];
+    __syncthreads();   // the boxes are read: their memory takes the rows
   }
-  if (i >= R) return;
-  const int64_t row = tq * p.Hq + head;
+  const int row0 = qb * 32 * QW + 32 * w;        // this wave's first row
+  const int64_t row = tq * p.Hq + head;          // this lane's
   if (p.nsplit > 1) {
-    const int64_t at = (int64_t)split * p.B * p.Sq * p.Hq + row;
-    float* orow = p.Opart + at * DH;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *(f32x4*)(orow + 32 * d + 8 * g + 4 * h) =
-            f32x4{oacc[d][4 * g + 0], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]};
-    if (h == 0) p.MLpart[at] = make_float2(m_run, l_tot);
+    if constexpr (KG > 1) {   // cross_choice takes parts with several key groups only
+      const int64_t at = (int64_t)split * p.B * p.Sq * p.Hq + row;
+      store_rows<ND>(smem + wave * row_area<ND, float>(), p.Opart, at * DH + kg * ND * 32, R - row0, oacc, 1.0f, lane);
+      if (kg == 0 && h == 0 && i < R) p.MLpart[at] = make_float2(m_run, l_tot);
+    }
     return;
   }
-  if (p.lse && h == 0) p.lse[row] = nkb > 0 ? m_run + __builtin_amdgcn_logf(l_tot) : -__builtin_inff();
-  const float inv = nkb > 0 ? 1.0f / l_tot : 0.0f;
-  uint16_t* orow = p.O + tq * p.ldo + head * DH;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *(bf16x4*)(orow + 32 * d + 8 * g + 4 * h) =
-          bf16x4{(__bf16)(oacc[d][4 * g + 0] * inv), (__bf16)(oacc[d][4 * g + 1] * inv),
-                 (__bf16)(oacc[d][4 * g + 2] * inv), (__bf16)(oacc[d][4 * g + 3] * inv)};
+  if (p.lse && kg == 0 && h == 0 && i < R) p.lse[row] = nkb > 0 ? m_run + __builtin_amdgcn_logf(l_tot) : -__builtin_inff();
+  // O times 1 / l of its row (the lane's own)
+  store_rows<ND>(smem + wave * row_area<ND, __bf16>(), (__bf16*)p.O, tq * p.ldo + head * DH + kg * ND * 32, R - row0, oacc,
+                 nkb > 0 ? 1.0f / l_tot : 0.0f, lane);
 }
 
 // O = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - M), M = max m_s.  A row of
@@ -250,7 +277,7 @@ __global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams p) {
   const int grp = threadIdx.x >> 5, c4 = threadIdx.x & 31;
   const int64_t tq = row / p.Hq;
   const int head = (int)(row - tq * p.Hq), b = (int)(tq / p.Sq);
-  const int parts = cross_range(key_count(p, b), p.nsplit, 0).parts;
+  const int parts = cross_range(key_count(p, b), p.by_split, 0).parts;
   float M = -3.0e38f;
   for (int s = c4; s < parts; s += 32) M = fmaxf(M, p.MLpart[s * rows + row].x);
 #pragma unroll
@@ -313,11 +340,11 @@ hipError_t launch_cross_attention(const CrossParams& p, const CrossChoice& c, hi
   const int64_t rows = (int64_t)p.G * p.Sq, nqb = (rows + 32 * c.qw - 1) / (32 * c.qw);
   const dim3 grid((unsigned)(nqb * p.B * p.Hk * p.nsplit));
   if (c.qw == 1)
-    hipLaunchKernelGGL((cross_attention_kernel<1, 4, 32>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((cross_attention_kernel<1, 4, 32, 2, 1>), grid, dim3(256), 0, s, p);
   else if (c.kg == 2)
-    hipLaunchKernelGGL((cross_attention_kernel<4, 2, 64>), grid, dim3(512), 0, s, p);
+    hipLaunchKernelGGL((cross_attention_kernel<4, 2, 64, 2, 2>), grid, dim3(512), 0, s, p);
   else
-    hipLaunchKernelGGL((cross_attention_kernel<4, 1, 32>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((cross_attention_kernel<4, 1, 32, 3, 3>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

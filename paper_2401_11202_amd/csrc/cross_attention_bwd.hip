@@ -4,15 +4,16 @@
 // log-sum-exp; P = 0 for keys at and behind len_b):
 //     D  = rowsum(dO * O)             dV = P^T dO        dP = dO V^T
 //     dS = P * (dP - D)               dQ = scale dS K    dK = scale dS^T Q
-// Each pass holds one axis of the scores in registers and streams the other
+// Up to 128 keys a sequence, one pass (cross_bwd_one_pass_kernel).  Above, each
+// pass holds one axis of the scores in registers and streams the other
 // through LDS, so that a gradient has one writer and a fixed order (no
 // atomics), the G query heads of a key head included:
 //  * dq: workgroup = 128 of the G Sq query rows of a (sequence, key head), 4
 //    waves x 32, keys in tiles of 64; S^T = K Q^T and dP^T = V dO^T put one row
 //    on a lane, dQ^T += K^T dS^T.  It also writes D.
 //  * dv and dk: workgroup = 128 keys of a (sequence, key head), 4 waves x 32;
-//    the rows of its G heads in tiles of 64, head after head; S = Q K^T and dP =
-//    dO V^T put one key on a lane, dV^T += dO^T P, dK^T += Q^T dS.
+//    its G Sq query rows in tiles of 64; S = Q K^T and dP = dO V^T put one key on
+//    a lane, dV^T += dO^T P, dK^T += Q^T dS.
 // Where the axis that is held is short (few queries in dq, few keys in dk and
 // dv) the streamed one is shared out over parts, whose float32 results an
 // ordered reduction adds.  P and dS are rounded to bf16 for their products
@@ -37,23 +38,62 @@ __device__ __forceinline__ int key_count(const CrossBwdParams& p, int b) {
   return p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
 }
 
-// A lane's 64 of the 128 x 32 results of a wave: columns 32 d + 8 g + 4 h.. of
-// its row, as bf16 or as float32.
-__device__ __forceinline__ void store_row(uint16_t* out, const f32x16* a, float f, int h) {
+// The 64-row tiles of the G Sq query rows of a (sequence, key head), Q and dO
+// side by side: row i is position i / G of head i mod G.  Addresses ascend with
+// the rows, so a descriptor that ends with the tile's last row makes those
+// behind it zeros.  Where G divides 16, a lane's rows lie at one offset from a
+// tile's first position and a fixed step apart; else each is divided by G (8 %
+// of the dk and dv passes).
+template <bool EVEN>
+struct RowTiles {
+  const uint16_t *q, *g;
+  int64_t ldq, ldg;
+  Div by_g;
+  int R, w, lane;
+  uint32_t oq, og, chunk;
+  __device__ __forceinline__ RowTiles(const CrossBwdParams& p, int b, int kvh, int w_, int lane_)
+      : q(p.Q + (int64_t)b * p.Sq * p.ldq + kvh * p.G * DH), g(p.dO + (int64_t)b * p.Sq * p.ldg + kvh * p.G * DH), ldq(p.ldq),
+        ldg(p.ldg), by_g(p.by_g), R(p.G * p.Sq), w(w_), lane(lane_) {
+    const int l4 = lane >> 4, r = 4 * w + l4, s = by_g.quot(r);
+    chunk = ((lane & 15) ^ (l4 << 2) ^ (w & 3)) << 4;   // row 16 j + r sits at the same chunk for every j
+    const uint32_t in = (uint32_t)by_g.rem(r, s) * ROWB + chunk;
+    oq = (uint32_t)s * (uint32_t)(ldq * 2) + in;
+    og = (uint32_t)s * (uint32_t)(ldg * 2) + in;
+  }
+  __device__ __forceinline__ void load(int it, char* tile) const {
+    const int i0 = it * TR, s0 = by_g.quot(i0), last = min(i0 + TR, R) - 1, sl = by_g.quot(last);
+    const uint32_t tail = (uint32_t)by_g.rem(last, sl) * ROWB + ROWB;
+    const __amdgpu_buffer_rsrc_t rq = make_rsrc(q + s0 * ldq, (uint32_t)((sl - s0) * ldq * 2) + tail);
+    const __amdgpu_buffer_rsrc_t rg = make_rsrc(g + s0 * ldg, (uint32_t)((sl - s0) * ldg * 2) + tail);
+    auto put = [&](int j, uint32_t a, uint32_t b) {
+      char* const t = tile + (4 * j + w) * 1024;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)t, 16, a, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, (lds_void*)(t + TILE), 16, b, 0, 0, 0);
+    };
+    if constexpr (EVEN) {
+      const uint32_t n = by_g.quot(16), sq = n * (uint32_t)(ldq * 2), sg = n * (uint32_t)(ldg * 2);
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+      for (int j = 0; j < TR / 16; ++j) put(j, oq + j * sq, og + j * sg);
+    } else {
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *(bf16x4*)(out + 32 * d + 8 * g + 4 * h) = bf16x4{(__bf16)(a[d][4 * g + 0] * f), (__bf16)(a[d][4 * g + 1] * f),
-                                                        (__bf16)(a[d][4 * g + 2] * f), (__bf16)(a[d][4 * g + 3] * f)};
+      for (int j = 0; j < TR / 16; ++j) {
+        const int i = i0 + 16 * j + 4 * w + (lane >> 4), s = by_g.quot(i);
+        const uint32_t in = (uint32_t)by_g.rem(i, s) * ROWB + chunk;
+        put(j, (uint32_t)(s - s0) * (uint32_t)(ldq * 2) + in, (uint32_t)(s - s0) * (uint32_t)(ldg * 2) + in);
+      }
+    }
+  }
+};
+
+// A wave's 32 rows of 128 results times f, through its share of the tiles'
+// memory (free behind the loops' last barrier), as bf16 or as float32 parts.
+__device__ __forceinline__ void store(char* smem, int w, uint16_t* out, int64_t off, int rows, const f32x16* a, float f, int lane) {
+  store_rows<4>(smem + w * row_area<4, __bf16>(), (__bf16*)out, off, rows, a, f, lane);
 }
-__device__ __forceinline__ void store_row(float* out, const f32x16* a, float f, int h) {
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *(f32x4*)(out + 32 * d + 8 * g + 4 * h) =
-          f32x4{a[d][4 * g + 0] * f, a[d][4 * g + 1] * f, a[d][4 * g + 2] * f, a[d][4 * g + 3] * f};
+__device__ __forceinline__ void store(char* smem, int w, float* out, int64_t off, int rows, const f32x16* a, float f, int lane) {
+  char* const area = smem + w * row_area<2, float>();
+  store_rows<2>(area, out, off, rows, a, f, lane);
+  store_rows<2>(area, out, off + 64, rows, a + 2, f, lane);
 }
 
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -63,15 +103,14 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
 
-  const int R = p.G * p.Sq, nbh = p.B * p.Hk;
-  const int bh = blockIdx.x % nbh, rest = blockIdx.x / nbh;
-  const int part = rest % p.q_parts, qb = rest / p.q_parts;
-  const int b = bh / p.Hk, kvh = bh - b * p.Hk;
-  const CrossRange range = cross_range(key_count(p, b), p.q_parts, part);
+  const int R = p.G * p.Sq;
+  const int rest = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, rest);
+  const int qb = p.by_q_parts.quot(rest), part = p.by_q_parts.rem(rest, qb);
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
   const int i = qb * 128 + 32 * w + col;
-  const int ic = min(i, R - 1), sq = ic / p.G;
+  const int ic = min(i, R - 1), sq = p.by_g.quot(ic);
   const int64_t tq = (int64_t)b * p.Sq + sq;
-  const int head = kvh * p.G + ic - sq * p.G;
+  const int head = kvh * p.G + p.by_g.rem(ic, sq);
 
   // Q and dO of this lane's row (B operands), D = rowsum(dO * O)
   bf16x8 qf[8], gf[8];
@@ -93,6 +132,7 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
   const float lse = p.lse[tq * p.Hq + head];
   if (part == 0 && h == 0 && i < R) p.Dstat[tq * p.Hq + head] = Dq;
 
+  const CrossRange range = cross_range(key_count(p, b), p.by_q_parts, part);
   const uint16_t* kbase = p.K + ((int64_t)b * p.Sk + range.begin) * p.ldk + kvh * DH;
   const uint16_t* vbase = p.V + ((int64_t)b * p.Sk + range.begin) * p.ldv + kvh * DH;
   const int nkeys = range.end - range.begin, nkb = (nkeys + TR - 1) / TR;
@@ -151,31 +191,32 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
     iter(kb, std::integral_constant<int, 0>{});
     if (kb + 1 < nkb) iter(kb + 1, std::integral_constant<int, 1>{});
   }
-  if (i >= R) return;
+  const int rows = R - qb * 128 - 32 * w;
   if (p.q_parts > 1)
-    store_row(p.dQpart + (((int64_t)part * p.B * p.Sq + tq) * p.Hq + head) * DH, dq, p.scale, h);
+    store(smem, w, p.dQpart, (((int64_t)part * p.B * p.Sq + tq) * p.Hq + head) * DH, rows, dq, p.scale, lane);
   else
-    store_row(p.dQ + tq * p.lddq + head * DH, dq, p.scale, h);
+    store(smem, w, p.dQ, tq * p.lddq + head * DH, rows, dq, p.scale, lane);
 }
 
 // MODE 1: dV (S and P, dV^T += dO^T P); MODE 2: dK (S, P and dP, dK^T += Q^T
 // dS).  One pass doing both would hold twice the accumulators, which leaves one
 // wave a SIMD; forming S again costs less.
-template <int MODE>
+template <int MODE, bool EVEN>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void cross_bwd_dkv_kernel(CrossBwdParams p) {
   constexpr bool DO_K = MODE == 2;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE];
-  __shared__ float stat[2][2][TR];   // [stage][-lse / c, -D][row]
+  // one object: with several, the compiler tells them apart, takes every tile
+  // read for one of the tiles being loaded and waits for those
+  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE + 2 * 2 * TR * 4];
+  float (*const stat)[2][TR] = (float (*)[2][TR])(smem + 2 * 2 * TILE);   // [stage][-lse / c, -D][row]
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, col = lane & 31;
 
-  const int nbh = p.B * p.Hk;
-  const int bh = blockIdx.x % nbh, rest = blockIdx.x / nbh;
-  const int part = rest % p.k_parts, kblk = rest / p.k_parts;
-  const int b = bh / p.Hk, kvh = bh - b * p.Hk;
-  const int len = key_count(p, b);
+  const int rest = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, rest);
+  const int kblk = p.by_k_parts.quot(rest), part = p.by_k_parts.rem(rest, kblk);
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
+  const int len = key_count(p, b), R = p.G * p.Sq;
   const int kj = kblk * 128 + 32 * w + col;          // this lane's key
   const int64_t tk = (int64_t)b * p.Sk + kj;
 
@@ -195,35 +236,33 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
         if (DO_K) vf[ds] = *(const bf16x8*)(vrow + 16 * ds);
       }
     }
-    // items: the 64-row tiles of head 0, of head 1, ...; a part takes a run of them
-    const int nqb = (p.Sq + TR - 1) / TR;
-    const int64_t items = (int64_t)p.G * nqb, per = (items + p.k_parts - 1) / p.k_parts;
-    const int64_t it0 = min(items, part * per), it1 = min(items, it0 + per);
+    const int tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
+    const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
+    const RowTiles<EVEN> rt(p, b, kvh, w, lane);
     const float inv_c = 1.0f / p.scale_log2;
     float st_l = 0.0f, st_d = 0.0f;
-    auto gload = [&](int64_t it, int buf) {
-      const int g = (int)(it / nqb), qb = (int)(it - (int64_t)g * nqb), head = kvh * p.G + g;
-      const int rows = min(TR, p.Sq - qb * TR);
-      const int64_t t0 = (int64_t)b * p.Sq + qb * TR;
-      char* t = smem + buf * 2 * TILE;
-      tile_load<TR, 4>(p.Q + t0 * p.ldq + head * DH, p.ldq, rows, t, w, lane);
-      tile_load<TR, 4>(p.dO + t0 * p.ldg + head * DH, p.ldg, rows, t + TILE, w, lane);
+    auto gload = [&](int it, int buf) {
+      rt.load(it, smem + buf * 2 * TILE);
       if (tid < TR) {
-        const int64_t at = (t0 + tid) * p.Hq + head;
-        st_l = tid < rows ? p.lse[at] : __builtin_inff();   // a missing row: P = 2^-inf
-        if (DO_K) st_d = tid < rows ? p.Dstat[at] : 0.0f;
+        // nothing looks at the loaded values before sstore: a use here would wait
+        // for the tiles' loads too
+        const int i = min(it * TR + tid, R - 1), sq = p.by_g.quot(i);
+        const int64_t at = ((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq);
+        st_l = p.lse[at];
+        if (DO_K) st_d = p.Dstat[at];
       }
     };
-    auto sstore = [&](int buf) {
+    auto sstore = [&](int it, int buf) {
       if (tid < TR) {
-        stat[buf][0][tid] = -st_l * inv_c;
-        stat[buf][1][tid] = -st_d;
+        const bool row = it * TR + tid < R;   // a missing row: P = 2^-inf
+        lds_write((char*)&stat[buf][0][tid], row ? -st_l * inv_c : -__builtin_inff());
+        if (DO_K) lds_write((char*)&stat[buf][1][tid], row ? -st_d : 0.0f);
       }
     };
     TileTr tr;
     tr.init(lane);
     const float c = p.scale_log2;
-    auto iter = [&](int64_t it, auto stage) {
+    auto iter = [&](int it, auto stage) {
       constexpr int cur = decltype(stage)::value;
       if (it + 1 < it1) gload(it + 1, cur ^ 1);
       const char* qs = smem + cur * 2 * TILE;
@@ -234,11 +273,11 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
         f32x16 s, dp;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const f32x4 l4 = *(const f32x4*)&stat[cur][0][32 * t + 8 * q + 4 * h];
+          const f32x4 l4 = lds_read<f32x4>((const char*)&stat[cur][0][32 * t + 8 * q + 4 * h]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[4 * q + j] = l4[j];
           if (DO_K) {
-            const f32x4 d4 = *(const f32x4*)&stat[cur][1][32 * t + 8 * q + 4 * h];
+            const f32x4 d4 = lds_read<f32x4>((const char*)&stat[cur][1][32 * t + 8 * q + 4 * h]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) dp[4 * q + j] = d4[j];
           }
@@ -262,17 +301,17 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
 #pragma unroll
           for (int d = 0; d < 4; ++d) acc[d] = mfma(tr.read(DO_K ? qs : gs, 2 * t + uu, d), pf[uu], acc[d]);
       }
-      if (it + 1 < it1) sstore(cur ^ 1);
+      if (it + 1 < it1) sstore(it + 1, cur ^ 1);
       WAIT_VMCNT(0);
       __syncthreads();
     };
     if (it0 < it1) {
       gload(it0, 0);
-      sstore(0);
+      sstore(it0, 0);
     }
     WAIT_VMCNT(0);
     __syncthreads();
-    for (int64_t it = it0; it < it1; it += 2) {
+    for (int it = it0; it < it1; it += 2) {
       iter(it, std::integral_constant<int, 0>{});
       if (it + 1 < it1) iter(it + 1, std::integral_constant<int, 1>{});
     }
@@ -281,43 +320,263 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
       for (int d = 0; d < 4; ++d) zero(acc[d]);
     }
   }
-  if (kj >= p.Sk) return;
   const float f = DO_K ? p.scale : 1.0f;
+  const int rows = p.Sk - kblk * 128 - 32 * w;
   if (p.k_parts > 1)
-    store_row((DO_K ? p.dKpart : p.dVpart) + (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH, acc, f, h);
+    store(smem, w, DO_K ? p.dKpart : p.dVpart, (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH, rows, acc, f, lane);
   else
-    store_row((DO_K ? p.dK + tk * p.lddk : p.dV + tk * p.lddv) + kvh * DH, acc, f, h);
+    store(smem, w, DO_K ? p.dK : p.dV, tk * (DO_K ? p.lddk : p.lddv) + kvh * DH, rows, acc, f, lane);
+}
+
+// dS of a 64-row tile as [128 keys][64 rows] bf16: 16-byte chunk c of key k at
+// position c ^ ds_swz(k).  The writes of a wave's 32 keys (8 bytes a lane, one
+// column) spread over 16 positions, and a transposed read (4 keys x 64 bytes)
+// over all banks: two keys share a 256-byte line of banks, keys 2 apart take
+// its other half.
+__device__ __forceinline__ int ds_swz(int key) { return (((key >> 1) & 1) << 2) ^ ((key >> 2) & 3); }
+__device__ __forceinline__ int ds_off(int key, int colb) {
+  return key * 128 + (((colb >> 4) ^ ds_swz(key)) << 4) + (colb & 15);
+}
+
+// All three gradients in one pass where a sequence has at most 128 keys: S and
+// dP are formed once (5 products instead of 8), and D = sum_j P_j dP_j comes
+// from the weights themselves, so that O is not read and its rounding to bf16,
+// which with few keys is of the size of the other roundings, stays out.
+// Workgroup = the keys of a (sequence, key head) and a part of its query rows:
+// four waves of 32 keys hold K and V as operands and dK and dV as sums; rows
+// come in tiles of 64.  Per tile a wave forms S = Q K^T and dP = dO V^T of its
+// keys and dV^T += dO^T P; the waves add up D, go on to dS and dK^T += Q^T dS, and
+// leave dS in LDS; then each takes 32 columns of dQ^T = K^T dS^T over all keys,
+// with its K^T operands in registers.  Some 350 registers: one wave a SIMD, one
+// workgroup a CU.
+template <bool EVEN>
+__global__ __launch_bounds__(NT, 1) void cross_bwd_one_pass_kernel(CrossBwdParams p) {
+  constexpr int DS = 2 * 2 * TILE;                   // after the two stages
+  constexpr int ROWS = DS + 128 * 128;               // the waves' row areas
+  constexpr int STAT = ROWS + 4 * row_area<1, __bf16>();
+  __shared__ __attribute__((aligned(1024))) char smem[STAT + 6 * TR * 4];
+  float (*const stat)[TR] = (float (*)[TR])(smem + STAT);   // [stage][-lse / c]
+  float (*const dsum)[TR] = stat + 2;                       // [wave]: its keys' share of D
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, col = lane & 31;
+
+  const int part = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, part);
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
+  const int len = key_count(p, b), R = p.G * p.Sq;
+  const int kj = 32 * w + col;                       // this lane's key
+  const bool on = kj < len;
+
+  // K into the first stage, V into the second (rows behind len are zeros)
+  const int64_t tk0 = (int64_t)b * p.Sk;
+  tile_load<128, 4>(p.K + tk0 * p.ldk + kvh * DH, p.ldk, len, smem, w, lane);
+  tile_load<128, 4>(p.V + tk0 * p.ldv + kvh * DH, p.ldv, len, smem + 2 * TILE, w, lane);
+  TileTr tr;
+  tr.init(lane);
+  WAIT_VMCNT(0);
+  __syncthreads();
+  bf16x8 kf[8], vf[8], kt[8];
+#pragma unroll
+  for (int ds = 0; ds < 8; ++ds) {
+    kf[ds] = tile_rows(smem, 32 * w, col, h, ds);
+    vf[ds] = tile_rows(smem + 2 * TILE, 32 * w, col, h, ds);
+    kt[ds] = tr.read(smem, ds, w);                   // K^T: columns 32 w.., keys 16 ds..
+  }
+  __syncthreads();
+
+  const int tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
+  const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
+  const RowTiles<EVEN> rt(p, b, kvh, w, lane);
+  const float c = p.scale_log2, inv_c = 1.0f / p.scale_log2;
+  float st_l = 0.0f;
+  auto gload = [&](int it, int buf) {
+    rt.load(it, smem + buf * 2 * TILE);
+    if (tid < TR) {
+      const int i = min(it * TR + tid, R - 1), sq = p.by_g.quot(i);
+      st_l = p.lse[((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq)];
+    }
+  };
+  auto sstore = [&](int it, int buf) {   // a missing row: P = 2^-inf
+    if (tid < TR) lds_write((char*)&stat[buf][tid], it * TR + tid < R ? -st_l * inv_c : -__builtin_inff());
+  };
+  f32x16 dk[4], dv[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    zero(dk[d]);
+    zero(dv[d]);
+  }
+  auto iter = [&](int it, auto stage) {
+    constexpr int cur = decltype(stage)::value;
+    if (it + 1 < it1) gload(it + 1, cur ^ 1);
+    const char* qs = smem + cur * 2 * TILE;
+    const char* gs = qs + TILE;
+    f32x16 s[2], dp[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 l4 = lds_read<f32x4>((const char*)&stat[cur][32 * t + 8 * q + 4 * h]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[t][4 * q + j] = l4[j];
+      }
+      zero(dp[t]);
+#pragma unroll
+      for (int ds = 0; ds < 8; ++ds) {
+        s[t] = mfma(tile_rows(qs, 32 * t, col, h, ds), kf[ds], s[t]);
+        dp[t] = mfma(tile_rows(gs, 32 * t, col, h, ds), vf[ds], dp[t]);
+      }
+    }
+    // P, its share of D, dV
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 pf[2];
+      float x[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[t][v] = on ? __builtin_amdgcn_exp2f(s[t][v] * c) : 0.0f;
+        x[v] = s[t][v] * dp[t][v];
+      }
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[t][v], s[t][v + 1]);
+      // The sums of x over the 32 keys: each step halves the rows a lane holds
+      // and doubles the keys in them; lane col ends with row element col / 2.
+#pragma unroll
+      for (int m = 16, n = 8; m >= 2; m >>= 1, n >>= 1) {
+        const bool up = (col & m) != 0;
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+          const float keep = up ? x[e + n] : x[e], send = up ? x[e] : x[e + n];
+          x[e] = keep + __shfl_xor(send, m);
+        }
+      }
+      x[0] += __shfl_xor(x[0], 1);
+      if (!(col & 1)) lds_write((char*)&dsum[w][32 * t + 8 * (col >> 3) + 4 * h + ((col >> 1) & 3)], x[0]);
+#pragma unroll
+      for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * t + uu, d), pf[uu], dv[d]);
+    }
+    lds_barrier();
+    // dS, dK, and dS for everyone
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 df[2];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int r = 32 * t + 8 * q + 4 * h;
+        f32x4 D = lds_read<f32x4>((const char*)&dsum[0][r]);
+#pragma unroll
+        for (int u = 1; u < 4; ++u) D += lds_read<f32x4>((const char*)&dsum[u][r]);
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const int v = 4 * q + j;   // P is 0 for keys behind len, whose dP is 0
+          put2(df[v >> 3], v & 7, s[t][v] * (dp[t][v] - D[j]), s[t][v + 1] * (dp[t][v + 1] - D[j + 1]));
+        }
+        const bf16x4 o = {df[q >> 1][4 * (q & 1) + 0], df[q >> 1][4 * (q & 1) + 1], df[q >> 1][4 * (q & 1) + 2],
+                          df[q >> 1][4 * (q & 1) + 3]};
+        lds_write(smem + DS + ds_off(kj, 2 * r), o);
+      }
+#pragma unroll
+      for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, 2 * t + uu, d), df[uu], dk[d]);
+    }
+    if (it + 1 < it1) sstore(it + 1, cur ^ 1);
+    WAIT_VMCNT(0);
+    __syncthreads();
+    // dQ^T: columns 32 w.. of both 32-row halves over all keys
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 dq;
+      zero(dq);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int key = 16 * u + tr.row, colb = 64 * t + tr.colb;
+        const lds_i16x4_t lo = lds_read_tr16(smem + DS + ds_off(key, colb));
+        const lds_i16x4_t hi = lds_read_tr16(smem + DS + ds_off(key + 8, colb));
+        dq = mfma(kt[u], __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), dq);
+      }
+      const int i = it * TR + 32 * t + col, ic = min(i, R - 1), sq = p.by_g.quot(ic);
+      store_rows<1>(smem + ROWS + w * row_area<1, __bf16>(), (__bf16*)p.dQ,
+                    ((int64_t)b * p.Sq + sq) * p.lddq + (kvh * p.G + p.by_g.rem(ic, sq)) * DH + 32 * w, R - it * TR - 32 * t,
+                    &dq, p.scale, lane);
+    }
+  };
+  if (it0 < it1) {
+    gload(it0, 0);
+    sstore(it0, 0);
+  }
+  WAIT_VMCNT(0);
+  __syncthreads();
+  for (int it = it0; it < it1; it += 2) {
+    iter(it, std::integral_constant<int, 0>{});
+    if (it + 1 < it1) iter(it + 1, std::integral_constant<int, 1>{});
+  }
+  __syncthreads();   // the last tile's dS is read
+  // Q's rows of keys behind len met P = 0, so their sums are 0
+  const int64_t tk = tk0 + kj;
+  const int rows = p.Sk - 32 * w;
+  if (p.k_parts > 1) {
+    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH;
+    store(smem, w, p.dKpart, at, rows, dk, p.scale, lane);
+    store(smem, w, p.dVpart, at, rows, dv, 1.0f, lane);
+  } else {
+    store(smem, w, p.dK, tk * p.lddk + kvh * DH, rows, dk, p.scale, lane);
+    store(smem, w, p.dV, tk * p.lddv + kvh * DH, rows, dv, 1.0f, lane);
+  }
+}
+
+// Four columns a thread; the parts' loads in flight together.
+__global__ __launch_bounds__(256) void part_sum_kernel(PartSum p) {
+  const int64_t stride = p.rows * p.cols, quads = stride / 4;
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (q >= quads) return;
+  const float* src = p.part[blockIdx.y] + 4 * q;
+  f32x4 s = *(const f32x4*)src;
+#pragma unroll 8
+  for (int i = 1; i < p.parts; ++i) s += *(const f32x4*)(src + i * stride);
+  const int64_t row = quads < ((int64_t)1 << 31) ? p.by_cols4.quot((int)q) : q / (p.cols / 4);
+  *(bf16x4*)(p.out[blockIdx.y] + row * p.ld[blockIdx.y] + 4 * (q - row * (p.cols / 4))) =
+      bf16x4{(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
 }
 
 constexpr int64_t kCUs = 256;
 
 }  // namespace
 
-void cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, int* q_parts, int* k_parts) {
-  // Parts until there is a workgroup for every CU, none of them shorter than 4
-  // tiles of the streamed axis.
-  auto parts = [](int64_t grid, int64_t tiles) {
+CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk) {
+  // Parts until there is a workgroup for every CU, none of them shorter than
+  // `least` tiles of the streamed axis.
+  auto parts = [](int64_t grid, int64_t tiles, int64_t least) {
     int64_t n = grid > 0 ? kCUs / grid : 1;
-    if (n > tiles / 4) n = tiles / 4;
+    if (n > tiles / least) n = tiles / least;
     return (int)(n > 1 ? n : 1);
   };
-  const int64_t G = Hq / Hk;
-  *q_parts = parts(B * Hk * ((G * Sq + 127) / 128), (Sk + 63) / 64);
-  *k_parts = parts(B * Hk * ((Sk + 127) / 128), G * ((Sq + 63) / 64));
+  const int64_t R = Hq / Hk * Sq;
+  // without keys the dq pass alone runs, and writes zeros
+  if (Sk > 0 && Sk <= 128) return {true, 1, parts(B * Hk, (R + 63) / 64, 2)};
+  return {false, parts(B * Hk * ((R + 127) / 128), (Sk + 63) / 64, 4), parts(B * Hk * ((Sk + 127) / 128), (R + 63) / 64, 4)};
 }
 
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s) {
   const int64_t nbh = (int64_t)p.B * p.Hk;
-  if (pass == CROSS_DQ) {
-    const int64_t nqb = ((int64_t)p.G * p.Sq + 127) / 128;
-    hipLaunchKernelGGL(cross_bwd_dq_kernel, dim3((unsigned)(nqb * nbh * p.q_parts)), dim3(NT), 0, s, p);
-  } else {
-    const dim3 grid((unsigned)((p.Sk + 127) / 128 * nbh * p.k_parts));
-    if (pass == CROSS_DV)
-      hipLaunchKernelGGL(cross_bwd_dkv_kernel<1>, grid, dim3(NT), 0, s, p);
-    else
-      hipLaunchKernelGGL(cross_bwd_dkv_kernel<2>, grid, dim3(NT), 0, s, p);
-  }
+  const dim3 by_rows((unsigned)(((int64_t)p.G * p.Sq + 127) / 128 * nbh * p.q_parts));
+  const dim3 by_keys((unsigned)((p.Sk + 127) / 128 * nbh * p.k_parts));
+  const bool even = 16 % p.G == 0;
+  if (pass == CROSS_DQ)
+    hipLaunchKernelGGL(cross_bwd_dq_kernel, by_rows, dim3(NT), 0, s, p);
+  else if (pass == CROSS_ALL)
+    hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>, by_keys, dim3(NT), 0, s, p);
+  else if (pass == CROSS_DV)
+    hipLaunchKernelGGL((even ? cross_bwd_dkv_kernel<1, true> : cross_bwd_dkv_kernel<1, false>), by_keys, dim3(NT), 0, s, p);
+  else
+    hipLaunchKernelGGL((even ? cross_bwd_dkv_kernel<2, true> : cross_bwd_dkv_kernel<2, false>), by_keys, dim3(NT), 0, s, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_part_sum(const PartSum& p, hipStream_t s) {
+  const dim3 grid((unsigned)((p.rows * p.cols / 4 + 255) / 256), (unsigned)p.n);
+  hipLaunchKernelGGL(part_sum_kernel, grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

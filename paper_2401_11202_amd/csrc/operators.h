@@ -7,6 +7,23 @@
 
 namespace partir {
 
+// Division of 0 <= n < 2^31 by a divisor that the host knows: a high product,
+// an addition and a shift (with L = ceil(log2 d) and m = floor(2^32 (2^L - d) /
+// d) + 1, n / d = (hi32(m n) + n) >> L), where the compiler's division by a
+// variable is some 30 dependent instructions before a kernel's first load.
+struct Div {
+  uint32_t m, l, d;
+  static Div by(uint32_t d) {
+    uint32_t l = 0;
+    while (((uint64_t)1 << l) < d) ++l;
+    return Div{(uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1), l, d};
+  }
+  __device__ __forceinline__ int quot(int n) const {
+    return (int)((__umulhi(m, (uint32_t)n) + (uint32_t)n) >> l);
+  }
+  __device__ __forceinline__ int rem(int n, int q) const { return n - q * (int)d; }
+};
+
 // ---- rotary positions, alone or after a norm of each head (rotary.hip) ------
 // Index 0 is the queries, 1 the keys; a tensor without heads is not read.
 struct RotaryParams {
@@ -54,6 +71,7 @@ struct CrossParams {
   const int32_t* lens;     // [B] valid keys of each sequence, or NULL: Sk
   int64_t ldq, ldk, ldv, ldo;
   int B, Sq, Sk, Hq, Hk, G;
+  Div by_g, by_hk, by_nbh, by_nqb, by_split;   // G, Hk, B Hk, the row blocks of a (sequence, key head), nsplit
   float scale_log2;        // scale * log2(e)
   // key axis in nsplit parts (see cross_range): unnormalised outputs and
   // softmax statistics of the parts, joined by the combine launch
@@ -75,8 +93,10 @@ hipError_t launch_cross_combine(const CrossParams& p, hipStream_t s);
 struct CrossRange {
   int begin, end, parts;   // [begin, end), and how many parts hold keys
 };
-__host__ __device__ __forceinline__ CrossRange cross_range(int len, int nsplit, int split) {
-  const int nblk = (len + 63) / 64, per = (nblk + nsplit - 1) / nsplit;
+__device__ __forceinline__ CrossRange cross_range(int len, const Div& by_split, int split) {
+  const int nblk = (len + 63) / 64;
+  if (by_split.d == 1) return CrossRange{0, len, nblk > 0};
+  const int per = by_split.quot(nblk + (int)by_split.d - 1);
   CrossRange r;
   r.parts = per ? (nblk + per - 1) / per : 0;
   const long long b = (long long)split * per * 64, e = b + (long long)per * 64;
@@ -85,9 +105,10 @@ __host__ __device__ __forceinline__ CrossRange cross_range(int len, int nsplit, 
   return r;
 }
 
-// Gradients (cross_attention_bwd.hip).  The dq pass takes the key axis in
-// q_parts parts, the dk / dv passes the query axis in k_parts; more than one
-// part means fp32 partials for an ordered reduction.
+// Gradients (cross_attention_bwd.hip).  Up to 128 keys a sequence: one pass.
+// Above: a dq pass, which takes the key axis in q_parts parts, and dk and dv
+// passes.  The passes that yield dk and dv take the query rows in k_parts;
+// more than one part means fp32 partials for an ordered reduction.
 struct CrossBwdParams {
   const uint16_t *Q, *K, *V, *O, *dO;
   const float* lse;
@@ -98,12 +119,27 @@ struct CrossBwdParams {
   int64_t ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv;
   int B, Sq, Sk, Hq, Hk, G;
   int q_parts, k_parts;
+  Div by_g, by_hk, by_nbh, by_q_parts, by_k_parts;   // G, Hk, B Hk, the counts of parts
   float scale, scale_log2;
 };
-// (q_parts, k_parts)
-void cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, int* q_parts, int* k_parts);
-enum CrossBwdPass { CROSS_DQ, CROSS_DV, CROSS_DK };
+struct CrossBwdChoice {
+  bool one_pass;
+  int q_parts, k_parts;
+};
+CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
+enum CrossBwdPass { CROSS_ALL, CROSS_DQ, CROSS_DV, CROSS_DK };
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s);
+// Sums of parts of up to two matrices [rows, cols] with as many columns: out
+// (bf16, leading dim ld) = sum over the parts, in order.
+struct PartSum {
+  const float* part[2];
+  uint16_t* out[2];
+  int64_t ld[2];
+  int64_t rows;
+  int cols, parts, n;      // n matrices
+  Div by_cols4;            // cols / 4
+};
+hipError_t launch_part_sum(const PartSum& p, hipStream_t s);
 
 // ---- global norm of many tensors (grad_norm.hip) ----------------------------
 constexpr int kGradTensors = 112;             // tensors of one launch's table

@@ -15,7 +15,6 @@
 #include <vector>
 
 #include "../../include/partir.h"
-#include "kernels.h"
 #include "operators.h"
 
 namespace partir {
@@ -345,6 +344,11 @@ int run_cross(const void* Q, const void* K, const void* V, void* O, float* lse, 
   p.B = (int)z.B; p.Sq = (int)z.Sq; p.Sk = (int)z.Sk; p.Hq = (int)z.Hq; p.Hk = (int)z.Hk; p.G = (int)(z.Hq / z.Hk);
   p.scale_log2 = scale * kLog2e;
   p.nsplit = plan.c.nsplit;
+  p.by_g = Div::by(p.G);
+  p.by_hk = Div::by(p.Hk);
+  p.by_nbh = Div::by((uint32_t)(z.B * z.Hk));
+  p.by_nqb = Div::by((uint32_t)cdiv((int64_t)p.G * z.Sq, 32 * plan.c.qw));
+  p.by_split = Div::by(p.nsplit);
   if (p.nsplit > 1) {
     p.Opart = (float*)ws;
     p.MLpart = (float2*)((char*)ws + plan.o_bytes);
@@ -356,30 +360,24 @@ int run_cross(const void* Q, const void* K, const void* V, void* O, float* lse, 
 }
 
 struct CrossBwdPlan {
-  int q_parts = 1, k_parts = 1;
+  CrossBwdChoice c{};
   size_t d_bytes = 0, q_bytes = 0, k_bytes = 0;   // k_bytes: of dK's and of dV's partials each
   size_t ws() const { return d_bytes + q_bytes + 2 * k_bytes; }
 };
 CrossBwdPlan plan_cross_bwd(const CrossSizes& z) {
   CrossBwdPlan p;
-  if (z.B == 0) return p;
-  cross_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk, &p.q_parts, &p.k_parts);
-  p.d_bytes = align_up((size_t)z.B * z.Sq * z.Hq * 4);
-  if (p.q_parts > 1) p.q_bytes = align_up((size_t)p.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
-  if (p.k_parts > 1) p.k_bytes = align_up((size_t)p.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
+  p.c = cross_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk);
+  if (!p.c.one_pass) p.d_bytes = align_up((size_t)z.B * z.Sq * z.Hq * 4);
+  if (p.c.q_parts > 1) p.q_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
+  if (p.c.k_parts > 1) p.k_bytes = align_up((size_t)p.c.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
   return p;
 }
 
-// out (bf16) = sum over the parts, in order
-hipError_t reduce_parts(const float* partial, int parts, int64_t rows, int64_t cols, void* out, int64_t ld, hipStream_t s) {
-  ReduceParams r{};
-  r.partial = partial;
-  r.part_ld = cols;
-  r.part_stride = rows * cols;
-  r.R = parts; r.M = (int)rows; r.N = (int)cols;
-  r.C = out; r.ldc = ld;
-  r.out_bf16 = 1;
-  return launch_splitk_reduce(r, s);
+PartSum part_sum(int n, int parts, int64_t rows, int64_t cols) {
+  PartSum r{};
+  r.n = n; r.parts = parts; r.rows = rows; r.cols = (int)cols;
+  r.by_cols4 = Div::by((uint32_t)(cols / 4));
+  return r;
 }
 
 void fill_info(partir_plan_info* info, int shards, int launches, size_t ws, double flops) {
@@ -561,8 +559,12 @@ int partir_plan_cross_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int6
     if (int st = validate_cross(z)) return st;
     if (!info) return fail(PARTIR_E_NULL, "info must be non-NULL");
     const CrossBwdPlan p = plan_cross_bwd(z);
-    const int nq = B * Sq ? 1 + (p.q_parts > 1) : 0, nk = B * Sk ? 2 * (1 + (p.k_parts > 1)) : 0;
-    fill_info(info, std::max(p.q_parts, p.k_parts), nq + nk, p.ws(),
+    int launches = 0;
+    if (p.c.one_pass)
+      launches = B ? 1 + (p.c.k_parts > 1) : 0;
+    else
+      launches = (B * Sq ? 1 + (p.c.q_parts > 1) : 0) + (B * Sk ? 2 + (p.c.k_parts > 1) : 0);
+    fill_info(info, std::max(p.c.q_parts, p.c.k_parts), launches, p.ws(),
               10.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
     return PARTIR_OK;
   });
@@ -600,22 +602,36 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
     p.dVpart = (float*)(base + plan.d_bytes + plan.q_bytes + plan.k_bytes);
     p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.ldg = lddo; p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
     p.B = (int)B; p.Sq = (int)Sq; p.Sk = (int)Sk; p.Hq = (int)n_heads; p.Hk = (int)n_kv_heads; p.G = (int)(n_heads / n_kv_heads);
-    p.q_parts = plan.q_parts; p.k_parts = plan.k_parts;
+    p.q_parts = plan.c.q_parts; p.k_parts = plan.c.k_parts;
+    p.by_g = Div::by(p.G);
+    p.by_hk = Div::by(p.Hk);
+    p.by_nbh = Div::by((uint32_t)(B * n_kv_heads));
+    p.by_q_parts = Div::by(p.q_parts);
+    p.by_k_parts = Div::by(p.k_parts);
     p.scale = scale;
     p.scale_log2 = scale * kLog2e;
     if (int st = begin_launches()) return st;
     hipStream_t s = (hipStream_t)stream;
-    if (Tq > 0) {
-      if (int st = launched(launch_cross_backward(p, CROSS_DQ, s), "cross_bwd_dq")) return st;
-      if (p.q_parts > 1)
-        if (int st = launched(reduce_parts(p.dQpart, p.q_parts, Tq, cq, dQ, lddq, s), "cross_bwd_dq.reduce")) return st;
+    if (plan.c.one_pass) {   // so there are keys
+      if (int st = launched(launch_cross_backward(p, CROSS_ALL, s), "cross_bwd")) return st;
+    } else {
+      if (Tq > 0) {
+        if (int st = launched(launch_cross_backward(p, CROSS_DQ, s), "cross_bwd_dq")) return st;
+        if (p.q_parts > 1) {
+          PartSum r = part_sum(1, p.q_parts, Tq, cq);
+          r.part[0] = p.dQpart; r.out[0] = p.dQ; r.ld[0] = lddq;
+          if (int st = launched(launch_part_sum(r, s), "cross_bwd_dq.sum")) return st;
+        }
+      }
+      if (Tk == 0) return PARTIR_OK;
+      if (int st = launched(launch_cross_backward(p, CROSS_DV, s), "cross_bwd_dv")) return st;
+      if (int st = launched(launch_cross_backward(p, CROSS_DK, s), "cross_bwd_dk")) return st;
     }
-    if (Tk == 0) return PARTIR_OK;
-    if (int st = launched(launch_cross_backward(p, CROSS_DV, s), "cross_bwd_dv")) return st;
-    if (int st = launched(launch_cross_backward(p, CROSS_DK, s), "cross_bwd_dk")) return st;
     if (p.k_parts == 1) return PARTIR_OK;
-    if (int st = launched(reduce_parts(p.dVpart, p.k_parts, Tk, ck, dV, lddv, s), "cross_bwd_dv.reduce")) return st;
-    return launched(reduce_parts(p.dKpart, p.k_parts, Tk, ck, dK, lddk, s), "cross_bwd_dk.reduce");
+    PartSum r = part_sum(2, p.k_parts, Tk, ck);
+    r.part[0] = p.dKpart; r.out[0] = p.dK; r.ld[0] = lddk;
+    r.part[1] = p.dVpart; r.out[1] = p.dV; r.ld[1] = lddv;
+    return launched(launch_part_sum(r, s), "cross_bwd_dkv.sum");
   });
 }
 
