@@ -33,7 +33,7 @@ __device__ __forceinline__ int key_count(const CrossParams& p, int b) {
 template <int QW, int KG, int BKV, int NS, int OCC>
 __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(CrossParams p) {
   constexpr int NSUB = BKV / 32;
-  constexpr int LPB = 2 * BKV / (4 * QW);                       // tile loads of a wave per block
+  constexpr int LPB = 2 * BKV / (4 * QW);                       // tile loads of a wave per block, K and V
   constexpr int T_BYTES = BKV * ROWB, STAGE = 2 * T_BYTES;      // K tile, then V tile
   constexpr int ND = 4 / KG, PER = QW * 64;                     // 32-wide blocks of O that a key group finishes
   constexpr int MERGE = KG * (KG - 1) * ND * PER * 64, ML = KG * PER * 8;
@@ -79,13 +79,16 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
   const uint16_t* kbase = p.K + (int64_t)b * p.Sk * p.ldk + kvh * DH;
   const uint16_t* vbase = p.V + (int64_t)b * p.Sk * p.ldv + kvh * DH;
   char* const stages = smem + kg * NS * STAGE;
-  // key block kb of the part; the addresses are 64-bit, so a part may hold any
-  // number of bytes
-  auto gload = [&](int kb, int buf) {
+  // K or V of key block kb of the part into a stage; the addresses are 64-bit, so
+  // a part may hold any number of bytes
+  auto kload = [&](int kb, int buf) {
     const int64_t k0 = range.begin + (int64_t)kb * BKV;
-    const int rows = (int)min((int64_t)BKV, range.end - k0);
-    tile_load<BKV, QW>(kbase + k0 * p.ldk, p.ldk, rows, stages + buf * STAGE, w, lane);
-    tile_load<BKV, QW>(vbase + k0 * p.ldv, p.ldv, rows, stages + buf * STAGE + T_BYTES, w, lane);
+    tile_load<BKV, QW>(kbase + k0 * p.ldk, p.ldk, (int)min((int64_t)BKV, range.end - k0), stages + buf * STAGE, w, lane);
+  };
+  auto vload = [&](int kb, int buf) {
+    const int64_t k0 = range.begin + (int64_t)kb * BKV;
+    tile_load<BKV, QW>(vbase + k0 * p.ldv, p.ldv, (int)min((int64_t)BKV, range.end - k0), stages + buf * STAGE + T_BYTES, w,
+                       lane);
   };
 
   f32x16 oacc[4];
@@ -97,89 +100,123 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
   const int nkb = (range.end - range.begin + BKV - 1) / BKV;
   const float sl2 = p.scale_log2;
 
-  // A ring of NS stages: loads run NS - 1 blocks ahead.  Blocks behind the last
-  // are loaded too (no row of them is read: zeros), which keeps the counts of
-  // loads in flight constant.
+  // Rings of NS stages for K and for V: loads run ahead, and blocks behind the
+  // last are loaded too (no row of them is read: zeros), which keeps the counts
+  // of loads in flight constant.  Where a wave has its stages to itself (QW = 1)
+  // nothing but its own loads is waited for, and a stage is loaded anew as soon
+  // as its products are done; else a barrier a block says that everyone's loads
+  // have landed and that the stage loaded next is done with.
+  constexpr bool ALONE = QW == 1;
+  static_assert(!ALONE || NS == 2, "two blocks in flight");
 #pragma unroll
-  for (int n = 0; n < NS - 1; ++n) gload(n * KG + kg, n);
+  for (int n = 0; n < NS - !ALONE; ++n) {
+    kload(n * KG + kg, n);
+    vload(n * KG + kg, n);
+  }
   auto block = [&](auto stage_c, int kb) {
     constexpr int cur = decltype(stage_c)::value;
     __builtin_amdgcn_sched_barrier(0);
-    WAIT_VMCNT(LPB * (NS - 2));          // this wave's loads of the block have landed
-    asm volatile("s_barrier" ::: "memory");   // everyone's have, and the stage loaded next is done with
+    if constexpr (ALONE) {
+      WAIT_VMCNT(3 * LPB / 2);             // after this K: its V, the next K and V
+      asm volatile("" ::: "memory");
+    } else {
+      WAIT_VMCNT(LPB * (NS - 2));
+      asm volatile("s_barrier" ::: "memory");
+    }
     __builtin_amdgcn_sched_barrier(0);
-    gload(kb + KG * (NS - 1), (cur + NS - 1) % NS);
-    if (KG == 1 || kb < nkb) {
-      const char* ks = stages + cur * STAGE;
-      const char* vs = ks + T_BYTES;
-      __builtin_amdgcn_s_setprio(1);
-      f32x16 sacc[NSUB];
+    if constexpr (!ALONE) {
+      kload(kb + KG * (NS - 1), (cur + NS - 1) % NS);
+      vload(kb + KG * (NS - 1), (cur + NS - 1) % NS);
+    }
+    if (!ALONE && KG > 1 && kb >= nkb) return;
+    const char* ks = stages + cur * STAGE;
+    const char* vs = ks + T_BYTES;
+    __builtin_amdgcn_s_setprio(1);
+    f32x16 sacc[NSUB];
 #pragma unroll
-      for (int t = 0; t < NSUB; ++t) {
-        zero(sacc[t]);
+    for (int t = 0; t < NSUB; ++t) {
+      zero(sacc[t]);
 #pragma unroll
-        for (int ds = 0; ds < 8; ++ds) sacc[t] = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], sacc[t]);
-      }
-      __builtin_amdgcn_s_setprio(0);
-      const int left = range.end - (range.begin + kb * BKV);   // keys from this block on
-      if (left < BKV) {
+      for (int ds = 0; ds < 8; ++ds) sacc[t] = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], sacc[t]);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if constexpr (ALONE) {
+      __builtin_amdgcn_sched_barrier(0);   // the products hold what they read of the stage
+      WAIT_LGKMCNT(0);
+      asm volatile("" ::: "memory");
+      kload(kb + KG * NS, cur);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const int left = range.end - (range.begin + kb * BKV);   // keys from this block on
+    if (left < BKV) {
 #pragma unroll
-        for (int t = 0; t < NSUB; ++t)
+      for (int t = 0; t < NSUB; ++t)
 #pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= left) sacc[t][v] = -__builtin_inff();
-      }
-      float lsum = 0.0f;
-      bf16x8 pf[2 * NSUB];
-      auto weights = [&]() {
-        lsum = 0.0f;
+        for (int v = 0; v < 16; ++v)
+          if (32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= left) sacc[t][v] = -__builtin_inff();
+    }
+    float lsum = 0.0f;
+    bf16x8 pf[2 * NSUB];
+    auto weights = [&]() {
+      lsum = 0.0f;
 #pragma unroll
-        for (int t = 0; t < NSUB; ++t)
+      for (int t = 0; t < NSUB; ++t)
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][v], sl2, -m_run));
-            lsum += e;
-            pf[2 * t + (v >> 3)][v & 7] = (__bf16)e;
-          }
-      };
-      // m moves only where the block's maximum is more than 8 (log2 units)
-      // above it: weights stay below 2^8, exact range in float32 and bf16, and
-      // O is rescaled in few blocks.  A lane whose weights sum to at most 2^8
-      // has none above, so the maximum is taken only where some lane's sum is
-      // larger (or inf / NaN, as on the first block, where m is -1e30).
-      weights();
-      if (__builtin_amdgcn_ballot_w64(!(lsum <= 256.0f)) != 0) {
-        float mloc = -__builtin_inff();
-#pragma unroll
-        for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) mloc = fmaxf(mloc, sacc[t][v]);
-        mloc = fmaxf(mloc, __shfl_xor(mloc, 32));   // the partner lane holds the row's other keys
-        const float m_blk = mloc * sl2;
-        const bool move = m_blk > m_run + 8.0f;
-        if (__builtin_amdgcn_ballot_w64(move) != 0) {
-          const float m_new = move ? m_blk : m_run;
-          const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-          l_run *= alpha;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) oacc[d] *= alpha;
-          m_run = m_new;
-          weights();
+        for (int v = 0; v < 16; ++v) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][v], sl2, -m_run));
+          lsum += e;
+          pf[2 * t + (v >> 3)][v & 7] = (__bf16)e;
         }
+    };
+    // m moves only where the block's maximum is more than 8 (log2 units)
+    // above it: weights stay below 2^8, exact range in float32 and bf16, and
+    // O is rescaled in few blocks.  A lane whose weights sum to at most 2^8
+    // has none above, so the maximum is taken only where some lane's sum is
+    // larger (or inf / NaN, as on the first block, where m is -1e30).
+    weights();
+    if (__builtin_amdgcn_ballot_w64(!(lsum <= 256.0f)) != 0) {
+      float mloc = -__builtin_inff();
+#pragma unroll
+      for (int t = 0; t < NSUB; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mloc = fmaxf(mloc, sacc[t][v]);
+      mloc = fmaxf(mloc, __shfl_xor(mloc, 32));   // the partner lane holds the row's other keys
+      const float m_blk = mloc * sl2;
+      const bool move = m_blk > m_run + 8.0f;
+      if (__builtin_amdgcn_ballot_w64(move) != 0) {
+        const float m_new = move ? m_blk : m_run;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        l_run *= alpha;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) oacc[d] *= alpha;
+        m_run = m_new;
+        weights();
       }
-      l_run += lsum;
+    }
+    l_run += lsum;
+    if constexpr (ALONE) {
+      __builtin_amdgcn_sched_barrier(0);
+      WAIT_VMCNT(3 * LPB / 2);             // after this V: the next K and V, the K after
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
-      for (int u = 0; u < BKV / 16; ++u)
+    for (int u = 0; u < BKV / 16; ++u)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) oacc[d] = mfma(tr.read(vs, u, d), pf[u], oacc[d]);
+      for (int d = 0; d < 4; ++d) oacc[d] = mfma(tr.read(vs, u, d), pf[u], oacc[d]);
+    if constexpr (ALONE) {
+      __builtin_amdgcn_sched_barrier(0);
+      WAIT_LGKMCNT(0);
+      asm volatile("" ::: "memory");
+      vload(kb + KG * NS, cur);
     }
   };
   // NS blocks a trip, so that a block's stage is a constant and folds into the
-  // reads' offsets.  Every barrier is the workgroup's: the trip count does not
-  // depend on the group.
+  // reads' offsets.  With barriers the trip count is the workgroup's, not the
+  // group's.
   for (int kb = 0; kb < nkb; kb += NS * KG) {
-    block(std::integral_constant<int, 0>{}, kb + kg);
-    if (kb + KG < nkb) block(std::integral_constant<int, 1>{}, kb + KG + kg);
+    if (!ALONE || kb + kg < nkb) block(std::integral_constant<int, 0>{}, kb + kg);
+    if (ALONE ? kb + KG + kg < nkb : kb + KG < nkb) block(std::integral_constant<int, 1>{}, kb + KG + kg);
     if constexpr (NS > 2) {
       if (kb + 2 * KG < nkb) block(std::integral_constant<int, 2>{}, kb + 2 * KG + kg);
     }

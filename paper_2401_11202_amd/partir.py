@@ -909,10 +909,11 @@ def _rotary_args(Q, K, freqs, d_head, positions, S):
 
 def _rotary_new(Q, K, T):
     """New outputs of a rotary call and their leading dims."""
-    q = _torch.empty((T, Q.shape[1]), dtype=Q.dtype, device=Q.device)
+    cq = Q.shape[1]
     if K is None:
-        return (q, None), Q.shape[1], 0
-    return (q, _torch.empty((T, K.shape[1]), dtype=Q.dtype, device=Q.device)), Q.shape[1], K.shape[1]
+        return (Q.new_empty((T, cq)), None), cq, 0
+    ck = K.shape[1]
+    return (Q.new_empty((T, cq)), Q.new_empty((T, ck))), cq, ck
 
 
 def _rotary_given(out, names, Q, K, T):
@@ -1052,7 +1053,7 @@ def _cross_forward(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens, scal
         _gpu_all(Q=Q, K=K, V=V, k_lens=k_lens, out=out, lse=lse)
     dev = Q.device
     if fresh_o:
-        out = torch.empty((Tq, n_heads * d_head), dtype=torch.bfloat16, device=dev)
+        out = Q.new_empty((Tq, n_heads * d_head))
     if fresh_l:
         lse = torch.empty((Tq, n_heads), dtype=torch.float32, device=dev)
     ws, wsb = _workspace(dev, workspace, lib().partir_cross_attention_workspace, B, Sq, Sk, n_heads, Hk, d_head)
@@ -1088,8 +1089,7 @@ def cross_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, n
         _gpu_all(Q=Q, K=K, V=V, O=O, dO=dO, lse=lse, k_lens=k_lens, out=out)
     dev = Q.device
     if fresh:
-        out = (torch.empty((Tq, cq), dtype=bf, device=dev), torch.empty((Tk, ck), dtype=bf, device=dev),
-               torch.empty((Tk, ck), dtype=bf, device=dev))
+        out = (Q.new_empty((Tq, cq)), Q.new_empty((Tk, ck)), Q.new_empty((Tk, ck)))
     ws, wsb = _workspace(dev, workspace, lib().partir_cross_attention_backward_workspace, B, Sq, Sk, n_heads, Hk, d_head)
     _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()))
     _launch(dev, lib().partir_cross_attention_backward, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(lse),
@@ -1123,13 +1123,13 @@ def _grad_arrays(tensors, name):
         dtypes = list(map(T.dtype.__get__, tensors))
         dense = all(map(T.is_contiguous, tensors))
         devs = set(map(T.get_device, tensors))
-        ptrs, numel = array("Q", map(T.data_ptr, tensors)), array("q", map(T.numel, tensors))
+        ptrs, numel = array("Q", list(map(T.data_ptr, tensors))), array("q", list(map(T.numel, tensors)))
     except TypeError:
         i = next(i for i, t in enumerate(tensors) if not isinstance(t, T))
         _bad("PARTIR_E_NULL", f"{name}[{i}] must be a tensor")
     codes = {torch.float32: F32, torch.bfloat16: BF16}
     try:
-        dts = array("i", map(codes.__getitem__, dtypes))
+        dts = array("i", [codes[d] for d in dtypes])
     except KeyError:
         i = next(i for i, d in enumerate(dtypes) if d not in codes)
         _bad("PARTIR_E_DTYPE", f"{name}[{i}] has dtype {dtypes[i]}, expected float32 or bfloat16")
