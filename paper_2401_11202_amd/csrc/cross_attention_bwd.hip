@@ -44,7 +44,7 @@ __device__ __forceinline__ int key_count(const CrossBwdParams& p, int b) {
 // behind it zeros.  Where G divides 16, a lane's rows lie at one offset from a
 // tile's first position and a fixed step apart; else each is divided by G (8 %
 // of the dk and dv passes).
-template <bool EVEN>
+template <bool EVEN, int WAVES = 4>
 struct RowTiles {
   const uint16_t *q, *g;
   int64_t ldq, ldg;
@@ -55,7 +55,7 @@ struct RowTiles {
       : q(p.Q + (int64_t)b * p.Sq * p.ldq + kvh * p.G * DH), g(p.dO + (int64_t)b * p.Sq * p.ldg + kvh * p.G * DH), ldq(p.ldq),
         ldg(p.ldg), by_g(p.by_g), R(p.G * p.Sq), w(w_), lane(lane_) {
     const int l4 = lane >> 4, r = 4 * w + l4, s = by_g.quot(r);
-    chunk = ((lane & 15) ^ (l4 << 2) ^ (w & 3)) << 4;   // row 16 j + r sits at the same chunk for every j
+    chunk = ((lane & 15) ^ (l4 << 2) ^ (w & 3)) << 4;   // row 4 WAVES j + r sits at the same chunk for every j
     const uint32_t in = (uint32_t)by_g.rem(r, s) * ROWB + chunk;
     oq = (uint32_t)s * (uint32_t)(ldq * 2) + in;
     og = (uint32_t)s * (uint32_t)(ldg * 2) + in;
@@ -66,18 +66,18 @@ struct RowTiles {
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(q + s0 * ldq, (uint32_t)((sl - s0) * ldq * 2) + tail);
     const __amdgpu_buffer_rsrc_t rg = make_rsrc(g + s0 * ldg, (uint32_t)((sl - s0) * ldg * 2) + tail);
     auto put = [&](int j, uint32_t a, uint32_t b) {
-      char* const t = tile + (4 * j + w) * 1024;
+      char* const t = tile + (WAVES * j + w) * 1024;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)t, 16, a, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, (lds_void*)(t + TILE), 16, b, 0, 0, 0);
     };
     if constexpr (EVEN) {
-      const uint32_t n = by_g.quot(16), sq = n * (uint32_t)(ldq * 2), sg = n * (uint32_t)(ldg * 2);
+      const uint32_t n = by_g.quot(4 * WAVES), sq = n * (uint32_t)(ldq * 2), sg = n * (uint32_t)(ldg * 2);
 #pragma unroll
-      for (int j = 0; j < TR / 16; ++j) put(j, oq + j * sq, og + j * sg);
+      for (int j = 0; j < TR / (4 * WAVES); ++j) put(j, oq + j * sq, og + j * sg);
     } else {
 #pragma unroll
-      for (int j = 0; j < TR / 16; ++j) {
-        const int i = i0 + 16 * j + 4 * w + (lane >> 4), s = by_g.quot(i);
+      for (int j = 0; j < TR / (4 * WAVES); ++j) {
+        const int i = i0 + 4 * (WAVES * j + w) + (lane >> 4), s = by_g.quot(i);
         const uint32_t in = (uint32_t)by_g.rem(i, s) * ROWB + chunk;
         put(j, (uint32_t)(s - s0) * (uint32_t)(ldq * 2) + in, (uint32_t)(s - s0) * (uint32_t)(ldg * 2) + in);
       }
@@ -358,201 +358,165 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
     store(smem, w, DO_K ? p.dK : p.dV, tk * (DO_K ? p.lddk : p.lddv) + kvh * DH, rows, acc, f, lane);
 }
 
-// dS of a 64-row tile as [128 keys][64 rows] bf16: 16-byte chunk c of key k at
-// position c ^ ds_swz(k).  The writes of a wave's 32 keys (8 bytes a lane, one
-// column) spread over 16 positions, and a transposed read (4 keys x 64 bytes)
-// over all banks: two keys share a 256-byte line of banks, keys 2 apart take
-// its other half.
-__device__ __forceinline__ int ds_swz(int key) { return (((key >> 1) & 1) << 2) ^ ((key >> 2) & 3); }
-__device__ __forceinline__ int ds_off(int key, int colb) {
-  return key * 128 + (((colb >> 4) ^ ds_swz(key)) << 4) + (colb & 15);
-}
-
 // All three gradients in one pass where a sequence has at most 128 keys: S and
 // dP are formed once (5 products instead of 8), and D = sum_j P_j dP_j comes
 // from the weights themselves, so that O is not read and its rounding to bf16,
 // which with few keys is of the size of the other roundings, stays out.
-// Workgroup = the keys of a (sequence, key head) and a part of its query rows:
-// four waves of 32 keys hold K and V as operands and dK and dV as sums; rows
-// come in tiles of 64.  Per tile a wave forms S = Q K^T and dP = dO V^T of its
-// keys and dV^T += dO^T P; the waves add up D, go on to dS and dK^T += Q^T dS, and
-// leave dS in LDS; then each takes 32 columns of dQ^T = K^T dS^T over all keys,
-// with its K^T operands in registers.  Some 350 registers: one wave a SIMD, one
-// workgroup a CU.
+// Workgroup = the keys of a (sequence, key head) and a part of its query rows,
+// in tiles of 64; eight waves, two row halves x four groups of 32 keys, with K
+// and V as operands in registers.  Per tile
+//   a wave forms S^T = K Q^T and dP^T = V dO^T of its keys and rows (a lane owns a
+//     row), and leaves P and its share of D in LDS;
+//   with D, dS goes to LDS too, and dV^T += dO^T P over all rows, for its keys and
+//     half of the columns (the row half is the column half here);
+//   then dK^T += Q^T dS likewise, and 32 columns of dQ^T = K^T dS^T of its rows over
+//     all keys.
+// Three barriers a tile, the next one's loads in flight across them.  Two waves
+// a SIMD, one workgroup a CU.  (With the rows of S on the lanes' registers
+// instead, four waves of 32 keys and D from sums over lanes, 350 registers and
+// one wave a SIMD, it took 35 us for 2 x 4096 queries, 77 keys and 8 heads; 25 so.)
 template <bool EVEN>
-__global__ __launch_bounds__(NT, 1) void cross_bwd_one_pass_kernel(CrossBwdParams p) {
-  constexpr int DS = 2 * 2 * TILE;                   // after the two stages
-  constexpr int ROWS = DS + 128 * 128;               // the waves' row areas
-  constexpr int STAT = ROWS + 4 * row_area<1, __bf16>();
-  __shared__ __attribute__((aligned(1024))) char smem[STAT + 6 * TR * 4];
-  float (*const stat)[TR] = (float (*)[TR])(smem + STAT);   // [stage][-lse / c]
-  float (*const dsum)[TR] = stat + 2;                       // [wave]: its keys' share of D
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+__global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdParams p) {
+  // Two stages of Q and dO first: offsets below 64 KiB fold into the LDS
+  // instructions, so that both share their address registers.
+  constexpr int STAGES = 0, KT = 2 * 2 * TILE;       // K
+  constexpr int EP = KT + 128 * ROWB;                // P and dS of a tile, [64 rows][128 keys] as tiles
+  constexpr int ES = EP + TILE;
+  constexpr int DSUM = ES + TILE;                    // [key group][row]: shares of D
+  constexpr int ROWS = DSUM + 4 * TR * 4;            // the waves' row areas
+  __shared__ __attribute__((aligned(1024))) char smem[ROWS + 8 * row_area<1, __bf16>()];
+  static_assert(8 * row_area<2, float>() <= EP, "the end goes through the stages and K");
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = lane >> 5, col = lane & 31;
+  const int half = w & 1, kg = w >> 1;
 
   const int part = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, part);
   const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
-  const int len = key_count(p, b), R = p.G * p.Sq;
-  const int kj = 32 * w + col;                       // this lane's key
-  const bool on = kj < len;
+  const int R = p.G * p.Sq, tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
+  const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
+  const int len = key_count(p, b);
 
-  // K into the first stage, V into the second (rows behind len are zeros)
+  // K for good, V through the first stage (rows behind len are zeros)
   const int64_t tk0 = (int64_t)b * p.Sk;
-  tile_load<128, 4>(p.K + tk0 * p.ldk + kvh * DH, p.ldk, len, smem, w, lane);
-  tile_load<128, 4>(p.V + tk0 * p.ldv + kvh * DH, p.ldv, len, smem + 2 * TILE, w, lane);
+  tile_load<128, 8>(p.K + tk0 * p.ldk + kvh * DH, p.ldk, len, smem + KT, w, lane);
+  tile_load<128, 8>(p.V + tk0 * p.ldv + kvh * DH, p.ldv, len, smem + STAGES, w, lane);
+  const RowTiles<EVEN, 8> rt(p, b, kvh, w, lane);
   TileTr tr;
   tr.init(lane);
   WAIT_VMCNT(0);
   __syncthreads();
-  bf16x8 kf[8], vf[8], kt[8];
+  bf16x8 vf[8];
 #pragma unroll
-  for (int ds = 0; ds < 8; ++ds) {
-    kf[ds] = tile_rows(smem, 32 * w, col, h, ds);
-    vf[ds] = tile_rows(smem + 2 * TILE, 32 * w, col, h, ds);
-    kt[ds] = tr.read(smem, ds, w);                   // K^T: columns 32 w.., keys 16 ds..
-  }
+  for (int ds = 0; ds < 8; ++ds) vf[ds] = tile_rows(smem + STAGES, 32 * kg, col, h, ds);
   __syncthreads();
 
-  const int tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
-  const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
-  const RowTiles<EVEN> rt(p, b, kvh, w, lane);
-  const float c = p.scale_log2, inv_c = 1.0f / p.scale_log2;
-  float st_l = 0.0f;
+  const float c = p.scale_log2;
+  float lse_next = 0.0f;
+  // tile `it` into a stage, and the log-sum-exp of this lane's row of it
   auto gload = [&](int it, int buf) {
-    rt.load(it, smem + buf * 2 * TILE);
-    if (tid < TR) {
-      const int i = min(it * TR + tid, R - 1), sq = p.by_g.quot(i);
-      st_l = p.lse[((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq)];
-    }
+    rt.load(it, smem + STAGES + buf * 2 * TILE);
+    const int i = min(it * TR + 32 * half + col, R - 1), sq = p.by_g.quot(i);
+    lse_next = p.lse[((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq)];
   };
-  auto sstore = [&](int it, int buf) {   // a missing row: P = 2^-inf
-    if (tid < TR) lds_write((char*)&stat[buf][tid], it * TR + tid < R ? -st_l * inv_c : -__builtin_inff());
-  };
-  f32x16 dk[4], dv[4];
+  f32x16 dk[2], dv[2];
 #pragma unroll
-  for (int d = 0; d < 4; ++d) {
+  for (int d = 0; d < 2; ++d) {
     zero(dk[d]);
     zero(dv[d]);
   }
+  const int erow = 32 * half + col;                  // this lane's row of P and dS
   auto iter = [&](int it, auto stage) {
     constexpr int cur = decltype(stage)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    WAIT_VMCNT(0);                                   // the tile and lse have landed
+    lds_barrier();
+    const int row = it * TR + erow;
+    const float lse = row < R ? lse_next : __builtin_inff();   // a missing row: P = 0
     if (it + 1 < it1) gload(it + 1, cur ^ 1);
-    const char* qs = smem + cur * 2 * TILE;
+    const char* qs = smem + STAGES + cur * 2 * TILE;
     const char* gs = qs + TILE;
-    f32x16 s[2], dp[2];
+    f32x16 s, dp;
+    zero(s);
+    zero(dp);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int ds = 0; ds < 8; ++ds) {
+      s = mfma(tile_rows(smem + KT, 32 * kg, col, h, ds), tile_rows(qs, 32 * half, col, h, ds), s);
+      dp = mfma(vf[ds], tile_rows(gs, 32 * half, col, h, ds), dp);
+    }
+    // element v: key 32 kg + 8 (v / 4) + 4 h + v % 4
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse));
+    if (len < 32 * kg + 32) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (32 * kg + 8 * (v >> 2) + 4 * h + (v & 3) >= len) s[v] = 0.0f;
+    }
+    float d = 0.0f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) d = __builtin_fmaf(s[v], dp[v], d);
+    d += __shfl_xor(d, 32);
+    auto put = [&](char* e, f32x16 x) {   // four consecutive keys a lane and write
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const f32x4 l4 = lds_read<f32x4>((const char*)&stat[cur][32 * t + 8 * q + 4 * h]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[t][4 * q + j] = l4[j];
+        const bf16x4 o = {(__bf16)x[4 * q + 0], (__bf16)x[4 * q + 1], (__bf16)x[4 * q + 2], (__bf16)x[4 * q + 3]};
+        lds_write(e + tile_off(erow, 64 * kg + 16 * q + 8 * h), o);
       }
-      zero(dp[t]);
+    };
+    put(smem + EP, s);
+    if (h == 0) lds_write(smem + DSUM + (kg * TR + erow) * 4, d);
+    lds_barrier();
+    float D = 0.0f;
 #pragma unroll
-      for (int ds = 0; ds < 8; ++ds) {
-        s[t] = mfma(tile_rows(qs, 32 * t, col, h, ds), kf[ds], s[t]);
-        dp[t] = mfma(tile_rows(gs, 32 * t, col, h, ds), vf[ds], dp[t]);
-      }
-    }
-    // P, its share of D, dV
+    for (int g = 0; g < 4; ++g) D += lds_read<float>(smem + DSUM + (g * TR + erow) * 4);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      bf16x8 pf[2];
-      float x[16];
+    for (int v = 0; v < 16; ++v) dp[v] = s[v] * (dp[v] - D);
+    put(smem + ES, dp);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        s[t][v] = on ? __builtin_amdgcn_exp2f(s[t][v] * c) : 0.0f;
-        x[v] = s[t][v] * dp[t][v];
-      }
+    for (int u = 0; u < 4; ++u) {
+      const bf16x8 pf = tr.read(smem + EP, u, kg);
 #pragma unroll
-      for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[t][v], s[t][v + 1]);
-      // The sums of x over the 32 keys: each step halves the rows a lane holds
-      // and doubles the keys in them; lane col ends with row element col / 2.
-#pragma unroll
-      for (int m = 16, n = 8; m >= 2; m >>= 1, n >>= 1) {
-        const bool up = (col & m) != 0;
-#pragma unroll
-        for (int e = 0; e < n; ++e) {
-          const float keep = up ? x[e + n] : x[e], send = up ? x[e] : x[e + n];
-          x[e] = keep + __shfl_xor(send, m);
-        }
-      }
-      x[0] += __shfl_xor(x[0], 1);
-      if (!(col & 1)) lds_write((char*)&dsum[w][32 * t + 8 * (col >> 3) + 4 * h + ((col >> 1) & 3)], x[0]);
-#pragma unroll
-      for (int uu = 0; uu < 2; ++uu)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * t + uu, d), pf[uu], dv[d]);
+      for (int e = 0; e < 2; ++e) dv[e] = mfma(tr.read(gs, u, 2 * half + e), pf, dv[e]);
     }
     lds_barrier();
-    // dS, dK, and dS for everyone
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      bf16x8 df[2];
+    for (int u = 0; u < 4; ++u) {
+      const bf16x8 df = tr.read(smem + ES, u, kg);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int r = 32 * t + 8 * q + 4 * h;
-        f32x4 D = lds_read<f32x4>((const char*)&dsum[0][r]);
-#pragma unroll
-        for (int u = 1; u < 4; ++u) D += lds_read<f32x4>((const char*)&dsum[u][r]);
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const int v = 4 * q + j;   // P is 0 for keys behind len, whose dP is 0
-          put2(df[v >> 3], v & 7, s[t][v] * (dp[t][v] - D[j]), s[t][v + 1] * (dp[t][v + 1] - D[j + 1]));
-        }
-        const bf16x4 o = {df[q >> 1][4 * (q & 1) + 0], df[q >> 1][4 * (q & 1) + 1], df[q >> 1][4 * (q & 1) + 2],
-                          df[q >> 1][4 * (q & 1) + 3]};
-        lds_write(smem + DS + ds_off(kj, 2 * r), o);
-      }
-#pragma unroll
-      for (int uu = 0; uu < 2; ++uu)
-#pragma unroll
-        for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, 2 * t + uu, d), df[uu], dk[d]);
+      for (int e = 0; e < 2; ++e) dk[e] = mfma(tr.read(qs, u, 2 * half + e), df, dk[e]);
     }
-    if (it + 1 < it1) sstore(it + 1, cur ^ 1);
-    WAIT_VMCNT(0);
-    __syncthreads();
-    // dQ^T: columns 32 w.. of both 32-row halves over all keys
+    f32x16 dq;
+    zero(dq);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      f32x16 dq;
-      zero(dq);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int key = 16 * u + tr.row, colb = 64 * t + tr.colb;
-        const lds_i16x4_t lo = lds_read_tr16(smem + DS + ds_off(key, colb));
-        const lds_i16x4_t hi = lds_read_tr16(smem + DS + ds_off(key + 8, colb));
-        dq = mfma(kt[u], __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), dq);
-      }
-      const int i = it * TR + 32 * t + col, ic = min(i, R - 1), sq = p.by_g.quot(ic);
-      store_rows<1>(smem + ROWS + w * row_area<1, __bf16>(), (__bf16*)p.dQ,
-                    ((int64_t)b * p.Sq + sq) * p.lddq + (kvh * p.G + p.by_g.rem(ic, sq)) * DH + 32 * w, R - it * TR - 32 * t,
-                    &dq, p.scale, lane);
+    for (int u = 0; u < 8; ++u) {
+      // keys 16 u + 4 h.. and 16 u + 8 + 4 h.. of this lane's row, the order of the transposed reads
+      const lds_i16x4_t lo = lds_read<lds_i16x4_t>(smem + ES + tile_off(erow, 32 * u + 8 * h));
+      const lds_i16x4_t hi = lds_read<lds_i16x4_t>(smem + ES + tile_off(erow, 32 * u + 16 + 8 * h));
+      dq = mfma(tr.read(smem + KT, u, kg),
+                __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), dq);
     }
+    const int rc = min(row, R - 1), sq = p.by_g.quot(rc);
+    store_rows<1>(smem + ROWS + w * row_area<1, __bf16>(), (__bf16*)p.dQ,
+                  ((int64_t)b * p.Sq + sq) * p.lddq + (kvh * p.G + p.by_g.rem(rc, sq)) * DH + 32 * kg, R - it * TR - 32 * half,
+                  &dq, p.scale, lane);
   };
-  if (it0 < it1) {
-    gload(it0, 0);
-    sstore(it0, 0);
-  }
-  WAIT_VMCNT(0);
-  __syncthreads();
+  if (it0 < it1) gload(it0, 0);
   for (int it = it0; it < it1; it += 2) {
     iter(it, std::integral_constant<int, 0>{});
     if (it + 1 < it1) iter(it + 1, std::integral_constant<int, 1>{});
   }
-  __syncthreads();   // the last tile's dS is read
-  // Q's rows of keys behind len met P = 0, so their sums are 0
+  __syncthreads();
+  // 32 keys x 64 columns of dK and dV; keys behind len met P = 0 only
+  const int kj = 32 * kg + col, rows = p.Sk - 32 * kg;
   const int64_t tk = tk0 + kj;
-  const int rows = p.Sk - 32 * w;
+  char* const area = smem + w * row_area<2, float>();
   if (p.k_parts > 1) {
-    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH;
-    store(smem, w, p.dKpart, at, rows, dk, p.scale, lane);
-    store(smem, w, p.dVpart, at, rows, dv, 1.0f, lane);
+    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH + 64 * half;
+    store_rows<2>(area, p.dKpart, at, rows, dk, p.scale, lane);
+    store_rows<2>(area, p.dVpart, at, rows, dv, 1.0f, lane);
   } else {
-    store(smem, w, p.dK, tk * p.lddk + kvh * DH, rows, dk, p.scale, lane);
-    store(smem, w, p.dV, tk * p.lddv + kvh * DH, rows, dv, 1.0f, lane);
+    store_rows<2>(area, (__bf16*)p.dK, tk * p.lddk + kvh * DH + 64 * half, rows, dk, p.scale, lane);
+    store_rows<2>(area, (__bf16*)p.dV, tk * p.lddv + kvh * DH + 64 * half, rows, dv, 1.0f, lane);
   }
 }
 
@@ -596,7 +560,8 @@ hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hip
   if (pass == CROSS_DQ)
     hipLaunchKernelGGL(cross_bwd_dq_kernel, by_rows, dim3(NT), 0, s, p);
   else if (pass == CROSS_ALL)
-    hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>, by_keys, dim3(NT), 0, s, p);
+    hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>, by_keys, dim3(2 * NT), 0, s,
+                       p);
   else if (pass == CROSS_DV)
     hipLaunchKernelGGL((even ? cross_bwd_dkv_kernel<1, true> : cross_bwd_dkv_kernel<1, false>), by_keys, dim3(NT), 0, s, p);
   else
