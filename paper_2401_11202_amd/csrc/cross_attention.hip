@@ -18,6 +18,7 @@
 // descriptor ends before them), so what the padding holds, NaN included, does
 // not reach a product, and their scores are -inf.  A sequence without keys
 // gives 0 and a log-sum-exp of -inf.
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_tiles.h"
@@ -352,14 +353,15 @@ CrossChoice cross_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t 
   CrossChoice c;
   c.qw = rows <= 32 ? 1 : 4;
   const int64_t grid = B * Hk * ((rows + 32 * c.qw - 1) / (32 * c.qw));
-  c.nsplit = 1;
-  if (grid < kCUs) {
-    // the key axis in parts until there is a workgroup for every CU, none of
-    // them shorter than 4 blocks of 64 keys
-    int64_t n = kCUs / (grid > 0 ? grid : 1);
-    if (n > blocks / 4) n = blocks / 4;
-    if (n > 1) c.nsplit = (int)n;
-  }
+  // The key axis in parts where workgroups are few.  A workgroup takes 0.33 us for
+  // 64 keys of a tile of 32 rows and 0.77 us of one of 128 (measured at 8 to 64
+  // workgroups); 1000 rows of a part cost 0.2 us.  Unsplit / split so: 1 query, 32/8
+  // heads, 4096 keys 27 / 15 us, 1024 keys 10.5 / 14.5; 512 queries, 4 heads, 2048
+  // keys 32 / 18; 1024 queries, 8 heads, 1024 keys 21 / 25.  Above 64 parts joining
+  // them costs more than it saves (one key head, 65536 keys: 16 us with 64, 19
+  // with 256).
+  const int64_t most = grid > 0 ? std::min<int64_t>(std::min(kCUs / grid, blocks), 64) : 1;
+  c.nsplit = best_parts(most, blocks, c.qw == 1 ? 0.33 : 0.77, 2e-4 * (double)(B * Sq * Hq));
   if (c.qw == 1) {
     c.kg = 4;
     c.block = 32;

@@ -88,6 +88,23 @@ CrossChoice cross_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t 
 hipError_t launch_cross_attention(const CrossParams& p, const CrossChoice& c, hipStream_t s);
 hipError_t launch_cross_combine(const CrossParams& p, hipStream_t s);
 
+// The count of parts, up to `most`, that takes the least time: n parts leave a
+// workgroup steps / n steps of step_us, and from two on cost a launch that joins
+// them (about 5 us) and part_us each, their float32 rows written and read.
+inline int best_parts(int64_t most, int64_t steps, double step_us, double part_us) {
+  int best = 1;
+  double least = (double)steps * step_us;
+  for (int64_t n = 2; n <= most;) {
+    const double us = (double)((steps + n - 1) / n) * step_us + 5.0 + (double)n * part_us;
+    if (us < least) {
+      least = us;
+      best = (int)n;
+    }
+    n = n < most && 2 * n > most ? most : 2 * n;   // powers of two, and the most
+  }
+  return best;
+}
+
 // Keys of part `split` of nsplit of a sequence with len keys: whole blocks of
 // 64, shared out evenly; parts behind the last block are empty.
 struct CrossRange {
