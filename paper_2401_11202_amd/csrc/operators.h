@@ -49,8 +49,8 @@ struct RotaryParams {
 };
 // The token block, load width and grid of a call (host rule; the pointers are
 // not looked at).  Sets vec, tb, blocks and grid.
-void rotary_choice(RotaryParams& p, bool bf16, bool backward);
-constexpr int kRotaryMaxGrid = 2048, kRotaryMaxBwdGrid = 1024;
+enum RotaryPass { ROTARY, ROTARY_NORM, ROTARY_NORM_BWD };
+void rotary_choice(RotaryParams& p, bool bf16, RotaryPass pass);
 hipError_t launch_rotary(const RotaryParams& p, bool bf16, bool interleaved, bool norm, hipStream_t s);
 // Gradients of the norm and rotation together; gain gradients as partials.
 hipError_t launch_qk_norm_backward(const RotaryParams& p, bool bf16, bool interleaved, hipStream_t s);

@@ -122,7 +122,7 @@ int check_eps(float eps) {
 int run_rotary(RotaryParams& p, int dtype, int interleaved, bool norm, void* stream) {
   if (int st = validate_rotary(p, dtype)) return st;
   if (p.T == 0 || p.H[0] + p.H[1] == 0) return PARTIR_OK;
-  rotary_choice(p, dtype == PARTIR_BF16, false);
+  rotary_choice(p, dtype == PARTIR_BF16, norm ? ROTARY_NORM : ROTARY);
   if (int st = begin_launches()) return st;
   return launched(launch_rotary(p, dtype == PARTIR_BF16, interleaved != 0, norm, (hipStream_t)stream),
                   norm ? "qk_norm_rotary" : "rotary");
@@ -145,7 +145,7 @@ RotaryParams rotary_args(const void* Q, const void* K, void* Qo, void* Ko, const
 }
 
 // What the backward pass's workspace holds: a partial gain gradient for both
-// tensors from each workgroup, at most kRotaryMaxBwdGrid of them.
+// tensors from each workgroup.
 size_t qk_norm_backward_ws(const RotaryParams& p) {
   if (p.T <= 0 || p.H[0] + p.H[1] <= 0) return 0;
   return align_up((size_t)p.grid * 2 * p.dh * sizeof(float));
@@ -467,7 +467,7 @@ size_t partir_qk_norm_rotary_backward_workspace(int64_t T, int64_t n_heads, int6
   });
   if (st) return (size_t)-1;
   p.T = T;
-  rotary_choice(p, dtype == PARTIR_BF16, true);
+  rotary_choice(p, dtype == PARTIR_BF16, ROTARY_NORM_BWD);
   return qk_norm_backward_ws(p);
 }
 
@@ -490,7 +490,7 @@ int partir_qk_norm_rotary_backward(const void* Q, const void* K, const void* dQo
     if (!aligned(dgq, 4) || !aligned(dgk, 4)) return fail(PARTIR_E_LAYOUT, "gain gradients must be 4-byte aligned");
     const bool empty = p.T == 0 || p.H[0] + p.H[1] == 0;
     if (!empty) {
-      rotary_choice(p, dtype == PARTIR_BF16, true);
+      rotary_choice(p, dtype == PARTIR_BF16, ROTARY_NORM_BWD);
       if (int st = check_ws(qk_norm_backward_ws(p), ws, ws_bytes)) return st;
       p.dgpart = (float*)ws;
     }

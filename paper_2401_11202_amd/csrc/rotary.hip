@@ -357,17 +357,20 @@ hipError_t bwd(const RotaryParams& p, bool inter, hipStream_t s) {
 
 }  // namespace
 
-void rotary_choice(RotaryParams& p, bool bf16, bool backward) {
+void rotary_choice(RotaryParams& p, bool bf16, RotaryPass pass) {
   int v = bf16 ? 8 : 4;
   while (v > 1 && (p.rd % (2 * v) || p.dh % (2 * v))) v >>= 1;
   p.vec = v;
   const int lanes = pow2_ceil(p.dh / (2 * v)) < 64 ? pow2_ceil(p.dh / (2 * v)) : 64;
   const int64_t slots = NT / lanes;
   // Tokens of a block: enough rows for every row group where there are that
-  // many, few enough that the blocks fill the chip.
+  // many, few enough that the blocks fill the chip.  The rotation alone likes many
+  // short workgroups (8192 x 80 heads of 128: 75 us with 2048, 67 with 8192), with
+  // the norm the gains that each of them reads first count (8192 x 64 heads: 60
+  // with 2048, 69 with 8192), and the gradients leave a partial each.
+  const int64_t max_grid = pass == ROTARY ? 8192 : pass == ROTARY_NORM ? 2048 : 1024;
   const int H = p.H[0] + p.H[1];
-  const int64_t rows = p.T * H, max_grid = backward ? kRotaryMaxBwdGrid : kRotaryMaxGrid;
-  int64_t want = rows / max_grid;
+  int64_t want = p.T * H / max_grid;
   if (want < slots) want = slots;
   int64_t tb = H > 0 ? (want + H - 1) / H : 1;
   if (tb > MAX_TB) tb = MAX_TB;
