@@ -589,8 +589,8 @@ int partir_cross_attention_train(const void* Q, const void* K, const void* V, vo
 /* Gradients of partir_cross_attention for the cotangent dO of O, from the
  * forward's O and lse (formulas as partir_attention_backward).  dQ as Q; dK and
  * dV as K and V, summed over the query heads of a key head; keys behind
- * k_lens get zeros.  Every gradient is summed in a fixed order, without
- * atomics.  Workspace: the rowsums of dO * O and, where the queries or keys are
+ * k_lens get zeros.  The gradients must be apart from each other and from the
+ * inputs.  Every gradient is summed in a fixed order, without atomics.  Workspace: the rowsums of dO * O and, where the queries or keys are
  * few, fp32 parts of the gradients. */
 int partir_cross_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
                                     const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
@@ -615,7 +615,7 @@ int partir_grad_norm(const void* const* tensors, const int64_t* numel, const int
  * pointers; out[i] = tensors[i] scales in place (nothing is written where the
  * norm is within max_norm).  Where an element is infinite or NaN, so is the
  * norm, and nothing is scaled: the tensors are copied as they are.  Outputs must be apart from
- * each other and from other tensors' inputs (E_LAYOUT).  max_norm >= 0
+ * each other, from norm and from other tensors' inputs (E_LAYOUT).  max_norm >= 0
  * (E_UNSUPPORTED otherwise). */
 int partir_clip_grad_norm(const void* const* tensors, void* const* out, const int64_t* numel, const int* dtypes, int n,
                           double max_norm, float* norm, void* ws, size_t ws_bytes, void* stream);

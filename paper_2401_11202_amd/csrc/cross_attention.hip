@@ -27,6 +27,10 @@
 namespace partir {
 namespace {
 
+// The running maximum before the first key: below every finite score, and a
+// finite number, so that 2^(kNoMax - kNoMax) is 1.
+constexpr float kNoMax = -3.0e38f;
+
 __device__ __forceinline__ int key_count(const CrossParams& p, int b) {
   return p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
 }
@@ -95,7 +99,7 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
   f32x16 oacc[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) zero(oacc[d]);
-  float m_run = -1e30f, l_run = 0.0f;
+  float m_run = kNoMax, l_run = 0.0f;
   TileTr tr;
   tr.init(lane);
   const int nkb = (range.end - range.begin + BKV - 1) / BKV;
@@ -173,7 +177,7 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
     // above it: weights stay below 2^8, exact range in float32 and bf16, and
     // O is rescaled in few blocks.  A lane whose weights sum to at most 2^8
     // has none above, so the maximum is taken only where some lane's sum is
-    // larger (or inf / NaN, as on the first block, where m is -1e30).
+    // larger (or inf / NaN, as on the first block, where m is kNoMax).
     weights();
     if (__builtin_amdgcn_ballot_w64(!(lsum <= 256.0f)) != 0) {
       float mloc = -__builtin_inff();
@@ -248,11 +252,11 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
       }
     __syncthreads();
     float2 st[KG];
-    m_run = -1e30f;
+    m_run = kNoMax;
 #pragma unroll
     for (int g = 0; g < KG; ++g) {
       st[g] = ml[g * PER];
-      m_run = fmaxf(m_run, st[g].x);   // a group without keys holds (-1e30, 0, 0)
+      m_run = fmaxf(m_run, st[g].x);   // a group without keys holds (kNoMax, 0, 0)
     }
     f32x16 own[ND];
 #pragma unroll
@@ -316,7 +320,7 @@ __global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams p) {
   const int64_t tq = row / p.Hq;
   const int head = (int)(row - tq * p.Hq), b = (int)(tq / p.Sq);
   const int parts = cross_range(key_count(p, b), p.by_split, 0).parts;
-  float M = -3.0e38f;
+  float M = kNoMax;
   for (int s = c4; s < parts; s += 32) M = fmaxf(M, p.MLpart[s * rows + row].x);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));

@@ -37,6 +37,7 @@ struct RotaryParams {
   int64_t ldx[2], lddy[2], ldy[2];
   int64_t T, S;
   int H[2];
+  Div by_s, by_half, by_h, by_hw[2];   // S, rd / 2, H[0] + H[1], each H (1 for 0)
   int dh, rd;
   int pos64;               // positions are int64 (else int32)
   int vec;                 // values of a load (8, 4, 2, 1): 2 vec divides rd and dh
@@ -48,7 +49,7 @@ struct RotaryParams {
   float eps;
 };
 // The token block, load width and grid of a call (host rule; the pointers are
-// not looked at).  Sets vec, tb, blocks and grid.
+// not looked at).  Sets vec, tb, blocks, grid and the divisors.
 enum RotaryPass { ROTARY, ROTARY_NORM, ROTARY_NORM_BWD };
 void rotary_choice(RotaryParams& p, bool bf16, RotaryPass pass);
 hipError_t launch_rotary(const RotaryParams& p, bool bf16, bool interleaved, bool norm, hipStream_t s);

@@ -112,6 +112,17 @@ int validate_rotary(const RotaryParams& p, int dtype) {
     if (st) return st;
     if (!aligned(p.g[i], 16)) return fail(PARTIR_E_LAYOUT, "gains must be 16-byte aligned");
   }
+  if (p.T == 0) return PARTIR_OK;
+  for (int i = 0; i < 2; ++i) {
+    if (p.H[i] == 0) continue;
+    // in place means row for row; the other tensor's rows are read at other times
+    if ((p.y[i] == p.x[i] && p.T > 1 && p.ldy[i] != p.ldx[i]) ||
+        (p.lddy[i] >= 0 && p.y[i] == p.dy[i] && p.T > 1 && p.ldy[i] != p.lddy[i]))
+      return fail(PARTIR_E_LAYOUT, "an output in its input's place needs its leading dim");
+    const int o = 1 - i;
+    if (p.H[o] > 0 && (p.y[i] == p.x[o] || p.y[i] == p.y[o] || (p.lddy[o] >= 0 && p.y[i] == p.dy[o])))
+      return fail(PARTIR_E_LAYOUT, "the queries' and the keys' tensors share an output");
+  }
   return PARTIR_OK;
 }
 
@@ -180,9 +191,9 @@ struct Span {
 // Every written range is apart from every other and from every read range but
 // its own input's, which it is or is apart from: a value scaled twice, or
 // scaled before it is read, would depend on timing.
-int check_apart(const void* const* in, void* const* out, const int64_t* numel, const int* dtypes, int n) {
+int check_apart(const void* const* in, void* const* out, const int64_t* numel, const int* dtypes, int n, const float* norm) {
   std::vector<Span> w, r;
-  w.reserve(n);
+  w.reserve(n + 1);
   auto span = [&](const void* p, int i) {
     const uintptr_t lo = (uintptr_t)p;
     return Span{lo, lo + (uintptr_t)numel[i] * (dtypes[i] == PARTIR_BF16 ? 2 : 4), i};
@@ -192,18 +203,20 @@ int check_apart(const void* const* in, void* const* out, const int64_t* numel, c
     w.push_back(span(out[i], i));
     if (in[i] != out[i]) r.push_back(span(in[i], i));
   }
+  w.push_back(Span{(uintptr_t)norm, (uintptr_t)(norm + 1), n});
   auto before = [](const Span& a, const Span& b) { return a.lo < b.lo; };
   if (!std::is_sorted(w.begin(), w.end(), before)) std::sort(w.begin(), w.end(), before);
   if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
   for (size_t k = 1; k < w.size(); ++k)
     if (w[k].lo < w[k - 1].hi)
-      return fail(PARTIR_E_LAYOUT, "tensors %d and %d overlap", std::min(w[k].i, w[k - 1].i), std::max(w[k].i, w[k - 1].i));
+      return fail(PARTIR_E_LAYOUT, "tensors %d and %d overlap (%d: norm)", std::min(w[k].i, w[k - 1].i),
+                  std::max(w[k].i, w[k - 1].i), n);
   // inputs may overlap one another: the last end among those before counts
   size_t k = 0;
   for (const Span& s : r) {
     while (k < w.size() && w[k].hi <= s.lo) ++k;
     if (k < w.size() && w[k].lo < s.hi)
-      return fail(PARTIR_E_LAYOUT, "the output of tensor %d overlaps the input of tensor %d", w[k].i, s.i);
+      return fail(PARTIR_E_LAYOUT, "the output of tensor %d (%d: norm) overlaps the input of tensor %d", w[k].i, n, s.i);
   }
   return PARTIR_OK;
 }
@@ -249,7 +262,7 @@ int run_grads(const void* const* in, void* const* out, const int64_t* numel, con
   if (!aligned(norm, 4)) return fail(PARTIR_E_LAYOUT, "norm must be 4-byte aligned");
   if (int st = check_ws(grad_ws(n), ws, ws_bytes)) return st;
   if (clip)
-    if (int st = check_apart(in, out, numel, dtypes, n)) return st;
+    if (int st = check_apart(in, out, numel, dtypes, n, norm)) return st;
   std::vector<GradLaunch> all;
   all.reserve((size_t)cdiv(n, kGradTensors));
   grad_launches(in, out, numel, dtypes, n, all);
@@ -585,6 +598,10 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
         {"dQ", dQ, Tq, cq, lddq}, {"dK", dK, Tk, ck, lddk}, {"dV", dV, Tk, ck, lddv}};
     for (const auto& m : all)
       if (int st = check_matrix(m.name, m.p, m.rows, m.cols, m.ld, 2)) return st;
+    for (int o = 5; o < 8; ++o)
+      for (int i = 0; i < 8; ++i)
+        if (i != o && all[o].rows * all[i].rows > 0 && all[o].p == all[i].p)
+          return fail(PARTIR_E_LAYOUT, "%s must not be %s", all[o].name, all[i].name);
     if (int st = check_lens(k_lens)) return st;
     if (Tq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
     if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");

@@ -81,13 +81,13 @@ __device__ __host__ __forceinline__ int pow2_ceil(int n) {
 __device__ __forceinline__ void angles(const RotaryParams& p, int64_t t0, int nt, float2* cs) {
   const int half = p.rd >> 1;
   for (int e = threadIdx.x; e < nt * half; e += NT) {
-    const int k = e / half, i = e - k * half;
+    const int k = p.by_half.quot(e), i = p.by_half.rem(e, k);
     const int64_t t = t0 + k;
     double pos;
     if (p.pos)
       pos = p.pos64 ? (double)((const int64_t*)p.pos)[t] : (double)((const int32_t*)p.pos)[t];
     else
-      pos = (double)(t % p.S);
+      pos = (double)p.by_s.rem((int)t, p.by_s.quot((int)t));
     const double turns = pos * (p.freqs[i] * 0.15915494309189533577);   // 1 / (2 pi)
     const float f = (float)(turns - rint(turns));
     float s, c;
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryParams p) {
     angles(p, t0, nt, cs);
     __syncthreads();
     for (int r = slot; r < nt * H; r += slots) {
-      const int k = r / H, hh = r - k * H;
+      const int k = p.by_h.quot(r), hh = p.by_h.rem(r, k);
       const int w = hh >= p.H[0];
       const int head = w ? hh - p.H[0] : hh;
       const T* x = (const T*)p.x[w] + (t0 + k) * p.ldx[w] + head * p.dh;
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(NT) void qk_norm_backward_kernel(RotaryParams p) {
       angles(p, t0, nt, cs);
       __syncthreads();
       for (int r = slot; r < nt * H; r += slots) {
-        const int k = r / H, head = r - k * H;
+        const int k = p.by_hw[w].quot(r), head = p.by_hw[w].rem(r, k);
         float x[C][2 * V], u[C][2 * V];
         lane.load((const T*)p.x[w] + (t0 + k) * p.ldx[w] + head * p.dh, x);
         lane.load((const T*)p.dy[w] + (t0 + k) * p.lddy[w] + head * p.dh, u);
@@ -378,6 +378,11 @@ void rotary_choice(RotaryParams& p, bool bf16, RotaryPass pass) {
   p.tb = (int)tb;
   p.blocks = (p.T + tb - 1) / tb;
   p.grid = (int)(p.blocks < max_grid ? p.blocks : max_grid);
+  auto by = [](int64_t d) { return Div::by((uint32_t)(d > 1 ? d : 1)); };
+  p.by_s = by(p.S < p.T ? p.S : p.T);   // S >= T: row t stands at t
+  p.by_half = by(p.rd / 2);
+  p.by_h = by(H);
+  for (int w = 0; w < 2; ++w) p.by_hw[w] = by(p.H[w]);
 }
 
 hipError_t launch_rotary(const RotaryParams& p, bool bf16, bool interleaved, bool norm, hipStream_t s) {

@@ -892,10 +892,12 @@ def _rotary_args(Q, K, freqs, d_head, positions, S):
     ldk = 0 if K is None else _matrix(K, "K", T, ck, dt)
     rd = p64 = 0
     if freqs is not None:
-        if freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+        if not isinstance(freqs, torch.Tensor) or freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
             _bad("PARTIR_E_DTYPE", "freqs must be a dense 1-D float64 tensor")
         rd = 2 * freqs.shape[0]
     if positions is not None:
+        if not isinstance(positions, torch.Tensor):
+            _bad("PARTIR_E_NULL", "positions must be a tensor")
         if positions.dtype is torch.int64:
             p64 = 1
         elif positions.dtype is not torch.int32:
@@ -904,7 +906,7 @@ def _rotary_args(Q, K, freqs, d_head, positions, S):
             _bad("PARTIR_E_SHAPE", f"positions has shape {tuple(positions.shape)}, expected {(T,)}")
         if not positions.is_contiguous():
             _bad("PARTIR_E_LAYOUT", "positions must be contiguous")
-    return T, cq // d_head, ck // d_head, rd, (T if S is None else S) or 1, ldq, ldk, code, p64
+    return T, cq // d_head, ck // d_head, rd, max(T, 1) if S is None else S, ldq, ldk, code, p64
 
 
 def _rotary_new(Q, K, T):

@@ -11,6 +11,7 @@ from oracle import operators_oracle as OO
 from paper_2401_11202_amd import partir as P
 
 A, ODD, NULL = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x10004), None
+T1, T2, T3, T4, T5, T6, T7, T8 = (ctypes.c_void_p(0x100000 * i) for i in range(1, 9))   # tensors apart
 bf, f32 = torch.bfloat16, torch.float32
 
 
@@ -32,7 +33,7 @@ def status(fn):
 # ---------------------------------------------------------------------------
 # rotary and norms
 # ---------------------------------------------------------------------------
-ROT = dict(Q=A, K=A, Qo=A, Ko=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128, ldqo=256,
+ROT = dict(Q=T1, K=T2, Qo=T3, Ko=T4, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128, ldqo=256,
            ldko=128, dt=P.BF16, inter=0, inv=0, mag=1.0)
 
 
@@ -72,9 +73,9 @@ def test_nothing_to_do_launches_nothing():
     assert rotary(Hq=0, Hk=0, Q=NULL, K=NULL, Qo=NULL, Ko=NULL) == "PARTIR_OK"
 
 
-NORM = dict(Q=A, K=A, gq=A, gk=A, Qo=A, Ko=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128,
+NORM = dict(Q=T1, K=T2, gq=A, gk=A, Qo=T3, Ko=T4, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128,
             ldqo=256, ldko=128, dt=P.BF16, inter=0, mag=1.0, eps=1e-6)
-BWD = dict(Q=A, K=A, dQo=A, dKo=A, gq=A, gk=A, dQ=A, dK=A, dgq=A, dgk=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64,
+BWD = dict(Q=T1, K=T2, dQo=T3, dKo=T4, gq=A, gk=A, dQ=T5, dK=T6, dgq=A, dgk=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64,
            rd=64, ldq=256, ldk=128, lddqo=256, lddko=128, lddq=256, lddk=128, dt=P.BF16, inter=0, mag=1.0, eps=1e-6, ws=A,
            wsb=1 << 24)
 
@@ -242,7 +243,7 @@ def test_clip_binding_checks():
 # ---------------------------------------------------------------------------
 CROSS = dict(Q=A, K=A, V=A, O=A, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256, ldv=256, ldo=512, lens=NULL, scale=0.0,
              ws=NULL, wsb=0)
-CROSS_BWD = dict(Q=A, K=A, V=A, O=A, dO=A, lse=A, dQ=A, dK=A, dV=A, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256,
+CROSS_BWD = dict(Q=T1, K=T2, V=T3, O=T4, dO=T5, lse=A, dQ=T6, dK=T7, dV=T8, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256,
                  ldv=256, ldo=512, lddo=512, lddq=512, lddk=256, lddv=256, lens=NULL, scale=0.0, ws=A, wsb=1 << 30)
 
 
@@ -393,3 +394,64 @@ def test_without_keys_the_rowsums_have_their_workspace():
     assert P.plan_cross_attention_backward(2, 3, 0, 4, 2)["n_launches"] == 1
     assert P.plan_cross_attention_backward(2, 0, 5, 4, 2)["n_launches"] == 1
     assert P.plan_cross_attention_backward(0, 3, 5, 4, 2)["n_launches"] == 0
+
+
+# ---------------------------------------------------------------------------
+# tensors in each other's place
+# ---------------------------------------------------------------------------
+def at(x):
+    return ctypes.c_void_p(x)
+
+
+def test_rotary_outputs_are_their_inputs_or_apart():
+    apart = dict(Q=at(0x10000), K=at(0x20000), Qo=at(0x30000), Ko=at(0x40000))
+    assert rotary(**apart) == "PARTIR_E_HIP"
+    assert rotary(**dict(apart, Qo=apart["Q"], Ko=apart["K"])) == "PARTIR_E_HIP"            # in place
+    assert rotary(**dict(apart, Qo=apart["Q"], ldqo=264)) == "PARTIR_E_LAYOUT"
+    assert rotary(**dict(apart, Qo=apart["Q"], ldqo=264, T=1)) == "PARTIR_E_HIP"            # one row: no stride
+    assert rotary(**dict(apart, Qo=apart["K"])) == "PARTIR_E_LAYOUT"
+    assert rotary(**dict(apart, Qo=apart["Ko"])) == "PARTIR_E_LAYOUT"
+    b = dict(apart, dQo=at(0x50000), dKo=at(0x60000), dQ=at(0x70000), dK=at(0x80000))
+    b.pop("Qo"), b.pop("Ko")
+    assert bwd(**b) == "PARTIR_E_HIP"
+    assert bwd(**dict(b, dQ=b["dQo"], dK=b["dKo"])) == "PARTIR_E_HIP"
+    assert bwd(**dict(b, dQ=b["dKo"])) == "PARTIR_E_LAYOUT"
+    assert bwd(**dict(b, dQ=b["dQo"], lddq=512)) == "PARTIR_E_LAYOUT"
+
+
+def test_a_period_below_one_is_refused():
+    q, f = torch.zeros(16, 256, dtype=bf), torch.zeros(32, dtype=torch.float64)
+    for S in (0, -3):
+        assert rotary(S=S) == "PARTIR_E_SHAPE"
+    assert status(lambda: P.rotary(q, None, [1.0], d_head=64)) == "PARTIR_E_DTYPE"
+    assert status(lambda: P.rotary(q, None, f, d_head=64, positions=[0] * 16)) == "PARTIR_E_NULL"
+
+
+def test_cross_attention_gradients_are_apart():
+    names = ("Q", "K", "V", "O", "dO", "dQ", "dK", "dV")
+    p = {n: at(0x10000 * (i + 1)) for i, n in enumerate(names)}
+    assert cross_bwd(**p) == "PARTIR_E_HIP"
+    for o in ("dQ", "dK", "dV"):
+        for i in names:
+            if i != o:
+                assert cross_bwd(**dict(p, **{o: p[i]})) == "PARTIR_E_LAYOUT", (o, i)
+
+
+def test_the_norm_is_apart_from_the_tensors():
+    assert clip([0x20000], [100], [P.F32], norm=at(0x20000 + 396)) == "PARTIR_E_LAYOUT"
+    assert clip([0x20000], [100], [P.F32], norm=at(0x20000 + 400)) == "PARTIR_E_HIP"
+    assert clip([0x20000], [100], [P.F32], out=[0x30000], norm=at(0x20000)) == "PARTIR_E_LAYOUT"
+
+
+def test_division_by_a_product():
+    """The high product, addition and shift that the kernels divide by, as
+    formed on the host, for divisors and dividends around powers of two."""
+    rng = np.random.default_rng(0)
+    ds = sorted({d for k in range(31) for d in (2 ** k - 1, 2 ** k, 2 ** k + 1) if d > 0} | set(rng.integers(1, 2 ** 30, 200).tolist()))
+    for d in ds:
+        l = max(0, int(d - 1).bit_length())
+        m = (((1 << 32) * ((1 << l) - d)) // d + 1) & 0xFFFFFFFF
+        n = np.unique(np.concatenate([rng.integers(0, 2 ** 31, 200), np.arange(5), 2 ** 31 - 1 - np.arange(5),
+                                      np.clip(d * rng.integers(0, max(1, 2 ** 31 // d), 50) + rng.integers(-1, 2, 50), 0, 2 ** 31 - 1)])).astype(np.uint64)
+        s = ((np.uint64(m) * n) >> np.uint64(32)) + n
+        assert (s < 2 ** 32).all() and ((s >> np.uint64(l)) == n // np.uint64(d)).all(), d
