@@ -229,17 +229,17 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
     store(smem, w, p.dQ, tq * p.lddq + head * DH, rows, dq, p.scale, lane);
 }
 
-// MODE 1: dV (S and P, dV^T += dO^T P); MODE 2: dK (S, P and dP, dK^T += Q^T
-// dS).  One pass doing both would hold twice the accumulators, which leaves one
-// wave a SIMD; forming S again costs less.
-template <int MODE, bool EVEN>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void cross_bwd_dkv_kernel(CrossBwdParams p) {
-  constexpr bool DO_K = MODE == 2;
+// dK and dV: eight waves of 32 keys, K as an operand in registers, V in LDS (both
+// as registers would leave one wave a SIMD); rows in tiles of 64.  Per 32 rows a
+// wave forms S and P, dV^T += dO^T P, then dP and dS, dK^T += Q^T dS.
+template <bool EVEN>
+__global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams p) {
+  constexpr int STAGES = 0, VT = 2 * 2 * TILE, STAT = VT + 256 * ROWB;
   // one object: with several, the compiler tells them apart, takes every tile
   // read for one of the tiles being loaded and waits for those
-  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE + 2 * 2 * TR * 4];
-  float (*const stat)[2][TR] = (float (*)[2][TR])(smem + 2 * 2 * TILE);   // [stage][-lse / c, -D][row]
+  __shared__ __attribute__((aligned(1024))) char smem[STAT + 2 * 2 * TR * 4];
+  static_assert(8 * row_area<4, __bf16>() <= STAT && 8 * row_area<2, float>() <= STAT, "the end goes through the stages and V");
+  float (*const stat)[2][TR] = (float (*)[2][TR])(smem + STAT);   // [stage][-lse / c, -D][row]
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, col = lane & 31;
@@ -248,46 +248,47 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
   const int kblk = p.by_k_parts.quot(rest), part = p.by_k_parts.rem(rest, kblk);
   const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
   const int len = key_count(p, b), R = p.G * p.Sq;
-  const int kj = kblk * 128 + 32 * w + col;          // this lane's key
+  const int k0 = kblk * 256, kw = k0 + 32 * w;       // the workgroup's first key, the wave's
+  const int kj = kw + col;                           // this lane's
   const int64_t tk = (int64_t)b * p.Sk + kj;
 
-  f32x16 acc[4];
+  f32x16 dk[4], dv[4];
 #pragma unroll
-  for (int d = 0; d < 4; ++d) zero(acc[d]);
+  for (int d = 0; d < 4; ++d) {
+    zero(dk[d]);
+    zero(dv[d]);
+  }
   // workgroup-uniform: keys behind len_b get zeros
-  if (kblk * 128 < len) {
-    bf16x8 kf[8], vf[8];
+  if (k0 < len) {
+    const int64_t t0 = (int64_t)b * p.Sk + k0;
+    tile_load<256, 8>(p.V + t0 * p.ldv + kvh * DH, p.ldv, min(256, len - k0), smem + VT, w, lane);
+    bf16x8 kf[8];
     {
-      const int64_t t = (int64_t)b * p.Sk + min(kj, p.Sk - 1);
-      const uint16_t* krow = p.K + t * p.ldk + kvh * DH + 8 * h;
-      const uint16_t* vrow = p.V + t * p.ldv + kvh * DH + 8 * h;
+      const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, p.Sk - 1)) * p.ldk + kvh * DH + 8 * h;
 #pragma unroll
-      for (int ds = 0; ds < 8; ++ds) {
-        kf[ds] = *(const bf16x8*)(krow + 16 * ds);
-        if (DO_K) vf[ds] = *(const bf16x8*)(vrow + 16 * ds);
-      }
+      for (int ds = 0; ds < 8; ++ds) kf[ds] = *(const bf16x8*)(krow + 16 * ds);
     }
     const int tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
     const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
-    const RowTiles<EVEN> rt(p, b, kvh, w, lane);
+    const RowTiles<EVEN, 8> rt(p, b, kvh, w, lane);
     const float inv_c = 1.0f / p.scale_log2;
     float st_l = 0.0f, st_d = 0.0f;
     auto gload = [&](int it, int buf) {
-      rt.load(it, smem + buf * 2 * TILE);
+      rt.load(it, smem + STAGES + buf * 2 * TILE);
       if (tid < TR) {
         // nothing looks at the loaded values before sstore: a use here would wait
         // for the tiles' loads too
         const int i = min(it * TR + tid, R - 1), sq = p.by_g.quot(i);
         const int64_t at = ((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq);
         st_l = p.lse[at];
-        if (DO_K) st_d = p.Dstat[at];
+        st_d = p.Dstat[at];
       }
     };
     auto sstore = [&](int it, int buf) {
       if (tid < TR) {
         const bool row = it * TR + tid < R;   // a missing row: P = 2^-inf
         lds_write((char*)&stat[buf][0][tid], row ? -st_l * inv_c : -__builtin_inff());
-        if (DO_K) lds_write((char*)&stat[buf][1][tid], row ? -st_d : 0.0f);
+        lds_write((char*)&stat[buf][1][tid], row ? -st_d : 0.0f);
       }
     };
     TileTr tr;
@@ -296,41 +297,51 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
     auto iter = [&](int it, auto stage) {
       constexpr int cur = decltype(stage)::value;
       if (it + 1 < it1) gload(it + 1, cur ^ 1);
-      const char* qs = smem + cur * 2 * TILE;
+      const char* qs = smem + STAGES + cur * 2 * TILE;
       const char* gs = qs + TILE;
+      if (kw < len) {   // wave-uniform
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t) {
+          // the accumulators start at -lse / c and -D of their rows
+          auto start = [&](f32x16& x, int which) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        // the accumulators start at -lse / c and -D of their rows
-        f32x16 s, dp;
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 v = lds_read<f32x4>((const char*)&stat[cur][which][32 * t + 8 * q + 4 * h]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 l4 = lds_read<f32x4>((const char*)&stat[cur][0][32 * t + 8 * q + 4 * h]);
+              for (int j = 0; j < 4; ++j) x[4 * q + j] = v[j];
+            }
+          };
+          f32x16 s;
+          start(s, 0);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[4 * q + j] = l4[j];
-          if (DO_K) {
-            const f32x4 d4 = lds_read<f32x4>((const char*)&stat[cur][1][32 * t + 8 * q + 4 * h]);
+          for (int ds = 0; ds < 8; ++ds) s = mfma(tile_rows(qs, 32 * t, col, h, ds), kf[ds], s);
+          __builtin_amdgcn_sched_barrier(0);
+          bf16x8 pf[2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) dp[4 * q + j] = d4[j];
+          for (int v = 0; v < 16; v += 2) {
+            s[v] = __builtin_amdgcn_exp2f(s[v] * c);
+            s[v + 1] = __builtin_amdgcn_exp2f(s[v + 1] * c);
+            put2(pf[v >> 3], v & 7, s[v], s[v + 1]);
           }
+          __builtin_amdgcn_sched_barrier(0);
+          f32x16 dp;
+          start(dp, 1);
+#pragma unroll
+          for (int ds = 0; ds < 8; ++ds)
+            dp = mfma(tile_rows(gs, 32 * t, col, h, ds), tile_rows(smem + VT, 32 * w, col, h, ds), dp);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * t + uu, d), pf[uu], dv[d]);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[v] * dp[v], s[v + 1] * dp[v + 1]);
+#pragma unroll
+          for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, 2 * t + uu, d), pf[uu], dk[d]);
         }
-#pragma unroll
-        for (int ds = 0; ds < 8; ++ds) {
-          s = mfma(tile_rows(qs, 32 * t, col, h, ds), kf[ds], s);
-          if (DO_K) dp = mfma(tile_rows(gs, 32 * t, col, h, ds), vf[ds], dp);
-        }
-        bf16x8 pf[2];
-#pragma unroll
-        for (int v = 0; v < 16; v += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(s[v] * c), p1 = __builtin_amdgcn_exp2f(s[v + 1] * c);
-          if (DO_K)
-            put2(pf[v >> 3], v & 7, p0 * dp[v], p1 * dp[v + 1]);
-          else
-            put2(pf[v >> 3], v & 7, p0, p1);
-        }
-#pragma unroll
-        for (int uu = 0; uu < 2; ++uu)
-#pragma unroll
-          for (int d = 0; d < 4; ++d) acc[d] = mfma(tr.read(DO_K ? qs : gs, 2 * t + uu, d), pf[uu], acc[d]);
       }
       if (it + 1 < it1) sstore(it + 1, cur ^ 1);
       WAIT_VMCNT(0);
@@ -348,15 +359,21 @@ void cross_bwd_dkv_kernel(CrossBwdParams p) {
     }
     if (kj >= len) {   // a lane's key is its own column: what its sums hold goes nowhere else
 #pragma unroll
-      for (int d = 0; d < 4; ++d) zero(acc[d]);
+      for (int d = 0; d < 4; ++d) {
+        zero(dk[d]);
+        zero(dv[d]);
+      }
     }
   }
-  const float f = DO_K ? p.scale : 1.0f;
-  const int rows = p.Sk - kblk * 128 - 32 * w;
-  if (p.k_parts > 1)
-    store(smem, w, DO_K ? p.dKpart : p.dVpart, (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH, rows, acc, f, lane);
-  else
-    store(smem, w, DO_K ? p.dK : p.dV, tk * (DO_K ? p.lddk : p.lddv) + kvh * DH, rows, acc, f, lane);
+  const int rows = p.Sk - kw;
+  if (p.k_parts > 1) {
+    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH;
+    store(smem, w, p.dKpart, at, rows, dk, p.scale, lane);
+    store(smem, w, p.dVpart, at, rows, dv, 1.0f, lane);
+  } else {
+    store(smem, w, p.dK, tk * p.lddk + kvh * DH, rows, dk, p.scale, lane);
+    store(smem, w, p.dV, tk * p.lddv + kvh * DH, rows, dv, 1.0f, lane);
+  }
 }
 
 // All three gradients in one pass where a sequence has at most 128 keys: S and
@@ -551,23 +568,23 @@ CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, i
   // without keys the dq pass alone runs, and writes zeros
   if (Sk > 0 && Sk <= 128) return {true, 1, best_parts(most(B * Hk, rows), rows, 2.8, k_us)};
   return {false, best_parts(most(B * Hk * ((R + 127) / 128), keys), keys, 1.45, q_us),
-          best_parts(most(B * Hk * ((Sk + 127) / 128), rows), rows, 3.0, k_us)};
+          best_parts(most(B * Hk * ((Sk + 255) / 256), rows), rows, 3.0, k_us)};
 }
 
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s) {
   const int64_t nbh = (int64_t)p.B * p.Hk;
-  const dim3 by_rows((unsigned)(((int64_t)p.G * p.Sq + 127) / 128 * nbh * p.q_parts));
-  const dim3 by_keys((unsigned)((p.Sk + 127) / 128 * nbh * p.k_parts));
   const bool even = 16 % p.G == 0;
-  if (pass == CROSS_DQ)
-    hipLaunchKernelGGL(cross_bwd_dq_kernel, by_rows, dim3(NT), 0, s, p);
-  else if (pass == CROSS_ALL)
-    hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>, by_keys, dim3(2 * NT), 0, s,
-                       p);
-  else if (pass == CROSS_DV)
-    hipLaunchKernelGGL((even ? cross_bwd_dkv_kernel<1, true> : cross_bwd_dkv_kernel<1, false>), by_keys, dim3(NT), 0, s, p);
-  else
-    hipLaunchKernelGGL((even ? cross_bwd_dkv_kernel<2, true> : cross_bwd_dkv_kernel<2, false>), by_keys, dim3(NT), 0, s, p);
+  if (pass == CROSS_DQ) {
+    const int64_t blocks = ((int64_t)p.G * p.Sq + 127) / 128;
+    hipLaunchKernelGGL(cross_bwd_dq_kernel, dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
+  } else if (pass == CROSS_ALL) {
+    hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>,
+                       dim3((unsigned)(nbh * p.k_parts)), dim3(2 * NT), 0, s, p);
+  } else {
+    const int64_t blocks = ((int64_t)p.Sk + 255) / 256;
+    hipLaunchKernelGGL(even ? cross_bwd_dkv_kernel<true> : cross_bwd_dkv_kernel<false>,
+                       dim3((unsigned)(blocks * nbh * p.k_parts)), dim3(2 * NT), 0, s, p);
+  }
   return hipGetLastError();
 }
 

@@ -145,7 +145,7 @@ struct CrossBwdChoice {
   int q_parts, k_parts;
 };
 CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
-enum CrossBwdPass { CROSS_ALL, CROSS_DQ, CROSS_DV, CROSS_DK };
+enum CrossBwdPass { CROSS_ALL, CROSS_DQ, CROSS_DKV };
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s);
 // Sums of parts of up to two matrices [rows, cols] with as many columns: out
 // (bf16, leading dim ld) = sum over the parts, in order.

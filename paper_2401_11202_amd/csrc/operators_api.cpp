@@ -576,7 +576,7 @@ int partir_plan_cross_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int6
     if (p.c.one_pass)
       launches = B ? 1 + (p.c.k_parts > 1) : 0;
     else
-      launches = (B * Sq ? 1 + (p.c.q_parts > 1) : 0) + (B * Sk ? 2 + (p.c.k_parts > 1) : 0);
+      launches = (B * Sq ? 1 + (p.c.q_parts > 1) : 0) + (B * Sk ? 1 + (p.c.k_parts > 1) : 0);
     fill_info(info, std::max(p.c.q_parts, p.c.k_parts), launches, p.ws(),
               10.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
     return PARTIR_OK;
@@ -641,8 +641,7 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
         }
       }
       if (Tk == 0) return PARTIR_OK;
-      if (int st = launched(launch_cross_backward(p, CROSS_DV, s), "cross_bwd_dv")) return st;
-      if (int st = launched(launch_cross_backward(p, CROSS_DK, s), "cross_bwd_dk")) return st;
+      if (int st = launched(launch_cross_backward(p, CROSS_DKV, s), "cross_bwd_dkv")) return st;
     }
     if (p.k_parts == 1) return PARTIR_OK;
     PartSum r = part_sum(2, p.k_parts, Tk, ck);
