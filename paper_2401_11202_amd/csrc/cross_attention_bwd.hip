@@ -323,7 +323,6 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams
             s[v + 1] = __builtin_amdgcn_exp2f(s[v + 1] * c);
             put2(pf[v >> 3], v & 7, s[v], s[v + 1]);
           }
-          __builtin_amdgcn_sched_barrier(0);
           f32x16 dp;
           start(dp, 1);
 #pragma unroll
@@ -334,7 +333,6 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams
           for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
             for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * t + uu, d), pf[uu], dv[d]);
-          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[v] * dp[v], s[v + 1] * dp[v + 1]);
 #pragma unroll
