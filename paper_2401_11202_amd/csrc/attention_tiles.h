@@ -52,9 +52,11 @@ struct TileTr {
 // Streams `rows` rows of a [rows, 128] block of a bf16 matrix into an LDS tile
 // of ROWS rows, WAVES waves sharing the loads (wave w of them), 1 KiB or four
 // rows each.  The descriptor ends with the last of the rows: those behind it
-// are written as zeros, whatever the memory there holds.
+// are written as zeros, whatever the memory there holds.  Its offsets are 32-bit:
+// 128 rows are as many as reach there at any leading dim (2^24 values at most).
 template <int ROWS, int WAVES>
 __device__ __forceinline__ void tile_load(const uint16_t* base, int64_t ld, int rows, char* tile, int w, int lane) {
+  static_assert((int64_t)ROWS * 2 * (1 << 24) <= (int64_t)1 << 32, "a descriptor's offsets are 32-bit");
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows > 0 ? (uint32_t)((rows - 1) * ld * 2 + ROWB) : 0);
   const int l4 = lane >> 4, ch = lane & 15;
   const uint32_t ldb = (uint32_t)(ld * 2);

@@ -260,8 +260,12 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams
   }
   // workgroup-uniform: keys behind len_b get zeros
   if (k0 < len) {
-    const int64_t t0 = (int64_t)b * p.Sk + k0;
-    tile_load<256, 8>(p.V + t0 * p.ldv + kvh * DH, p.ldv, min(256, len - k0), smem + VT, w, lane);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {   // 256 rows of 2^24 values are more than a descriptor spans
+      const int64_t t0 = (int64_t)b * p.Sk + k0 + 128 * half;
+      tile_load<128, 8>(p.V + t0 * p.ldv + kvh * DH, p.ldv, min(128, len - k0 - 128 * half), smem + VT + 128 * half * ROWB, w,
+                        lane);
+    }
     bf16x8 kf[8];
     {
       const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, p.Sk - 1)) * p.ldk + kvh * DH + 8 * h;

@@ -237,6 +237,32 @@ def test_cache_of_more_than_four_gibibytes_a_sequence():
         check(name, x, r, t)
 
 
+@pytest.mark.parametrize("Sk", [100, 128, 256])
+def test_widest_leading_dims(Sk):
+    """Rows of 2^24 values: 128 of them span 32 bits of bytes, the values of the
+    results are those of dense arrays."""
+    Sq, H = 140, 2
+    Q, K, V, dO, *_ = make(1, Sq, Sk, H, 1, None, 9)
+    kw = dict(B=1, Sq=Sq, Sk=Sk, n_heads=H, n_kv_heads=1)
+    O, lse = P.cross_attention_train(Q, K, V, **kw)
+    ref = P.cross_attention_backward(Q, K, V, O, dO, lse, **kw)
+    wide = torch.empty((max(Sq, Sk), 2 ** 24), dtype=torch.bfloat16, device="cuda")
+    at = iter(range(8, 2 ** 24, 2 ** 21))
+
+    def view(rows, cols, x=None):
+        a = next(at)
+        v = wide[:rows, a:a + cols]
+        return v if x is None else v.copy_(x)
+    q, k, v, g = view(Sq, 256, Q), view(Sk, 128, K), view(Sk, 128, V), view(Sq, 256, dO)
+    o = view(Sq, 256)
+    P.cross_attention(q, k, v, out=o, **kw)
+    assert torch.equal(o, O)
+    out = (view(Sq, 256), view(Sk, 128), view(Sk, 128))
+    P.cross_attention_backward(q, k, v, o, g, lse, out=out, **kw)
+    for x, y in zip(out, ref):
+        assert torch.equal(x, y)
+
+
 def test_other_stream_and_replayed_graph():
     """A captured training step, replayed with new inputs and lengths, beside
     eager calls between the replays."""
