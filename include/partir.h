@@ -546,8 +546,9 @@ int partir_qk_norm_rotary(const void* Q, const void* K, const float* gq, const f
  *   dn = rotary^T(dy);  r = 1 / sqrt(mean(x^2) + eps);
  *   dx = r (g dn - x r^2 mean(x g dn));   dg = sum over tokens and heads of dn x r.
  * dQ, dK as Q, K (either may be its cotangent's array, pointer and leading dim
- * alike); dgq, dgk: [d_head] float32, either may be NULL: not stored.  The sums of dg are
- * taken in float32 in a fixed order.  With T = 0 or no heads dg is 0.
+ * alike); dgq, dgk: [d_head] float32, apart from each other, either may be
+ * NULL: not stored.  The sums of dg are taken in float32 in a fixed order.  With
+ * T = 0 or no heads dg is 0.
  * Workspace: the partial gain gradients. */
 int partir_qk_norm_rotary_backward(const void* Q, const void* K, const void* dQo, const void* dKo, const float* gq,
                                    const float* gk, void* dQ, void* dK, float* dgq, float* dgk, const double* freqs,
@@ -567,7 +568,8 @@ size_t partir_qk_norm_rotary_backward_workspace(int64_t T, int64_t n_heads, int6
  * k_lens: [B] int32 on the device, the valid keys of each sequence (clamped to
  * 0..Sk), or NULL: Sk.  Keys behind them are not read, whatever they hold.  A
  * query without keys gets 0.
- * scale <= 0 selects 1/sqrt(d_head).  d_head == 128.
+ * scale <= 0 selects 1/sqrt(d_head).  d_head == 128.  O may be Q (pointer and
+ * leading dim alike), else it is apart from the inputs.
  * With few queries the keys are evaluated in parts that are joined in order by
  * the combiner of partir_attention; the parts are the workspace (0 without).
  * Errors: E_NULL, E_SHAPE, E_DIVISIBILITY (n_kv_heads does not divide n_heads),
@@ -590,8 +592,9 @@ int partir_cross_attention_train(const void* Q, const void* K, const void* V, vo
  * forward's O and lse (formulas as partir_attention_backward).  dQ as Q; dK and
  * dV as K and V, summed over the query heads of a key head; keys behind
  * k_lens get zeros.  The gradients must be apart from each other and from the
- * inputs.  Every gradient is summed in a fixed order, without atomics.  Workspace: the rowsums of dO * O and, where the queries or keys are
- * few, fp32 parts of the gradients. */
+ * inputs.  Every gradient is summed in a fixed order, without atomics.
+ * Workspace: the rowsums of dO * O and, where the queries or keys are few, fp32
+ * parts of the gradients. */
 int partir_cross_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
                                     const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
                                     int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
@@ -614,9 +617,9 @@ int partir_grad_norm(const void* const* tensors, const int64_t* numel, const int
  * norm : 1), each value rounded once to its type.  out: HOST array of device
  * pointers; out[i] = tensors[i] scales in place (nothing is written where the
  * norm is within max_norm).  Where an element is infinite or NaN, so is the
- * norm, and nothing is scaled: the tensors are copied as they are.  Outputs must be apart from
- * each other, from norm and from other tensors' inputs (E_LAYOUT).  max_norm >= 0
- * (E_UNSUPPORTED otherwise). */
+ * norm, and nothing is scaled: the tensors are copied as they are.  Outputs must
+ * be apart from each other, from norm and from other tensors' inputs (E_LAYOUT).
+ * max_norm >= 0 (E_UNSUPPORTED otherwise). */
 int partir_clip_grad_norm(const void* const* tensors, void* const* out, const int64_t* numel, const int* dtypes, int n,
                           double max_norm, float* norm, void* ws, size_t ws_bytes, void* stream);
 size_t partir_grad_norm_workspace(int n);

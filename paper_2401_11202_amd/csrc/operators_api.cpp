@@ -300,9 +300,10 @@ int validate_cross(const CrossSizes& z) {
   const int64_t G = z.Hq / z.Hk;
   if (z.Sq * G > kMaxSize || z.B * z.Sq > kMaxSize || z.B * z.Sk > kMaxSize)
     return fail(PARTIR_E_SHAPE, "more than 2^30 query rows of a key head, queries or keys");
-  // workgroups of any launch (parts are asked for only below one a CU), and the threads of the join
-  if (z.B * z.Hk * std::max(cdiv(z.Sq * G, 32), cdiv(z.Sk, 128)) > ((int64_t)1 << 30) || z.B * z.Sq * z.Hq > ((int64_t)1 << 33))
-    return fail(PARTIR_E_SHAPE, "more than 2^30 workgroups");
+  // A launch is a grid of fewer than 2^32 threads: 256 for 128 query rows of a key
+  // head, 512 for 256 keys (parts are asked for only below one workgroup a CU).
+  if (z.B * z.Hk * std::max(cdiv(z.Sq * G, 128), 2 * cdiv(z.Sk, 256)) >= ((int64_t)1 << 24) || z.B * z.Sq * z.Hq > ((int64_t)1 << 33))
+    return fail(PARTIR_E_SHAPE, "more than 2^32 threads of a launch");
   return PARTIR_OK;
 }
 
@@ -348,6 +349,9 @@ int run_cross(const void* Q, const void* K, const void* V, void* O, float* lse, 
   if (int st = check_lens(lens)) return st;
   if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
   if (Tq == 0) return PARTIR_OK;
+  // a workgroup holds its rows of Q before it stores those of O, but others read K and V
+  if ((Tk > 0 && (O == K || O == V)) || (O == Q && Tq > 1 && ldo != ldq))
+    return fail(PARTIR_E_LAYOUT, "O must be Q, with its leading dim, or apart from the inputs");
   const CrossPlan plan = plan_cross(z);
   if (int st = check_ws(plan.ws(), ws, ws_bytes)) return st;
   CrossParams p{};
@@ -501,6 +505,7 @@ int partir_qk_norm_rotary_backward(const void* Q, const void* K, const void* dQo
     if (int st = check_eps(eps)) return st;
     if (int st = validate_rotary(p, dtype)) return st;
     if (!aligned(dgq, 4) || !aligned(dgk, 4)) return fail(PARTIR_E_LAYOUT, "gain gradients must be 4-byte aligned");
+    if (dgq && dgq == dgk) return fail(PARTIR_E_LAYOUT, "dgq must not be dgk");
     const bool empty = p.T == 0 || p.H[0] + p.H[1] == 0;
     if (!empty) {
       rotary_choice(p, dtype == PARTIR_BF16, ROTARY_NORM_BWD);

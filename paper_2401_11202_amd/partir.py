@@ -1029,7 +1029,7 @@ def cross_attention(Q, K, V, *, B: int, Sq: int, Sk: int, n_heads: int, n_kv_hea
     sequence, per head.  Q [B*Sq, n_heads * d_head], K, V [B*Sk, n_kv_heads *
     d_head] bf16 (views with a leading dim allowed), n_kv_heads dividing n_heads;
     k_lens [B] int32: the valid keys of each sequence (None: Sk); a query
-    without keys gets 0."""
+    without keys gets 0.  out: O to write into, Q itself allowed."""
     return _cross_forward(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens, scale, out, None, False, workspace,
                           stream)
 
@@ -1101,11 +1101,13 @@ def cross_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, n
 
 
 def plan_cross_attention(B, Sq, Sk, n_heads, n_kv_heads=None, d_head=128):
-    return _plan_sizes(lib().partir_plan_cross_attention, B, Sq, Sk, n_heads, n_kv_heads or n_heads, d_head)
+    return _plan_sizes(lib().partir_plan_cross_attention, B, Sq, Sk, n_heads,
+                       n_heads if n_kv_heads is None else n_kv_heads, d_head)
 
 
 def plan_cross_attention_backward(B, Sq, Sk, n_heads, n_kv_heads=None, d_head=128):
-    return _plan_sizes(lib().partir_plan_cross_attention_backward, B, Sq, Sk, n_heads, n_kv_heads or n_heads, d_head)
+    return _plan_sizes(lib().partir_plan_cross_attention_backward, B, Sq, Sk, n_heads,
+                       n_heads if n_kv_heads is None else n_kv_heads, d_head)
 
 
 def _plan_sizes(fn, *args):

@@ -211,6 +211,14 @@ def test_views_in_and_out_leave_their_surroundings():
         assert bool((f == 5.0).all())
 
 
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk", [(2, 37, 50, 4, 2), (1, 1, 5000, 4, 1), (2, 300, 500, 2, 2), (3, 2, 90, 2, 1)])
+def test_in_the_queries_place(B, Sq, Sk, Hq, Hk):
+    Q, K, V, *_ = make(B, Sq, Sk, Hq, Hk, None, 8)
+    kw = dict(B=B, Sq=Sq, Sk=Sk, n_heads=Hq, n_kv_heads=Hk)
+    want = P.cross_attention(Q, K, V, **kw)
+    assert P.cross_attention(Q, K, V, out=Q, **kw) is Q and torch.equal(Q, want)
+
+
 def test_cache_of_more_than_four_gibibytes_a_sequence():
     """2^32 values between the first and the last key: addresses past 32 bits
     in bytes and in elements, forward and gradients."""

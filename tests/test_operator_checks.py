@@ -75,7 +75,7 @@ def test_nothing_to_do_launches_nothing():
 
 NORM = dict(Q=T1, K=T2, gq=A, gk=A, Qo=T3, Ko=T4, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64, rd=64, ldq=256, ldk=128,
             ldqo=256, ldko=128, dt=P.BF16, inter=0, mag=1.0, eps=1e-6)
-BWD = dict(Q=T1, K=T2, dQo=T3, dKo=T4, gq=A, gk=A, dQ=T5, dK=T6, dgq=A, dgk=A, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64,
+BWD = dict(Q=T1, K=T2, dQo=T3, dKo=T4, gq=A, gk=A, dQ=T5, dK=T6, dgq=T7, dgk=T8, f=A, pos=NULL, p64=0, T=16, S=16, Hq=4, Hk=2, dh=64,
            rd=64, ldq=256, ldk=128, lddqo=256, lddko=128, lddq=256, lddk=128, dt=P.BF16, inter=0, mag=1.0, eps=1e-6, ws=A,
            wsb=1 << 24)
 
@@ -241,7 +241,7 @@ def test_clip_binding_checks():
 # ---------------------------------------------------------------------------
 # cross attention
 # ---------------------------------------------------------------------------
-CROSS = dict(Q=A, K=A, V=A, O=A, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256, ldv=256, ldo=512, lens=NULL, scale=0.0,
+CROSS = dict(Q=A, K=A, V=A, O=T1, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256, ldv=256, ldo=512, lens=NULL, scale=0.0,
              ws=NULL, wsb=0)
 CROSS_BWD = dict(Q=T1, K=T2, V=T3, O=T4, dO=T5, lse=A, dQ=T6, dK=T7, dV=T8, B=2, Sq=3, Sk=50, Hq=4, Hk=2, dh=128, ldq=512, ldk=256,
                  ldv=256, ldo=512, lddo=512, lddq=512, lddk=256, lddv=256, lens=NULL, scale=0.0, ws=A, wsb=1 << 30)
@@ -455,3 +455,34 @@ def test_division_by_a_product():
                                       np.clip(d * rng.integers(0, max(1, 2 ** 31 // d), 50) + rng.integers(-1, 2, 50), 0, 2 ** 31 - 1)])).astype(np.uint64)
         s = ((np.uint64(m) * n) >> np.uint64(32)) + n
         assert (s < 2 ** 32).all() and ((s >> np.uint64(l)) == n // np.uint64(d)).all(), d
+
+
+def test_the_output_of_attention_is_its_queries_or_apart():
+    assert cross(O=A, K=T2, V=T3) == "PARTIR_E_HIP"                            # in Q's place
+    assert cross(O=A, K=T2, V=T3, ldo=1024) == "PARTIR_E_LAYOUT"               # with other rows
+    assert cross(O=A, K=T2, V=T3, ldo=1024, B=1, Sq=1) == "PARTIR_E_HIP"       # a single row
+    assert cross(O=T2, K=T2) == "PARTIR_E_LAYOUT" and cross(O=T3, V=T3) == "PARTIR_E_LAYOUT"
+    assert cross(O=T2, K=T2, V=T2, Sk=0) == "PARTIR_E_HIP"                     # no key is read
+
+
+def test_a_launch_holds_fewer_than_2_32_threads():
+    one = dict(Sq=1, Sk=1, Hq=16, Hk=16, ldq=2048, ldk=2048, ldv=2048, ldo=2048, lddo=2048, lddq=2048, lddk=2048, lddv=2048,
+               ws=A, wsb=1 << 60)
+    f = lambda B: cross(B=B, **{k: v for k, v in one.items() if k in CROSS})  # noqa: E731
+    assert f(2 ** 19 - 1) == "PARTIR_E_HIP" and f(2 ** 19) == "PARTIR_E_SHAPE"
+    assert cross_bwd(B=2 ** 19 - 1, **one) == "PARTIR_E_HIP" and cross_bwd(B=2 ** 19, **one) == "PARTIR_E_SHAPE"
+    assert cross(**dict(CROSS, B=2 ** 20, Sq=1, Sk=0, Hq=16, Hk=16, ldq=2048, ldo=2048)) == "PARTIR_E_SHAPE"
+
+
+def test_plans_refuse_no_key_heads():
+    for plan in (P.plan_cross_attention, P.plan_cross_attention_backward):
+        assert status(lambda: plan(1, 1, 1, 4, 0)) == "PARTIR_E_SHAPE"
+        assert plan(1, 1, 1, 4) == plan(1, 1, 1, 4, 4)
+
+
+def test_gain_gradients_are_apart():
+    g = lambda dgq, dgk: name(P.lib().partir_qk_norm_rotary_backward(  # noqa: E731
+        T1, T2, T3, T4, NULL, NULL, T5, T6, dgq, dgk, A, NULL, 0, 8, 8, 2, 2, 64, 64, 128, 128, 128, 128, 128, 128, P.BF16, 0,
+        1.0, 1e-6, A, 1 << 24, None))
+    assert g(T7, T8) == g(T7, NULL) == g(NULL, NULL) == "PARTIR_E_HIP"
+    assert g(T7, T7) == "PARTIR_E_LAYOUT"
