@@ -137,7 +137,8 @@ struct CrossBwdParams {
   int64_t ldq, ldk, ldv, ldo, ldg, lddq, lddk, lddv;
   int B, Sq, Sk, Hq, Hk, G;
   int q_parts, k_parts;
-  Div by_g, by_hk, by_nbh, by_q_parts, by_k_parts;   // G, Hk, B Hk, the counts of parts
+  // G, Hk, B Hk, the 128-row blocks of a (sequence, key head), the counts of parts
+  Div by_g, by_hk, by_nbh, by_nqb, by_q_parts, by_k_parts;
   float scale, scale_log2;
 };
 struct CrossBwdChoice {

@@ -628,6 +628,7 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
     p.by_g = Div::by(p.G);
     p.by_hk = Div::by(p.Hk);
     p.by_nbh = Div::by((uint32_t)(B * n_kv_heads));
+    p.by_nqb = Div::by((uint32_t)std::max<int64_t>(cdiv((int64_t)p.G * Sq, 128), 1));
     p.by_q_parts = Div::by(p.q_parts);
     p.by_k_parts = Div::by(p.k_parts);
     p.scale = scale;
