@@ -29,8 +29,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # accumulator sets live at once; left to its heuristics the compiler parks
 # values in accumulation registers and copies them around every MFMA, so its
 # MFMAs are asked to use ordinary vector registers.
-# (the same for the cross attention kernels and for the small GEMM tiles, one workgroup per CU of which may use
-# the whole register file)
+# (the same for the cross attention kernels and for the small GEMM tiles, one
+# workgroup per CU of which may use the whole register file)
 EXTRA = {"attention_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
          "cross_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
          "cross_attention_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],

@@ -11,17 +11,23 @@
 //  * dq: workgroup = 128 of the G Sq query rows of a (sequence, key head), 4
 //    waves x 32, keys in tiles of 64; S^T = K Q^T and dP^T = V dO^T put one row
 //    on a lane, dQ^T += K^T dS^T.  It also writes D.
-//  * dv and dk: workgroup = 128 keys of a (sequence, key head), 4 waves x 32;
-//    its G Sq query rows in tiles of 64; S = Q K^T and dP = dO V^T put one key on
-//    a lane, dV^T += dO^T P, dK^T += Q^T dS.
-// Where the axis that is held is short (few queries in dq, few keys in dk and
-// dv) the streamed one is shared out over parts, whose float32 results an
-// ordered reduction adds.  P and dS are rounded to bf16 for their products
+//  * dkv: workgroup = 256 keys of a (sequence, key head), 8 waves x 32; its G Sq
+//    query rows in tiles of 64; S = Q K^T and dP = dO V^T put one key on a lane,
+//    dV^T += dO^T P, dK^T += Q^T dS.
+// Where the axis that is held is short (few queries in dq, few keys in dkv) the
+// streamed one is shared out over parts, whose float32 results an ordered
+// reduction adds.  P and dS are rounded to bf16 for their products
 // (within 2^-8 of their value), sums are float32.
 //
 // Rows and keys past their end are zero rows of the tiles; P is set to 0 for
-// keys behind len_b in dq, and the statistics of missing rows make P 0 in dk
-// and dv.  Keys behind len_b get zero gradients.
+// keys behind len_b in dq, and the statistics of missing rows make P 0 in dkv.
+// Keys behind len_b get zero gradients.
+//
+// What bounds them is the matrix units with exp2 and the conversions beside them.
+// 4 x 4096 queries over up to 2048 keys (80 % of them valid), 32 / 8 heads: dq 3
+// products, 0.66 TFLOP, 640 us; dkv 4 products, 0.88 TFLOP, 900 us.  The matrix
+// units are busy 56 and 49 % of the time; in dkv on three quarters of the compute
+// units only, as a workgroup behind its sequence's end has nothing to do.
 #include <algorithm>
 #include <type_traits>
 
@@ -44,7 +50,7 @@ __device__ __forceinline__ int key_count(const CrossBwdParams& p, int b) {
 // the rows, so a descriptor that ends with the tile's last row makes those
 // behind it zeros.  Where G divides 16, a lane's rows lie at one offset from a
 // tile's first position and a fixed step apart; else each is divided by G (8 %
-// of the dk and dv passes).
+// of dkv's time).
 template <bool EVEN, int WAVES = 4>
 struct RowTiles {
   const uint16_t *q, *g;
@@ -243,7 +249,11 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
 
 // dK and dV: eight waves of 32 keys, K as an operand in registers, V in LDS (both
 // as registers would leave one wave a SIMD); rows in tiles of 64.  Per 32 rows a
-// wave forms S and P, dV^T += dO^T P, then dP and dS, dK^T += Q^T dS.
+// wave forms S and P, dP, dV^T += dO^T P, then dS and dK^T += Q^T dS.  One pass for
+// both gradients forms S, P and dP once, 4 products where a pass for each takes
+// 5: 900 us for 1240 at the size above.  Two scheduling barriers keep phases
+// apart where the compiler would otherwise hold the operands of several at once
+// and spill; one at every phase costs their overlap (1130 us).
 template <bool EVEN>
 __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams p) {
   constexpr int STAGES = 0, VT = 2 * 2 * TILE, STAT = VT + 256 * ROWB;
@@ -572,10 +582,10 @@ constexpr int64_t kCUs = 256;
 
 CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk) {
   // A tile of 64 streamed rows takes a workgroup 2.8 us in the one pass, 1.45 us in
-  // the dq pass and 3 us in the dk and dv passes together; 1000 rows of a part cost
-  // 0.15 us.  One part / these: 2 x 4096 queries over 77 keys, 8 heads 187 / 30 us; 200
-  // queries over 2048 keys, 4 heads 77 / 41; 2048 queries over 200 keys, 4 heads 128 /
-  // 49; 500 over 500, 2 heads 53 / 36.
+  // dq and 3 us in dkv; 1000 rows of a part cost 0.15 us.  One part / these: 2 x 4096
+  // queries over 77 keys, 8 heads 187 / 30 us; 200 queries over 2048 keys, 4 heads
+  // 77 / 36; 2048 queries over 200 keys, 4 heads 128 / 45; 500 over 500, 2 heads 53 /
+  // 34.
   const int64_t R = Hq / Hk * Sq, rows = (R + 63) / 64, keys = (Sk + 63) / 64;
   auto most = [](int64_t grid, int64_t tiles) { return grid > 0 ? std::min(kCUs / grid, tiles) : 1; };
   const double q_us = 1.5e-4 * (double)(B * Sq * Hq), k_us = 2 * 1.5e-4 * (double)(B * Sk * Hk);

@@ -124,13 +124,13 @@ __device__ __forceinline__ CrossRange cross_range(int len, const Div& by_split, 
 }
 
 // Gradients (cross_attention_bwd.hip).  Up to 128 keys a sequence: one pass.
-// Above: a dq pass, which takes the key axis in q_parts parts, and dk and dv
-// passes.  The passes that yield dk and dv take the query rows in k_parts;
-// more than one part means fp32 partials for an ordered reduction.
+// Above: a dq pass, which takes the key axis in q_parts parts, and one for dk and
+// dv.  A pass that yields dk and dv takes the query rows in k_parts; more than
+// one part means fp32 partials for an ordered reduction.
 struct CrossBwdParams {
   const uint16_t *Q, *K, *V, *O, *dO;
   const float* lse;
-  float* Dstat;            // [B Sq][Hq] rowsums of dO * O, from the dq pass for the dk pass
+  float* Dstat;            // [B Sq][Hq] rowsums of dO * O, from the dq pass for the other
   uint16_t *dQ, *dK, *dV;
   float *dQpart, *dKpart, *dVpart;   // [parts][rows][heads * 128]
   const int32_t* lens;
