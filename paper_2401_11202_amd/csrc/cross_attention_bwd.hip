@@ -194,9 +194,11 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
     tile_load<TR, 4>(kbase + (int64_t)kb * TR * p.ldk, p.ldk, rows, t, w, lane);
     tile_load<TR, 4>(vbase + (int64_t)kb * TR * p.ldv, p.ldv, rows, t + TILE, w, lane);
   };
-  f32x16 dq[4];
+  f32x16 dq[4], nD;   // dP starts at -D: its first product reads it, where a subtraction would follow
 #pragma unroll
   for (int d = 0; d < 4; ++d) zero(dq[d]);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) nD[v] = -Dq;
   auto iter = [&](int kb, auto stage) {
     constexpr int cur = decltype(stage)::value;
     if (kb + 1 < nkb) gload(kb + 1, cur ^ 1);
@@ -205,9 +207,8 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
     const int left = nkeys - kb * TR;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x16 s, dp;
+      f32x16 s, dp = nD;
       zero(s);
-      zero(dp);
 #pragma unroll
       for (int ds = 0; ds < 8; ++ds) {
         s = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], s);
@@ -224,7 +225,7 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
       bf16x8 dsf[2];
 #pragma unroll
       for (int v = 0; v < 16; v += 2)
-        put2(dsf[v >> 3], v & 7, pr[v] * (dp[v] - Dq), pr[v + 1] * (dp[v + 1] - Dq));
+        put2(dsf[v >> 3], v & 7, pr[v] * dp[v], pr[v + 1] * dp[v + 1]);
 #pragma unroll
       for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
