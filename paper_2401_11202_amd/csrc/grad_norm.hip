@@ -127,7 +127,8 @@ __device__ __forceinline__ void chunk_scale(const T* x, T* y, int n, double f) {
   }
 }
 
-// Calls f(tensor, first element, elements) for this workgroup's chunks.
+// Calls f(tensor, whether it is bf16, first element, elements) for this
+// workgroup's chunks.
 template <typename F>
 __device__ __forceinline__ void for_chunks(const GradTable& t, F f) {
   const int64_t all = t.chunk0[t.n];
@@ -140,11 +141,12 @@ __device__ __forceinline__ void for_chunks(const GradTable& t, F f) {
   }
   int64_t c = c0;
   while (c < c1) {
-    const int64_t n = t.numel[lo], last = t.chunk0[lo + 1], first = t.chunk0[lo];
-    const int64_t step = kGradChunkBytes / (t.bf16[lo] ? 2 : 4);
+    const bool bf16 = (t.size[lo] & kGradBf16) != 0;
+    const int64_t n = (int64_t)(t.size[lo] & ~kGradBf16), last = t.chunk0[lo + 1], first = t.chunk0[lo];
+    const int64_t step = kGradChunkBytes / (bf16 ? 2 : 4);
     for (; c < c1 && c < last; ++c) {
       const int64_t at = (c - first) * step;
-      f(lo, at, (int)(n - at < step ? n - at : step));
+      f(lo, bf16, at, (int)(n - at < step ? n - at : step));
     }
     ++lo;
   }
@@ -153,9 +155,9 @@ __device__ __forceinline__ void for_chunks(const GradTable& t, F f) {
 __global__ __launch_bounds__(NT) void grad_sumsq_kernel(GradTable t, double* partial) {
   __shared__ double red[NT / 64];
   double s = 0.0;
-  for_chunks(t, [&](int i, int64_t at, int n) {
-    s += t.bf16[i] ? chunk_sumsq<__bf16, bf16x8>((const __bf16*)t.in[i] + at, n)
-                   : chunk_sumsq<float, f32x4>((const float*)t.in[i] + at, n);
+  for_chunks(t, [&](int i, bool bf16, int64_t at, int n) {
+    s += bf16 ? chunk_sumsq<__bf16, bf16x8>((const __bf16*)t.in[i] + at, n)
+              : chunk_sumsq<float, f32x4>((const float*)t.in[i] + at, n);
   });
   s = block_sum(s, red);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -182,9 +184,9 @@ __global__ __launch_bounds__(NT) void grad_scale_kernel(GradTable t, const doubl
   // NaN only where one of them is, and then scales nothing.
   const bool clip = v > max_norm && v <= 1.0e300;
   const double f = clip ? max_norm / v : 1.0;
-  for_chunks(t, [&](int i, int64_t at, int m) {
+  for_chunks(t, [&](int i, bool bf16, int64_t at, int m) {
     if (!clip && t.in[i] == t.out[i]) return;
-    if (t.bf16[i])
+    if (bf16)
       chunk_scale<__bf16, bf16x8>((const __bf16*)t.in[i] + at, (__bf16*)t.out[i] + at, m, f);
     else
       chunk_scale<float, f32x4>((const float*)t.in[i] + at, (float*)t.out[i] + at, m, f);

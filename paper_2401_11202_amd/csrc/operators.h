@@ -161,17 +161,18 @@ struct PartSum {
 hipError_t launch_part_sum(const PartSum& p, hipStream_t s);
 
 // ---- global norm of many tensors (grad_norm.hip) ----------------------------
-constexpr int kGradTensors = 112;             // tensors of one launch's table
+constexpr int kGradTensors = 144;             // tensors of one launch's table, which fills 4 KiB of arguments
 constexpr int kGradChunkBytes = 32768;        // bytes of one step of a workgroup
 constexpr int kGradMaxWorkgroups = 2048;
 struct GradTable {
   const void* in[kGradTensors];
   void* out[kGradTensors];
-  int64_t numel[kGradTensors];
-  int64_t chunk0[kGradTensors + 1];           // first chunk of each tensor; [n] = all
-  uint8_t bf16[kGradTensors];
+  uint64_t size[kGradTensors];                // elements, kGradBf16 added for bf16 (else float32)
+  uint32_t chunk0[kGradTensors + 1];          // first chunk of each tensor; [n] = all (at most 2^31)
   int n;
 };
+constexpr uint64_t kGradBf16 = (uint64_t)1 << 63;
+static_assert(sizeof(GradTable) + 32 <= 4096, "with the other arguments of a launch");
 // partial[w] = sum of squares of workgroup w's chunks
 hipError_t launch_grad_sumsq(const GradTable& t, double* partial, int workgroups, hipStream_t s);
 // norm = sqrt(sum of partial[0..n))

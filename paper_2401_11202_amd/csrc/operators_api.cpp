@@ -238,9 +238,9 @@ void grad_launches(const void* const* in, void* const* out, const int64_t* numel
       if (numel[i] == 0) continue;
       t.in[t.n] = in[i];
       t.out[t.n] = out ? out[i] : nullptr;
-      t.numel[t.n] = numel[i];
-      t.bf16[t.n] = dtypes[i] == PARTIR_BF16;
-      t.chunk0[t.n + 1] = t.chunk0[t.n] + cdiv(numel[i], kGradChunkBytes / (t.bf16[t.n] ? 2 : 4));
+      const bool bf16 = dtypes[i] == PARTIR_BF16;
+      t.size[t.n] = (uint64_t)numel[i] + (bf16 ? kGradBf16 : 0);
+      t.chunk0[t.n + 1] = t.chunk0[t.n] + (uint32_t)cdiv(numel[i], kGradChunkBytes / (bf16 ? 2 : 4));
       ++t.n;
     }
     if (t.n == 0) {

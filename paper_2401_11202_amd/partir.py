@@ -1118,48 +1118,48 @@ def _plan_sizes(fn, *args):
 
 
 def _grad_arrays(tensors, name):
-    """Host arrays (addresses, counts, dtypes) of a list of dense tensors, and
-    the set of their GPUs' indexes (-1: the CPU).  Read by maps over the whole list,
-    which cost a third of a loop over hundreds of tensors."""
+    """Addresses (a host array), counts and dtypes (lists) of a list of dense
+    tensors, and the set of their GPUs' indexes (-1: the CPU).  Read by maps over
+    the whole list, which cost a third of a loop over hundreds of tensors."""
     torch = _th()
     T = torch.Tensor
     try:
         dtypes = list(map(T.dtype.__get__, tensors))
         dense = all(map(T.is_contiguous, tensors))
         devs = set(map(T.get_device, tensors))
-        ptrs, numel = array("Q", list(map(T.data_ptr, tensors))), array("q", list(map(T.numel, tensors)))
+        ptrs, numel = array("Q", list(map(T.data_ptr, tensors))), list(map(T.numel, tensors))
     except TypeError:
         i = next(i for i, t in enumerate(tensors) if not isinstance(t, T))
         _bad("PARTIR_E_NULL", f"{name}[{i}] must be a tensor")
-    codes = {torch.float32: F32, torch.bfloat16: BF16}
-    try:
-        dts = array("i", [codes[d] for d in dtypes])
-    except KeyError:
-        i = next(i for i, d in enumerate(dtypes) if d not in codes)
-        _bad("PARTIR_E_DTYPE", f"{name}[{i}] has dtype {dtypes[i]}, expected float32 or bfloat16")
     if not dense:
         i = next(i for i, t in enumerate(tensors) if not t.is_contiguous())
         _bad("PARTIR_E_LAYOUT", f"{name}[{i}] must be dense (contiguous)")
-    return ptrs, numel, dts, devs
+    return ptrs, numel, dtypes, devs
 
 
 def _grad_call(fn, tensors, norm, workspace, stream, outs=None, max_norm=None):
     torch = _th()
     tensors = list(tensors)
-    ptrs, numel, dts, devs = _grad_arrays(tensors, "tensors")
+    ptrs, numel, dtypes, devs = _grad_arrays(tensors, "tensors")
+    codes = {torch.float32: F32, torch.bfloat16: BF16}
+    try:
+        dts = array("i", list(map(codes.__getitem__, dtypes)))
+    except KeyError:
+        i = next(i for i, d in enumerate(dtypes) if d not in codes)
+        _bad("PARTIR_E_DTYPE", f"tensors[{i}] has dtype {dtypes[i]}, expected float32 or bfloat16")
     optrs = ptrs
     if outs is not None:
         outs = list(outs)
         if len(outs) != len(tensors):
             _bad("PARTIR_E_SHAPE", f"out must hold {len(tensors)} tensors")
-        optrs, onumel, odts, odevs = _grad_arrays(outs, "out")
+        optrs, onumel, odtypes, odevs = _grad_arrays(outs, "out")
         devs |= odevs
         if onumel != numel:
             i = next(i for i in range(len(outs)) if onumel[i] != numel[i])
             _bad("PARTIR_E_SHAPE", f"out[{i}] has {onumel[i]} elements, expected {numel[i]}")
-        if odts != dts:
-            i = next(i for i in range(len(outs)) if odts[i] != dts[i])
-            _bad("PARTIR_E_DTYPE", f"out[{i}] has dtype {outs[i].dtype}, expected {tensors[i].dtype}")
+        if odtypes != dtypes:
+            i = next(i for i in range(len(outs)) if odtypes[i] != dtypes[i])
+            _bad("PARTIR_E_DTYPE", f"out[{i}] has dtype {odtypes[i]}, expected {dtypes[i]}")
     if norm is not None:
         devs.add(_req(norm, "norm", (), torch.float32).get_device())
     if len(devs) > 1 or -1 in devs:
@@ -1171,6 +1171,7 @@ def _grad_call(fn, tensors, norm, workspace, stream, outs=None, max_norm=None):
     n = len(tensors)
     ws, wsb = _workspace(dev, workspace, lib().partir_grad_norm_workspace, n)
     _on_stream(stream, ws if workspace is None else None, norm if fresh else None)
+    numel = array("q", numel)
     host = [a.buffer_info()[0] for a in (ptrs, optrs, numel, dts)]     # the arrays outlive the call
     if max_norm is None:
         _launch(dev, fn, host[0], host[2], host[3], n, _ptr(norm), _ptr(ws), wsb, stream=stream)
