@@ -22,7 +22,7 @@
 // What bounds it.  Many rows: the matrix units, beside which exp2 and the
 // conversions of a score take about as long (16 of the first, 4 cycles a value
 // elsewhere); three waves a SIMD in different phases hide one behind the other.
-// 4 x 4096 queries over up to 2048 keys, 32 / 8 heads (0.44 TFLOP): 425 us, 1.03
+// 4 x 4096 queries over up to 2048 keys, 32 / 8 heads (0.44 TFLOP): 430 us, 1.02
 // PFLOP/s, the matrix units busy 57 % of the time.  With 64-key blocks and two
 // stages (two waves a SIMD) 452, with two key groups 456.  Few rows: the reading
 // of K and V; 131072 keys of 8 key heads (537 MB): 93 us, 5.8 TB/s, and 5 for the

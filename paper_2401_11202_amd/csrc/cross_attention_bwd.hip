@@ -25,8 +25,8 @@
 //
 // What bounds them is the matrix units with exp2 and the conversions beside them.
 // 4 x 4096 queries over up to 2048 keys (80 % of them valid), 32 / 8 heads: dq 3
-// products, 0.66 TFLOP, 640 us; dkv 4 products, 0.88 TFLOP, 900 us.  The matrix
-// units are busy 56 and 49 % of the time; in dkv on three quarters of the compute
+// products, 0.66 TFLOP, 610 us; dkv 4 products, 0.88 TFLOP, 830 us.  The matrix
+// units are busy 58 and 49 % of the time; in dkv on three quarters of the compute
 // units only, as a workgroup behind its sequence's end has nothing to do.
 #include <algorithm>
 #include <type_traits>
@@ -114,8 +114,8 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
   int qb, bh, part = 0;
   if (p.q_parts == 1 && (p.by_nbh.d & 7) == 0) {
     // as in the forward pass an XCD takes one (sequence, key head) after the other,
-    // whose K and V stay in its L2 (four at a time in its 4 MiB: 818 MB read of
-    // memory and 700 us at 4 x 4096 queries over 2048 keys, 32 / 8 heads; 640 us so)
+    // whose K and V stay in its L2 (four at a time in its 4 MiB: 818 MB read and
+    // 700 us at 4 x 4096 queries over 2048 keys, 32 / 8 heads; 535 MB and 640 us so)
     const int j = blockIdx.x >> 3, n = p.by_nqb.quot(j);
     bh = n * 8 + (blockIdx.x & 7);
     qb = p.by_nqb.rem(j, n);
@@ -252,9 +252,9 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
 // as registers would leave one wave a SIMD); rows in tiles of 64.  Per 32 rows a
 // wave forms S and P, dP, dV^T += dO^T P, then dS and dK^T += Q^T dS.  One pass for
 // both gradients forms S, P and dP once, 4 products where a pass for each takes
-// 5: 900 us for 1240 at the size above.  Two scheduling barriers keep phases
+// 5, and three quarters of their time at the size above.  Two scheduling barriers keep phases
 // apart where the compiler would otherwise hold the operands of several at once
-// and spill; one at every phase costs their overlap (1130 us).
+// and spill; one at every phase costs their overlap (24 % more).
 template <bool EVEN>
 __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams p) {
   constexpr int STAGES = 0, VT = 2 * 2 * TILE, STAT = VT + 256 * ROWB;
