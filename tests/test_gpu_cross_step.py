@@ -117,3 +117,42 @@ def test_single_tokens_continue_a_prompt():
         for b in range(B):
             top = np.repeat(np.abs(big[b, :LENS[b]]).max(0), Hq // Hk, 0).reshape(-1)
             assert (np.abs(got[b] - host(whole[at])[b]) <= 4 * 2.0 ** -8 * top).all()
+
+
+def test_two_streams_at_once():
+    """Two chains of every operator, one replayed from a graph and one issued on
+    another stream meanwhile, give what each gives alone."""
+    f = P.rotary_frequencies(DH)
+    gain = I.gaussian(322, 9, (DH,), 1.0, "f32").to_device()
+    lens = torch.tensor(LENS, dtype=torch.int32, device="cuda")
+    sets = [[I.gaussian(322, 4 * n + i, (r, c)).to_device() for i, (r, c) in
+             enumerate(((B * Sq, Hq * DH), (B * Sk, 2 * Hk * DH), (B * Sq, Hq * DH)))] for n in range(2)]
+
+    def chain(Q, KV, dO):
+        q, _ = P.qk_norm_rotary(Q, None, gain, None, f, d_head=DH, S=Sq)
+        k, _ = P.rotary(KV[:, :Hk * DH], None, f, d_head=DH, S=Sk)
+        kw = dict(B=B, Sq=Sq, Sk=Sk, n_heads=Hq, n_kv_heads=Hk, k_lens=lens)
+        o, lse = P.cross_attention_train(q, k, KV[:, Hk * DH:], **kw)
+        dq, dk, dv = P.cross_attention_backward(q, k, KV[:, Hk * DH:], o, dO, lse, **kw)
+        dx, _, dg, _ = P.qk_norm_rotary_backward(Q, None, dq, None, gain, None, f, d_head=DH, S=Sq)
+        clipped = [torch.empty_like(t) for t in (dx, dk, dv, dg)]
+        return [o, lse, P.clip_grad_norm([dx, dk, dv, dg], 0.5, out=clipped), *clipped]
+    want = [chain(*s) for s in sets]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        captured = chain(*sets[0])
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in (side, other):
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        for t in captured:
+            t.fill_(7.0)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            g.replay()
+        with torch.cuda.stream(other):
+            eager = [chain(*sets[1]) for _ in range(3)]
+        torch.cuda.synchronize()
+        for got, ref in [(captured, want[0])] + [(e, want[1]) for e in eager]:
+            for x, y in zip(got, ref):
+                assert torch.equal(x, y)
