@@ -490,10 +490,10 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdP
     // element v: key 32 kg + 8 (v / 4) + 4 h + v % 4
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse));
-    if (len < 32 * kg + 32) {
+    if (len < 32 * kg + 32) {   // dP too: 0 times a row of dO that is not finite would reach D
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        if (32 * kg + 8 * (v >> 2) + 4 * h + (v & 3) >= len) s[v] = 0.0f;
+        if (32 * kg + 8 * (v >> 2) + 4 * h + (v & 3) >= len) s[v] = dp[v] = 0.0f;
     }
     float d = 0.0f;
 #pragma unroll
@@ -549,8 +549,16 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdP
     if (it + 1 < it1) iter(it + 1, std::integral_constant<int, 1>{});
   }
   __syncthreads();
-  // 32 keys x 64 columns of dK and dV; keys behind len met P = 0 only
+  // 32 keys x 64 columns of dK and dV.  Keys behind len met P = 0 only, but times
+  // rows of Q and dO that need not be finite.
   const int kj = 32 * kg + col, rows = p.Sk - 32 * kg;
+  if (kj >= len) {
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      zero(dk[d]);
+      zero(dv[d]);
+    }
+  }
   const int64_t tk = tk0 + kj;
   char* const area = smem + w * row_area<2, float>();
   if (p.k_parts > 1) {
