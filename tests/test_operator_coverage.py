@@ -6,6 +6,7 @@ import pytest
 from oracle import operators_oracle as OO
 from paper_2401_11202_amd import partir as P
 from tests import test_gpu_cross_loops as L
+from tests import test_gpu_operator_runs as R
 from tests.gpu_common import TOL_REL_FRO, rel_fro
 
 DH, CUS = 128, 256
@@ -40,6 +41,14 @@ def test_the_gradient_tests_stream_many_tiles():
             assert -(-Hq // Hk * Sq // 64) >= 6
         assert {16 % (Hq // Hk) == 0 for _, _, _, Hq, Hk, _ in shapes} == {True, False}   # rows by steps, and divided
     assert any(P.plan_cross_attention_backward(*s[:5])["n_virtual_shards"] > 1 for s in L.LONG_KEYS)
+
+
+def test_the_run_tests_take_more_than_one_block_or_chunk():
+    for cases, grid in ((R.ROTARY, 8192), (R.NORM, 2048), (R.GRADIENTS, 1024)):
+        for T, *_ in cases:
+            assert -(-T // 16) > grid
+    for sizes, kinds in R.CHUNKS:
+        assert len(sizes) <= 144 and sum(-(-n * k.itemsize // 32768) for n, k in zip(sizes, kinds)) > 2 * 2048
 
 
 @pytest.mark.parametrize("Sq,Sk,Hq,Hk", [(100, 4100, 2, 1), (1, 4096, 16, 16), (200, 300, 2, 1), (64, 257, 1, 1)])
