@@ -10,7 +10,8 @@
 // in float64: float32 overflows from 2e19 on and loses the small tensors of a
 // sum of 1e9 terms; conversions and adds of float64 are well within what the
 // load rate leaves.  The partial sums are added in a fixed order by every
-// workgroup of the second pass for itself, which saves a launch between.
+// workgroup of the second pass for itself, which saves a launch between; more
+// than kGradDirect of them are added to kGradFolded by a launch first.
 //
 // What bounds it is HBM: one read for the norm, one read and one write for the
 // scaling, which is left out where nothing would change (in place, N <=
@@ -163,10 +164,22 @@ __global__ __launch_bounds__(NT) void grad_sumsq_kernel(GradTable t, double* par
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-__device__ __forceinline__ double norm_of(const double* partial, int n, double* red) {
+// the sum of partial[i0 .. i1), in every thread
+__device__ __forceinline__ double sum_of(const double* partial, int i0, int i1, double* red) {
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += NT) s += partial[i];
-  return sqrt(block_sum(s, red));
+  for (int i = i0 + (int)threadIdx.x; i < i1; i += NT) s += partial[i];
+  return block_sum(s, red);
+}
+
+__device__ __forceinline__ double norm_of(const double* partial, int n, double* red) {
+  return sqrt(sum_of(partial, 0, n, red));
+}
+
+__global__ __launch_bounds__(NT) void grad_fold_kernel(const double* partial, int n, double* folded) {
+  __shared__ double red[NT / 64];
+  const int i0 = (int)((int64_t)n * blockIdx.x / gridDim.x), i1 = (int)((int64_t)n * (blockIdx.x + 1) / gridDim.x);
+  const double s = sum_of(partial, i0, i1, red);
+  if (threadIdx.x == 0) folded[blockIdx.x] = s;
 }
 
 __global__ __launch_bounds__(NT) void grad_norm_kernel(const double* partial, int n, float* norm) {
@@ -197,6 +210,11 @@ __global__ __launch_bounds__(NT) void grad_scale_kernel(GradTable t, const doubl
 
 hipError_t launch_grad_sumsq(const GradTable& t, double* partial, int workgroups, hipStream_t s) {
   hipLaunchKernelGGL(grad_sumsq_kernel, dim3((unsigned)workgroups), dim3(NT), 0, s, t, partial);
+  return hipGetLastError();
+}
+
+hipError_t launch_grad_fold(const double* partial, int n, double* folded, hipStream_t s) {
+  hipLaunchKernelGGL(grad_fold_kernel, dim3(kGradFolded), dim3(NT), 0, s, partial, n, folded);
   return hipGetLastError();
 }
 

@@ -164,6 +164,8 @@ hipError_t launch_part_sum(const PartSum& p, hipStream_t s);
 constexpr int kGradTensors = 144;             // tensors of one launch's table, which fills 4 KiB of arguments
 constexpr int kGradChunkBytes = 32768;        // bytes of one step of a workgroup
 constexpr int kGradMaxWorkgroups = 2048;
+constexpr int kGradDirect = 2048;             // partial sums that a launch adds as they are
+constexpr int kGradFolded = 256;              // more of them are added to these first
 struct GradTable {
   const void* in[kGradTensors];
   void* out[kGradTensors];
@@ -175,6 +177,8 @@ constexpr uint64_t kGradBf16 = (uint64_t)1 << 63;
 static_assert(sizeof(GradTable) + 32 <= 4096, "with the other arguments of a launch");
 // partial[w] = sum of squares of workgroup w's chunks
 hipError_t launch_grad_sumsq(const GradTable& t, double* partial, int workgroups, hipStream_t s);
+// folded[w] = the sum of run w of kGradFolded even runs of partial[0..n)
+hipError_t launch_grad_fold(const double* partial, int n, double* folded, hipStream_t s);
 // norm = sqrt(sum of partial[0..n))
 hipError_t launch_grad_norm(const double* partial, int n, float* norm, hipStream_t s);
 // out = in * (norm > max_norm ? max_norm / norm : 1) with the norm of the
