@@ -272,16 +272,26 @@ def _gpu_all(**named):
 
 
 def _on_stream(stream, *tensors):
-    """Kernels run on `stream`: tensors allocated here on the current stream
-    are marked as used there, so the caching allocator does not hand their
-    memory out again before those kernels finish."""
+    """Kernels run on `stream` (a Stream or a raw handle): tensors allocated
+    here come from the current stream's memory, which kernels issued there may
+    still read or write, so `stream` waits for those; and the tensors are marked
+    as used there, so the caching allocator does not hand their memory out again
+    before the call's kernels finish."""
     if stream is None:
         return
+    tensors = [t for t in tensors if t is not None and t.numel() > 0]
+    if not tensors:
+        return
     torch = _th()
-    if isinstance(stream, torch.cuda.Stream) and stream != torch.cuda.current_stream(stream.device):
-        for t in tensors:
-            if t is not None and t.numel() > 0:
-                t.record_stream(stream)
+    dev = tensors[0].device
+    here = torch.cuda.current_stream(dev)
+    if _stream(stream) == here.cuda_stream:
+        return
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=dev) if stream else torch.cuda.default_stream(dev)
+    stream.wait_stream(here)
+    for t in tensors:
+        t.record_stream(stream)
 
 
 def _workspace(device, ws, query, *sizes):
