@@ -490,10 +490,10 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdP
     // element v: key 32 kg + 8 (v / 4) + 4 h + v % 4
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse));
-    if (len < 32 * kg + 32) {   // dP too: 0 times a row of dO that is not finite would reach D
+    if (len < 32 * kg + 32) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        if (32 * kg + 8 * (v >> 2) + 4 * h + (v & 3) >= len) s[v] = dp[v] = 0.0f;
+        if (32 * kg + 8 * (v >> 2) + 4 * h + (v & 3) >= len) s[v] = 0.0f;
     }
     float d = 0.0f;
 #pragma unroll
@@ -538,6 +538,7 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdP
       dq = mfma(tr.read(smem + KT, u, kg),
                 __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), dq);
     }
+    if (len == 0) zero(dq);   // a row of dO that is not finite, times weights of 0
     const int rc = min(row, R - 1), sq = p.by_g.quot(rc);
     store_rows<1>(smem + ROWS + w * row_area<1, __bf16>(), (__bf16*)p.dQ,
                   ((int64_t)b * p.Sq + sq) * p.lddq + (kvh * p.G + p.by_g.rem(rc, sq)) * DH + 32 * kg, R - it * TR - 32 * half,
