@@ -291,7 +291,7 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams
     }
     bf16x8 kf[8];
     {
-      const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, p.Sk - 1)) * p.ldk + kvh * DH + 8 * h;
+      const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, len - 1)) * p.ldk + kvh * DH + 8 * h;
 #pragma unroll
       for (int ds = 0; ds < 8; ++ds) kf[ds] = *(const bf16x8*)(krow + 16 * ds);
     }
