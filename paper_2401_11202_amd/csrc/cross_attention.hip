@@ -11,7 +11,10 @@
 // registers, and exp2(S^T - m), rounded to bf16 (within 2^-8 of its value, as
 // the weights of partir_attention), is the B operand of
 //     O^T[128 x 32 rows] += V_blk^T P^T
-// with V^T from transposed LDS reads.  Sums and O are float32; groups and key
+// with V^T from transposed LDS reads.  Where rows are few the matrix units wait
+// for K and V, and what that rounding leaves is a second operand (within 2^-16
+// then), so that O's error is its own rounding: 1.66e-3 of its size, 2.34e-3 with
+// one (64 x 8192 keys, 363 us either way; the smallest calls take 0.3 to 0.7 us more).  Sums and O are float32; groups and key
 // parts join by (m, l, O) (+) (m', l', O'), in a fixed order.
 //
 // Keys at and behind len_b are never read: their tile rows are zeros (the
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
           if (32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= left) sacc[t][v] = -__builtin_inff();
     }
     float lsum = 0.0f;
-    bf16x8 pf[2 * NSUB];
+    bf16x8 pf[2 * NSUB], pl[2 * NSUB];   // the weights in bf16, and what is left of them (few rows)
     auto weights = [&]() {
       lsum = 0.0f;
 #pragma unroll
@@ -179,7 +182,9 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
         for (int v = 0; v < 16; ++v) {
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][v], sl2, -m_run));
           lsum += e;
-          pf[2 * t + (v >> 3)][v & 7] = (__bf16)e;
+          const __bf16 hi = (__bf16)e;
+          pf[2 * t + (v >> 3)][v & 7] = hi;
+          if constexpr (ALONE) pl[2 * t + (v >> 3)][v & 7] = (__bf16)(e - (float)hi);
         }
     };
     // m moves only where the block's maximum is more than 8 (log2 units)
@@ -217,7 +222,11 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
 #pragma unroll
     for (int u = 0; u < BKV / 16; ++u)
 #pragma unroll
-      for (int d = 0; d < 4; ++d) oacc[d] = mfma(tr.read(vs, u, d), pf[u], oacc[d]);
+      for (int d = 0; d < 4; ++d) {
+        const bf16x8 v = tr.read(vs, u, d);
+        oacc[d] = mfma(v, pf[u], oacc[d]);
+        if constexpr (ALONE) oacc[d] = mfma(v, pl[u], oacc[d]);
+      }
     if constexpr (ALONE) {
       __builtin_amdgcn_sched_barrier(0);
       WAIT_LGKMCNT(0);
