@@ -522,7 +522,9 @@ int partir_rotary_frequencies(int64_t rotary_dim, double base, int scaling, doub
  * interleaved: pairs are (x[2i], x[2i+1]), else (x[i], x[i + rotary_dim / 2]).
  * freqs: [rotary_dim / 2] float64 on the device.  positions: [T] int32, or
  * int64 with positions64 != 0; NULL: row t stands at t mod S (S >= 1).
- * Positions may be of any size: angles are formed in float64.
+ * Angles are formed in float64: one of a radians is off by up to a 2^-51
+ * radians, which is float32's precision up to 2^27 radians (position times
+ * freqs[i]) and bf16's up to 2^42.
  * d_head: a multiple of 8 up to 256; rotary_dim even, 0..d_head.
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_LAYOUT, E_UNSUPPORTED, E_HIP. */
 int partir_rotary(const void* Q, const void* K, void* Qo, void* Ko, const double* freqs, const void* positions,
@@ -533,6 +535,9 @@ int partir_rotary(const void* Q, const void* K, void* Qo, void* Ko, const double
 /* RMS norm of every head of Q and K over its d_head values with a gain shared
  * by the heads, then the rotation of partir_rotary, in one pass:
  *   n = g * x / sqrt(mean(x^2) + eps),  y = rotary(n).
+ * The mean is taken in float32: a head whose squares pass its range (values from
+ * about 1e18 on) gives 0, and with eps = 0 one of zeros, or of values below
+ * 1e-19, gives NaN or infinities.
  * gq, gk: [d_head] float32, or NULL for gains of 1.  rotary_dim = 0 is the
  * norms alone (freqs may be NULL).  Otherwise as partir_rotary. */
 int partir_qk_norm_rotary(const void* Q, const void* K, const float* gq, const float* gk, void* Qo, void* Ko,
@@ -570,8 +575,9 @@ size_t partir_qk_norm_rotary_backward_workspace(int64_t T, int64_t n_heads, int6
  * query without keys gets 0.
  * scale <= 0 selects 1/sqrt(d_head).  d_head == 128.  O may be Q (pointer and
  * leading dim alike), else it is apart from the inputs.
- * With few queries the keys are evaluated in parts that are joined in order by
- * the combiner of partir_attention; the parts are the workspace (0 without).
+ * With few queries the keys are evaluated in parts that are joined in order,
+ * by the softmax combiner as in partir_attention; the parts are the workspace (0
+ * without).
  * Errors: E_NULL, E_SHAPE, E_DIVISIBILITY (n_kv_heads does not divide n_heads),
  * E_LAYOUT, E_WORKSPACE, E_UNSUPPORTED (scale), E_HIP. */
 int partir_cross_attention(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t Sq, int64_t Sk,
@@ -591,10 +597,13 @@ int partir_cross_attention_train(const void* Q, const void* K, const void* V, vo
 /* Gradients of partir_cross_attention for the cotangent dO of O, from the
  * forward's O and lse (formulas as partir_attention_backward).  dQ as Q; dK and
  * dV as K and V, summed over the query heads of a key head; keys behind
- * k_lens get zeros.  The gradients must be apart from each other and from the
- * inputs.  Every gradient is summed in a fixed order, without atomics.
- * Workspace: the rowsums of dO * O and, where the queries or keys are few, fp32
- * parts of the gradients. */
+ * k_lens get zeros, and so does dQ of a sequence without keys, whatever dO and Q
+ * hold.  The gradients must be apart from each other and from the inputs.  Every
+ * gradient is summed in a fixed order, without atomics.
+ * The softmax gradient's D is the rowsum of P * dP up to 256 valid keys, and of
+ * dO * O above.
+ * Workspace: D of every query (Sk = 0 or above 128) and, where the queries or
+ * keys are few, fp32 parts of the gradients. */
 int partir_cross_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
                                     const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
                                     int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
@@ -607,16 +616,17 @@ size_t partir_cross_attention_backward_workspace(int64_t B, int64_t Sq, int64_t 
  * norm[0] (device, float32).  tensors, numel, dtypes: HOST arrays of device
  * pointers, element counts and partir_dtypes (F32 and BF16 may be mixed); a
  * tensor is dense and aligned to its element type only, so it may be a view
- * into a flat bucket.  Squares are summed in float64, in a fixed order.  No
- * tensors, or empty ones: 0.
+ * into a flat bucket.  Squares are summed in float64, in a fixed order; a norm
+ * above float32's range is stored as infinity.  No tensors, or empty ones: 0.
  * Errors: E_NULL, E_SHAPE, E_DTYPE, E_LAYOUT, E_WORKSPACE, E_HIP. */
 int partir_grad_norm(const void* const* tensors, const int64_t* numel, const int* dtypes, int n, float* norm, void* ws,
                      size_t ws_bytes, void* stream);
 
 /* partir_grad_norm, then out[i] = tensors[i] * (norm > max_norm ? max_norm /
- * norm : 1), each value rounded once to its type.  out: HOST array of device
- * pointers; out[i] = tensors[i] scales in place (nothing is written where the
- * norm is within max_norm).  Where an element is infinite or NaN, so is the
+ * norm : 1) with the float64 norm, each value a float64 product rounded to
+ * float32 and, in bf16, from there to bf16.  out: HOST array of device pointers;
+ * out[i] = tensors[i] scales in place (nothing is written where the norm is
+ * within max_norm).  Where an element is infinite or NaN, so is the
  * norm, and nothing is scaled: the tensors are copied as they are.  Outputs must
  * be apart from each other, from norm and from other tensors' inputs (E_LAYOUT).
  * max_norm >= 0 (E_UNSUPPORTED otherwise). */
