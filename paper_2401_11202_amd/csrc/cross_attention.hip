@@ -14,7 +14,7 @@
 // with V^T from transposed LDS reads.  Where rows are few the matrix units wait
 // for K and V, and what that rounding leaves is a second operand (within 2^-16
 // then), so that O's error is its own rounding: 1.66e-3 of its size, 2.34e-3 with
-// one (64 x 8192 keys, 363 us either way; the smallest calls take 0.3 to 0.7 us more).  Sums and O are float32; groups and key
+// one (64 x 8192 keys, 363 us either way; the smallest calls take 0.2 to 0.6 us more).  Sums and O are float32; groups and key
 // parts join by (m, l, O) (+) (m', l', O'), in a fixed order.
 //
 // Keys at and behind len_b are never read: their tile rows are zeros (the
@@ -174,6 +174,7 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
     }
     float lsum = 0.0f;
     bf16x8 pf[2 * NSUB], pl[2 * NSUB];   // the weights in bf16, and what is left of them (few rows)
+    f32x16 ef[NSUB];                     // the weights (few rows)
     auto weights = [&]() {
       lsum = 0.0f;
 #pragma unroll
@@ -182,9 +183,10 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
         for (int v = 0; v < 16; ++v) {
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][v], sl2, -m_run));
           lsum += e;
-          const __bf16 hi = (__bf16)e;
-          pf[2 * t + (v >> 3)][v & 7] = hi;
-          if constexpr (ALONE) pl[2 * t + (v >> 3)][v & 7] = (__bf16)(e - (float)hi);
+          if constexpr (ALONE)
+            ef[t][v] = e;
+          else
+            pf[2 * t + (v >> 3)][v & 7] = (__bf16)e;
         }
     };
     // m moves only where the block's maximum is more than 8 (log2 units)
@@ -214,6 +216,14 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(Cros
     }
     l_run += lsum;
     if constexpr (ALONE) {
+#pragma unroll
+      for (int t = 0; t < NSUB; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const __bf16 hi = (__bf16)ef[t][v];
+          pf[2 * t + (v >> 3)][v & 7] = hi;
+          pl[2 * t + (v >> 3)][v & 7] = (__bf16)(ef[t][v] - (float)hi);
+        }
       __builtin_amdgcn_sched_barrier(0);
       WAIT_VMCNT(3 * LPB / 2);             // after this V: the next K and V, the K after
       asm volatile("" ::: "memory");
