@@ -12,24 +12,25 @@
 // the weights of partir_attention), is the B operand of
 //     O^T[128 x 32 rows] += V_blk^T P^T
 // with V^T from transposed LDS reads.  Where rows are few the matrix units wait
-// for K and V, and what that rounding leaves is a second operand (within 2^-16
-// then), so that O's error is its own rounding: 1.66e-3 of its size, 2.34e-3 with
-// one (64 x 8192 keys, 363 us either way; the smallest calls take 0.2 to 0.6 us more).  Sums and O are float32; groups and key
-// parts join by (m, l, O) (+) (m', l', O'), in a fixed order.
+// for K and V, and what that rounding leaves is a second operand (the weights
+// are within 2^-16 then), so that O's error is its own rounding: 1.66e-3 of its
+// size, 2.34e-3 with one (64 x 8192 keys, 363 us either way; the smallest calls
+// take 0.2 to 0.6 us more).  Sums and O are float32; groups and key parts join by
+// (m, l, O) (+) (m', l', O'), in a fixed order.
 //
 // Keys at and behind len_b are never read: their tile rows are zeros (the
 // descriptor ends before them), so what the padding holds, NaN included, does
 // not reach a product, and their scores are -inf.  A sequence without keys
 // gives 0 and a log-sum-exp of -inf.
 //
-// What bounds it.  Many rows: the matrix units, beside which exp2 and the
-// conversions of a score take about as long (16 of the first, 4 cycles a value
-// elsewhere); three waves a SIMD in different phases hide one behind the other.
-// 4 x 4096 queries over up to 2048 keys, 32 / 8 heads (0.44 TFLOP): 430 us, 1.02
-// PFLOP/s, the matrix units busy 57 % of the time.  With 64-key blocks and two
-// stages (two waves a SIMD) 452, with two key groups 456.  Few rows: the reading
-// of K and V; 131072 keys of 8 key heads (537 MB): 93 us, 5.8 TB/s, and 5 for the
-// join; 32 sequences of up to 1501 keys (109 MB): 28 us.
+// What bounds it.  Many rows: the matrix units, and exp2 and the conversions of
+// a score, which take about as long (16 cycles of the first, 4 a value elsewhere)
+// and lie behind one another's time only in part, with three waves a SIMD: busy
+// 57 and 45 % of the time, they still add up to all of it.  4 x 4096 queries over up to 2048 keys, 32 / 8 heads (0.44 TFLOP): 430 us, 1.02
+// PFLOP/s.  With 64-key blocks and two stages (two waves a SIMD) 452, with two key
+// groups 456.  Few rows: the reading of K and V; 131072 keys of 8 key heads (537
+// MB): 93 us, 5.8 TB/s, and 5 for the join; 32 sequences of up to 1501 keys (109
+// MB): 27 us.
 #include <algorithm>
 #include <type_traits>
 

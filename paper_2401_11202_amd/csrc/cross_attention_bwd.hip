@@ -253,8 +253,10 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
 // wave forms S and P, dP, dV^T += dO^T P, then dS and dK^T += Q^T dS.  One pass for
 // both gradients forms S, P and dP once, 4 products where a pass for each takes
 // 5, and three quarters of their time at the size above.  Two scheduling barriers keep phases
-// apart where the compiler would otherwise hold the operands of several at once
-// and spill; one at every phase costs their overlap (24 % more).
+// apart where the compiler would otherwise hold the operands of several at once;
+// one at every phase costs their overlap (24 % more).  Eight registers (nine
+// without EVEN) are spilled still, addresses of the tiles' loads and of the
+// statistics, of which a tile reads four or five back.
 template <bool EVEN>
 __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams p) {
   constexpr int STAGES = 0, VT = 2 * 2 * TILE, STAT = VT + 256 * ROWB;

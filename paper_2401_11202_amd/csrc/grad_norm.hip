@@ -5,13 +5,19 @@
 // launch for up to kGradTensors tensors: the table of the tensors travels in
 // the kernel arguments, so nothing is uploaded and nothing kept.  A workgroup
 // takes a run of consecutive 32 KiB chunks, 16 bytes a lane and load, eight
-// loads in flight; chunks never cross a tensor, so the ends of a tensor that
-// are not 16-byte aligned cost a few single loads there.  Squares are summed
-// in float64: float32 overflows from 2e19 on and loses the small tensors of a
-// sum of 1e9 terms; conversions and adds of float64 are well within what the
-// load rate leaves.  The partial sums are added in a fixed order by every
-// workgroup of the second pass for itself, which saves a launch between; more
-// than kGradDirect of them are added to kGradFolded by a launch first.
+// loads in flight; chunks never cross a tensor.  Squares are summed in float64:
+// float32 overflows from 2e19 on and loses the small tensors of a sum of 1e9
+// terms; conversions and adds of float64 are well within what the load rate
+// leaves.  The partial sums are added in a fixed order by every workgroup of the
+// second pass for itself, which saves a launch between; more than kGradDirect of
+// them are added to kGradFolded by a launch first.
+//
+// A tensor off a 16-byte boundary has every chunk start and end off one: single
+// values there, and one load at a time between them.  Where input and output lie
+// differently to the boundary, scaling goes by single values.  128 tensors of
+// 2^20 values, replayed, norm / clipping apart: float32 108 / 335 us aligned, 143 /
+// 412 at 8 bytes from the boundary, 114 / 498 with the output alone there; bf16 59 /
+// 182, 66 / 213, 58 / 370.
 //
 // What bounds it is HBM: one read for the norm, one read and one write for the
 // scaling, which is left out where nothing would change (in place, N <=
