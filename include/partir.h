@@ -483,7 +483,8 @@ size_t partir_decoder_layer_workspace(int64_t B, int64_t S, int64_t D, int64_t n
 
 /* ------------------------------------------------------------------------ */
 /* Operators beside the nests: positions, norms of queries and keys,           */
-/* attention to another sequence, the norm of the gradients.                   */
+/* attention to another sequence, dropout, the join with the residual stream,  */
+/* the norm of the gradients.                                                  */
 /* ------------------------------------------------------------------------ */
 /* These take their leading dimensions as arguments, so that queries, keys and
  * values can be column blocks of one fused projection.  The conventions above
@@ -611,6 +612,65 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
                                     const int32_t* k_lens, float scale, void* ws, size_t ws_bytes, void* stream);
 size_t partir_cross_attention_backward_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
                                                  int64_t d_head);
+
+/* Dropout from a counter-based generator: Y = R + (kept ? X / share kept : 0).
+ * X, Y: [T, D], R: [T, D] of Y's type or NULL (none); x_dtype and y_dtype F32 or
+ * BF16 each, leading dims ldx, ldr, ldy.  Y may be X (pointer, type and leading dim
+ * alike) or R, else it is apart from them.
+ * seed: two uint64 on the DEVICE, key and stream (a layer's number, a step's), read
+ * when the call runs, so that a captured graph takes what they hold at its replay.
+ * Element (t, d) is kept where the 16 bits that Philox 4x32 (Salmon et al., 2011;
+ * ten rounds) gives it are below k = floor((1 - p) 65536 + 1/2), and then multiplied
+ * by 65536 / k: p counts in steps of 1 / 65536.  Key: seed[0]; counter: (d / 8,
+ * row0 + t, low and high half of seed[1]); the bits: half d % 2 (0: the low one) of
+ * word (d % 8) / 2.  So the mask depends on the seed and the element's place only:
+ * the gradient is the same call on the cotangent of Y, without R; parts of the rows
+ * drop what the whole does, with row0 the number of their first.  What is dropped
+ * is 0 (R) whatever X holds there.
+ * p within 0..1 (1: all is dropped).  row0 + T at most 2^32.  D may be any size up
+ * to 2^24; rows start on 16 bytes.
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_LAYOUT, E_UNSUPPORTED (p), E_HIP. */
+int partir_dropout(const void* X, const void* R, void* Y, int64_t T, int64_t D, int64_t ldx, int64_t ldr, int64_t ldy,
+                   int x_dtype, int y_dtype, double p, const uint64_t* seed, int64_t row0, void* stream);
+
+/* Joins a block's output Y with the residual stream X, and norms the sum for the
+ * next block, in one pass:
+ *   U = post_norm ? g_post * Y / sqrt(mean(Y^2) + eps) : Y
+ *   H = X + scale * gate * dropout(U)
+ *   N = g_pre * H / sqrt(mean(H^2) + eps)
+ * X, H: [T, D] x_dtype; Y, N: [T, D] y_dtype (F32 or BF16 each); means are over the
+ * D values of a row, in float32, N is taken from H before it is rounded.  H may be X
+ * and N may be Y (pointer and leading dim alike), else they are apart from all
+ * else.  N may be NULL: no next norm.
+ * g_post, g_pre: [D] f32, or NULL: 1.  gate: [ceil(T / gate_rows), D] f32, leading
+ * dim ldgate, or NULL: 1; row t takes gate row t / gate_rows.
+ * p, seed, row0: dropout of U as in partir_dropout; seed may be NULL with p = 0.
+ * D: a multiple of 8 up to 16384.
+ * Errors: E_NULL, E_SHAPE, E_DTYPE, E_LAYOUT, E_UNSUPPORTED (p, eps, scale), E_HIP. */
+int partir_residual_norm(const void* X, const void* Y, const float* g_post, const float* gate, const float* g_pre, void* H,
+                         void* N, int64_t T, int64_t D, int64_t gate_rows, int64_t ldx, int64_t ldy, int64_t ldgate,
+                         int64_t ldh, int64_t ldn, int x_dtype, int y_dtype, int post_norm, float scale, double p,
+                         const uint64_t* seed, int64_t row0, float eps, void* stream);
+
+/* Gradients of partir_residual_norm for the cotangents dH (x_dtype; NULL: 0) and dN
+ * (y_dtype; NULL: the forward had no N), from the X and Y that the forward read
+ * (nothing is kept by it; X is not read without dN).  H is formed again in float32.
+ *   dX (x_dtype): the gradient of H, dN's share included;  dY (y_dtype);
+ *   dg_post, dg_pre: [D] f32;  dgate: [ceil(T / gate_rows), D] f32, dense; each of
+ *   the three may be NULL (not stored), and must be without its operand
+ *   (E_UNSUPPORTED).
+ * dX may be dH and dY may be dN (pointer and leading dim alike); else the outputs
+ * are apart from each other and from every input.  Sums over rows are float32, in a
+ * fixed order, without atomics.  With T = 0 dg_post and dg_pre are 0.
+ * Workspace: the rows' partial sums; gate_rows = 0 in its query: no gate.
+ * Errors: as partir_residual_norm, and E_WORKSPACE. */
+int partir_residual_norm_backward(const void* X, const void* Y, const void* dH, const void* dN, const float* g_post,
+                                  const float* gate, const float* g_pre, void* dX, void* dY, float* dg_post, float* dgate,
+                                  float* dg_pre, int64_t T, int64_t D, int64_t gate_rows, int64_t ldx, int64_t ldy,
+                                  int64_t lddh, int64_t lddn, int64_t ldgate, int64_t lddx, int64_t lddy, int x_dtype,
+                                  int y_dtype, int post_norm, float scale, double p, const uint64_t* seed, int64_t row0,
+                                  float eps, void* ws, size_t ws_bytes, void* stream);
+size_t partir_residual_norm_backward_workspace(int64_t T, int64_t D, int64_t gate_rows);
 
 /* Global norm of n tensors, sqrt of the sum of every element's square, into
  * norm[0] (device, float32).  tensors, numel, dtypes: HOST arrays of device

@@ -1,9 +1,12 @@
-// Launch interface between operators_api.cpp and the kernels of the operators
-// around the loop nests: rotary positions and per-head norms, cross attention,
-// the global norm of gradients.  Plain structs passed by value.
+// Launch interface between operators_api.cpp, stream_api.cpp and the kernels of
+// the operators around the loop nests: rotary positions and per-head norms, cross
+// attention, the global norm of gradients, dropout, the join of a block with the
+// residual stream.  Plain structs passed by value.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include "philox.h"
 
 namespace partir {
 
@@ -185,5 +188,50 @@ hipError_t launch_grad_norm(const double* partial, int n, float* norm, hipStream
 // partials, which is also stored where `norm` is not NULL
 hipError_t launch_grad_scale(const GradTable& t, const double* partial, int n, double max_norm, float* norm,
                              int workgroups, hipStream_t s);
+
+// ---- dropout (dropout.hip) --------------------------------------------------
+struct DropoutParams {
+  const void *x, *r;       // [T, D], leading dims ldx, ldr; r, the residual, may be NULL
+  void* y;                 // [T, D], of r's type, leading dim ldy
+  int64_t ldx, ldr, ldy, T;
+  int D, cols8;            // cols8 = groups of eight columns of a row, the last perhaps shorter
+  Div by_cols8;
+  Dropout drop;
+};
+hipError_t launch_dropout(const DropoutParams& p, bool x_bf16, bool y_bf16, hipStream_t s);
+
+// ---- join of a block's output with the residual stream (residual_norm.hip) ---
+struct JoinParams {
+  const void *x, *y;       // residual stream and block output [T, D], each of its type
+  const void *dh, *dn;     // backward: cotangents of h (or NULL: 0) and n (NULL: no next norm)
+  void *h, *n;             // forward: the sum, and the next block's input (or NULL)
+  void *dx, *dy;
+  const float *g_post, *g_pre;   // gains [D], or NULL: 1
+  const float* gate;       // [ceil(T / gate_rows), D], or NULL: 1; row t takes gate row t / gate_rows
+  int64_t ldx, ldy, lddh, lddn, ldh, ldn, lddx, lddy, ldgate;
+  int64_t T, gate_rows;
+  int D, post;             // post: the block's output is normed
+  float scale;             // the factor of what dropout keeps included
+  float eps;
+  Dropout drop;
+  // who takes which rows (join_choice): waves of a row, workers (workgroups, or
+  // waves where a row is one wave's); backward: worker w takes `per` rows of span
+  // w / chunks, spans being a gate's row or several whole ones
+  int waves;
+  int64_t workers, span, chunks, per;
+  float *part_post, *part_pre, *part_gate;   // backward: [workers][D] sums, each may be NULL
+  float* dgate_rows;                         // backward: dgate itself, where a worker has whole gate rows
+};
+void join_choice(JoinParams& p, bool backward);
+hipError_t launch_join(const JoinParams& p, bool x_bf16, bool y_bf16, hipStream_t s);
+hipError_t launch_join_backward(const JoinParams& p, bool x_bf16, bool y_bf16, hipStream_t s);
+// Sums of parts for up to three matrices [outs, D]: row o adds parts o * parts ..
+struct JoinSums {
+  const float* part[3];
+  float* out[3];
+  int64_t outs[3], parts[3];
+  int n, D;
+};
+hipError_t launch_join_reduce(const JoinSums& q, hipStream_t s);
 
 }  // namespace partir

@@ -45,7 +45,8 @@ EXPORTS = ("partir_loop_matmul", "partir_loop_matmul_workspace", "partir_mlp_blo
            "partir_clip_grad_norm", "partir_grad_norm_workspace", "partir_cross_attention",
            "partir_cross_attention_workspace", "partir_cross_attention_train", "partir_cross_attention_backward",
            "partir_cross_attention_backward_workspace", "partir_plan_cross_attention",
-           "partir_plan_cross_attention_backward")
+           "partir_plan_cross_attention_backward", "partir_dropout", "partir_residual_norm",
+           "partir_residual_norm_backward", "partir_residual_norm_backward_workspace")
 
 
 class PartirError(RuntimeError):
@@ -154,6 +155,10 @@ def lib():
         "partir_cross_attention_backward_workspace": (SZ, [I64] * 6),
         "partir_plan_cross_attention": (I32, [I64] * 6 + [ctypes.POINTER(PlanInfo)]),
         "partir_plan_cross_attention_backward": (I32, [I64] * 6 + [ctypes.POINTER(PlanInfo)]),
+        "partir_dropout": (I32, [P, P, P, I64, I64, I64, I64, I64, I32, I32, D, P, I64, P]),
+        "partir_residual_norm": (I32, [P] * 7 + [I64] * 8 + [I32, I32, I32, F, D, P, I64, F, P]),
+        "partir_residual_norm_backward": (I32, [P] * 12 + [I64] * 10 + [I32, I32, I32, F, D, P, I64, F, P, SZ, P]),
+        "partir_residual_norm_backward_workspace": (SZ, [I64, I64, I64]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -1125,6 +1130,171 @@ def _plan_sizes(fn, *args):
     info = PlanInfo()
     _check(fn(*args, ctypes.byref(info)))
     return info.as_dict()
+
+
+def _rows(t, name, rows, cols):
+    """dtype code and leading dim of a row-major [rows, cols] f32 or bf16 tensor, a view perhaps."""
+    if not isinstance(t, _th().Tensor):
+        _bad("PARTIR_E_NULL", f"{name} must be a tensor")
+    return _dt(t), _matrix(t, name, rows, cols, t.dtype)
+
+
+def _seed(seed):
+    if seed is not None:
+        torch = _th()
+        if not isinstance(seed, torch.Tensor):
+            _bad("PARTIR_E_NULL", "seed must be a tensor")
+        if seed.dtype is not torch.int64 and seed.dtype is not torch.uint64:
+            _bad("PARTIR_E_DTYPE", f"seed has dtype {seed.dtype}, expected int64 or uint64")
+        _req(seed, "seed", (2,), seed.dtype)
+
+
+def _pitch(cols, dtype):
+    """The least leading dim of rows of `cols` values that start on 16 bytes."""
+    return -(-cols // 8) * 8 if dtype is _torch.bfloat16 else -(-cols // 4) * 4
+
+
+def _same_device(first, *ts):
+    """A call's tensors (None left out) on one GPU."""
+    if not _one_gpu(first[1], *(t for _, t in ts)):
+        _gpu_all(**dict((first, *ts)))
+
+
+def dropout(X, p: float, seed, *, residual=None, row0: int = 0, out_dtype=None, out=None, stream=None):
+    """Dropout of X [T, D] (f32 or bf16, a view with a leading dim allowed), on top of
+    `residual` if given: residual + (kept ? X / share kept : 0), of out_dtype
+    (the residual's, or X's).  seed: two int64 on the GPU, key and stream; the mask
+    is a function of them and of (row0 + t, d), so the gradient is the same call on
+    the cotangent, without the residual.  out: where to write it, X or the residual
+    allowed."""
+    if not isinstance(X, _th().Tensor) or X.dim() != 2:
+        _bad("PARTIR_E_SHAPE", "X must be a 2-D tensor")
+    T, D = X.shape
+    xd, ldx = _rows(X, "X", T, D)
+    if seed is None:
+        _bad("PARTIR_E_NULL", "seed must be a tensor")
+    _seed(seed)
+    if out_dtype is None:
+        out_dtype = (X if out is None and residual is None else residual if out is None else out).dtype
+    ldr = 0 if residual is None else _matrix(residual, "residual", T, D, out_dtype)
+    fresh = out is None
+    if not fresh:
+        ldo = _matrix(out, "out", T, D, out_dtype)
+    _same_device(("X", X), ("seed", seed), ("residual", residual), ("out", out))
+    wide = _pitch(D, out_dtype)
+    if fresh:
+        out, ldo = X.new_empty((T, wide), dtype=out_dtype), wide
+        _on_stream(stream, out)
+        if wide != D:
+            out = out[:, :D]
+    if T == 1:       # one row: any leading dim will do
+        ldx, ldr, ldo = _pitch(D, X.dtype), wide, wide
+    _launch(X.device, lib().partir_dropout, _ptr(X), _ptr(residual), _ptr(out), T, D, ldx, ldr, ldo, xd, _dt(out), float(p),
+            _ptr(seed), row0, stream=stream)
+    return out
+
+
+def _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed):
+    """Checked sizes of a join: (T, D, gate_rows, ldx, ldy, ldgate, x_dtype, y_dtype)."""
+    torch = _th()
+    if not isinstance(Y, torch.Tensor) or Y.dim() != 2:
+        _bad("PARTIR_E_SHAPE", "Y must be a 2-D tensor")
+    T, D = Y.shape
+    xd, ldx = _rows(X, "X", T, D)
+    yd, ldy = _rows(Y, "Y", T, D)
+    _opt(g_post, "g_post", (D,), torch.float32)
+    _opt(g_pre, "g_pre", (D,), torch.float32)
+    ldg = 0
+    if gate is not None:
+        if gate_rows is None:
+            gate_rows = max(T, 1)
+        if gate_rows < 1:
+            _bad("PARTIR_E_SHAPE", f"gate_rows = {gate_rows}")
+        ldg = _matrix(gate, "gate", -(-T // gate_rows), D, torch.float32)
+    _seed(seed)
+    return T, D, gate_rows if gate is not None else 0, ldx, ldy, ldg, xd, yd
+
+
+def residual_norm(X, Y, *, g_post=None, post_norm: bool = False, gate=None, gate_rows: Optional[int] = None, g_pre=None,
+                  next_norm: bool = True, scale: float = 1.0, p: float = 0.0, seed=None, row0: int = 0, eps: float = 1e-6,
+                  out=None, norm_out=None, stream=None):
+    """H = X + scale * gate * dropout(U) with U = Y, or with post_norm g_post * Y /
+    sqrt(mean(Y^2) + eps); and with next_norm N = g_pre * H / sqrt(mean(H^2) + eps).
+    X [T, D] (the residual stream) and Y [T, D] (a block's output) f32 or bf16, each
+    of its type; D a multiple of 8.  g_post, g_pre: gains [D] f32, or None for 1.
+    gate [ceil(T / gate_rows), D] f32: row t takes gate row t // gate_rows (None: one
+    row for all).  p, seed, row0: as dropout.  out, norm_out: where to write H (X
+    allowed) and N (Y allowed).  Returns (H, N), N None without next_norm."""
+    T, D, rows, ldx, ldy, ldg, xd, yd = _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed)
+    if norm_out is not None and not next_norm:
+        _bad("PARTIR_E_UNSUPPORTED", "norm_out without next_norm")
+    fresh_h, fresh_n = out is None, next_norm and norm_out is None
+    ldh = D if fresh_h else _matrix(out, "out", T, D, X.dtype)
+    ldn = D if norm_out is None else _matrix(norm_out, "norm_out", T, D, Y.dtype)
+    _same_device(("Y", Y), ("X", X), ("g_post", g_post), ("gate", gate), ("g_pre", g_pre), ("seed", seed), ("out", out),
+                 ("norm_out", norm_out))
+    if fresh_h:
+        out = X.new_empty((T, D))
+    if fresh_n:
+        norm_out = Y.new_empty((T, D))
+    _on_stream(stream, out if fresh_h else None, norm_out if fresh_n else None)
+    _launch(Y.device, lib().partir_residual_norm, _ptr(X), _ptr(Y), _ptr(g_post), _ptr(gate), _ptr(g_pre), _ptr(out),
+            _ptr(norm_out), T, D, rows, ldx, ldy, ldg, ldh, ldn, xd, yd, bool(post_norm), float(scale), float(p), _ptr(seed),
+            row0, float(eps), stream=stream)
+    return out, norm_out
+
+
+def residual_norm_backward(X, Y, dH, dN, *, g_post=None, post_norm: bool = False, gate=None,
+                           gate_rows: Optional[int] = None, g_pre=None, next_norm: bool = True, scale: float = 1.0,
+                           p: float = 0.0, seed=None, row0: int = 0, eps: float = 1e-6, out=None, gain_out=None,
+                           workspace=None, stream=None):
+    """Gradients (dX, dY, dg_post, dgate, dg_pre) of residual_norm for the cotangents
+    dH of H (None: 0) and dN of N, from the X and Y that the forward read.  dg_post,
+    dgate and dg_pre are f32, None without their operand.  out: (dX, dY) to write
+    into, dH and dN themselves allowed; gain_out: (dg_post, dgate, dg_pre)."""
+    torch = _th()
+    T, D, rows, ldx, ldy, ldg, xd, yd = _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed)
+    if (dN is None) == bool(next_norm):
+        _bad("PARTIR_E_NULL", "dN must be given exactly with next_norm")
+    if dH is None and dN is None:
+        _bad("PARTIR_E_NULL", "dH or dN must be given")
+    lddh = 0 if dH is None else _matrix(dH, "dH", T, D, X.dtype)
+    lddn = 0 if dN is None else _matrix(dN, "dN", T, D, Y.dtype)
+    f32 = torch.float32
+    wants = ((D,) if g_post is not None else None, tuple(gate.shape) if gate is not None else None,
+             (D,) if g_pre is not None else None)
+    if wants[0] is not None and not post_norm:
+        _bad("PARTIR_E_UNSUPPORTED", "g_post without post_norm")
+    if wants[2] is not None and not next_norm:
+        _bad("PARTIR_E_UNSUPPORTED", "g_pre without next_norm")
+    fresh, fresh_g = out is None, gain_out is None
+    lddx = lddy = D
+    if not fresh:
+        if len(out) != 2:
+            _bad("PARTIR_E_SHAPE", "out must hold (dX, dY)")
+        lddx, lddy = _matrix(out[0], "dX", T, D, X.dtype), _matrix(out[1], "dY", T, D, Y.dtype)
+    if not fresh_g:
+        if len(gain_out) != 3:
+            _bad("PARTIR_E_SHAPE", "gain_out must hold (dg_post, dgate, dg_pre)")
+        for t, shape, name in zip(gain_out, wants, ("dg_post", "dgate", "dg_pre")):
+            if t is not None and shape is None:
+                _bad("PARTIR_E_UNSUPPORTED", f"{name} without its operand")
+            _opt(t, name, shape, f32)
+    _same_device(("Y", Y), ("X", X), ("dH", dH), ("dN", dN), ("g_post", g_post), ("gate", gate), ("g_pre", g_pre),
+                 ("seed", seed), *(() if fresh else (("dX", out[0]), ("dY", out[1]))),
+                 *(() if fresh_g else zip(("dg_post", "dgate", "dg_pre"), gain_out)))
+    dev = Y.device
+    if fresh:
+        out = (X.new_empty((T, D)), Y.new_empty((T, D)))
+    if fresh_g:
+        gain_out = tuple(None if s is None else torch.empty(s, dtype=f32, device=dev) for s in wants)
+    ws, wsb = _workspace(dev, workspace, lib().partir_residual_norm_backward_workspace, T, D, rows)
+    _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()), *(gain_out if fresh_g else ()))
+    _launch(dev, lib().partir_residual_norm_backward, _ptr(X), _ptr(Y), _ptr(dH), _ptr(dN), _ptr(g_post), _ptr(gate),
+            _ptr(g_pre), _ptr(out[0]), _ptr(out[1]), _ptr(gain_out[0]), _ptr(gain_out[1]), _ptr(gain_out[2]), T, D, rows,
+            ldx, ldy, lddh, lddn, ldg, lddx, lddy, xd, yd, bool(post_norm), float(scale), float(p), _ptr(seed), row0,
+            float(eps), _ptr(ws), wsb, stream=stream)
+    return (*out, *gain_out)
 
 
 def _grad_arrays(tensors, name):
