@@ -483,7 +483,8 @@ size_t partir_decoder_layer_workspace(int64_t B, int64_t S, int64_t D, int64_t n
 
 /* ------------------------------------------------------------------------ */
 /* Operators beside the nests: positions, norms of queries and keys,           */
-/* attention to another sequence, dropout, the join with the residual stream,  */
+/* attention to another sequence, masked attention, dropout, the join with the  */
+/* residual stream,                                                            */
 /* the norm of the gradients.                                                  */
 /* ------------------------------------------------------------------------ */
 /* These take their leading dimensions as arguments, so that queries, keys and
@@ -613,6 +614,64 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
 size_t partir_cross_attention_backward_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
                                                  int64_t d_head);
 
+/* Masked attention: what a decoder's own tokens need beside partir_attention.
+ * Query s of a sequence stands at position p = q_start + s, key j at position j.
+ *   z = scale q k;   cap > 0:  z = cap tanh(z / cap);   slopes:  z = z - slopes[h] |p - j|
+ *   O = softmax(z) V over the keys j that the query sees:
+ *     j < k_len,  causal:  j <= p or j < prefix_len,  documents: q_docs = k_docs.
+ * A query that sees no key, or stands at or behind its sequence's q_len, gets 0. */
+typedef struct partir_attention_mask {
+  int causal;
+  float cap;                   /* 0: none, else 2^-10 .. 2^10                                       */
+  const float* slopes;         /* device [n_heads], or NULL: no bias; no gradient is formed         */
+  const int32_t* k_lens;       /* device [B] valid keys (clamped to 0..Sk), or NULL: Sk             */
+  const int32_t* q_lens;       /* device [B] valid queries (clamped to 0..Sq), or NULL: Sq          */
+  const int32_t* q_starts;     /* device [B] positions of the first queries (clamped to +-2^29),
+                                  or NULL: Sk - Sq                                                  */
+  const int32_t* prefix_lens;  /* device [B] keys that every query sees, or NULL: none; with causal */
+  const int32_t* q_docs;       /* device [B*Sq] and                                                 */
+  const int32_t* k_docs;       /* device [B*Sk] document numbers, any int32, or both NULL           */
+} partir_attention_mask;
+
+/* Q, K, V, O, sizes, leading dims, scale: as partir_cross_attention (d_head == 128,
+ * any Sq and Sk, shared key heads).  A training row of packed documents has Sq = Sk
+ * and q_docs = k_docs; a padded batch k_lens = q_lens; new tokens over a cache Sq
+ * new rows, k_lens with them included and q_starts = k_lens - Sq.
+ * mask: HOST struct, read during the call.  Queries and keys behind their lens are
+ * not read, whatever they hold.  What the lens leave must be finite: a masked key's
+ * values are multiplied by 0.  Blocks of 64 keys that no query of a tile sees are
+ * not read either: documents in one piece each cost what their own lengths do.
+ * Workspace: tables of the documents, and the parts as in partir_cross_attention.
+ * Errors: as partir_cross_attention; E_NULL (mask, one of q_docs and k_docs),
+ * E_UNSUPPORTED (cap, prefix_lens without causal), E_LAYOUT (O or lse overlaps an
+ * input: O may be Q, with its leading dim). */
+int partir_masked_attention(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t Sq, int64_t Sk,
+                            int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk, int64_t ldv,
+                            int64_t ldo, const partir_attention_mask* mask, float scale, void* ws, size_t ws_bytes,
+                            void* stream);
+size_t partir_masked_attention_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                         int64_t d_head, const partir_attention_mask* mask);
+
+/* The forward of a training step: also the base-2 log-sum-exp of every query's
+ * z, lse [B*Sq, n_heads] fp32 (-inf for a query that gets 0).  Same workspace. */
+int partir_masked_attention_train(const void* Q, const void* K, const void* V, void* O, float* lse, int64_t B, int64_t Sq,
+                                  int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                  int64_t ldv, int64_t ldo, const partir_attention_mask* mask, float scale, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* Gradients of partir_masked_attention for the cotangent dO of O, from the forward's
+ * O and lse.  dQ as Q; dK and dV as K and V, summed over the query heads of a key
+ * head.  Queries that get 0 have no gradient and give none; keys that no query sees
+ * get 0.  The gradients must be apart from each other and from the inputs.  Every
+ * gradient is summed in a fixed order, without atomics. */
+int partir_masked_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                                     const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
+                                     int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                     int64_t ldv, int64_t ldo, int64_t lddo, int64_t lddq, int64_t lddk, int64_t lddv,
+                                     const partir_attention_mask* mask, float scale, void* ws, size_t ws_bytes, void* stream);
+size_t partir_masked_attention_backward_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                                  int64_t d_head, const partir_attention_mask* mask);
+
 /* Dropout from a counter-based generator: Y = R + (kept ? X / share kept : 0).
  * X, Y: [T, D], R: [T, D] of Y's type or NULL (none); x_dtype and y_dtype F32 or
  * BF16 each, leading dims ldx, ldr, ldy.  Y may be X (pointer, type and leading dim
@@ -737,6 +796,11 @@ int partir_plan_cross_attention(int64_t B, int64_t Sq, int64_t Sk, int64_t n_hea
                                 partir_plan_info* info);
 int partir_plan_cross_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
                                          int64_t d_head, partir_plan_info* info);
+/* likewise; flops: with every key seen */
+int partir_plan_masked_attention(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
+                                 const partir_attention_mask* mask, partir_plan_info* info);
+int partir_plan_masked_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                          int64_t d_head, const partir_attention_mask* mask, partir_plan_info* info);
 
 /* Human-readable shard table of the last plan built on this thread
  * (views, offsets, tile grid and #sum realisation per launch).  The string is

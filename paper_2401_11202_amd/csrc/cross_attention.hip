@@ -32,309 +32,11 @@
 // MB): 93 us, 5.8 TB/s, and 5 for the join; 32 sequences of up to 1501 keys (109
 // MB): 27 us.
 #include <algorithm>
-#include <type_traits>
 
-#include "attention_tiles.h"
-#include "operators.h"
+#include "cross_attention_kernel.h"
 
 namespace partir {
 namespace {
-
-// The running maximum before the first key: below every finite score, and a
-// finite number, so that 2^(kNoMax - kNoMax) is 1.
-constexpr float kNoMax = -3.0e38f;
-
-__device__ __forceinline__ int key_count(const CrossParams& p, int b) {
-  return p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
-}
-
-template <int QW, int KG, int BKV, int NS, int OCC>
-__global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(CrossParams p) {
-  constexpr int NSUB = BKV / 32;
-  constexpr int LPB = 2 * BKV / (4 * QW);                       // tile loads of a wave per block, K and V
-  constexpr int T_BYTES = BKV * ROWB, STAGE = 2 * T_BYTES;      // K tile, then V tile
-  constexpr int ND = 4 / KG, PER = QW * 64;                     // 32-wide blocks of O that a key group finishes
-  constexpr int MERGE = KG * (KG - 1) * ND * PER * 64, ML = KG * PER * 8;
-  static_assert(KG * NS * STAGE >= MERGE + ML && KG * NS * STAGE >= QW * KG * row_area<ND, __bf16>() &&
-                (KG == 1 || KG * NS * STAGE >= QW * KG * row_area<ND, float>()), "the stages are reused");
-  __shared__ __attribute__((aligned(1024))) char smem[KG * NS * STAGE];
-
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int w = wave % QW, kg = wave / QW;
-  const int h = lane >> 5, col = lane & 31;
-
-  const int R = p.G * p.Sq;
-  int qb, bh, split = 0;
-  if (p.nsplit == 1 && (p.by_nbh.d & 7) == 0) {
-    // Workgroup i runs on XCD i mod 8: an XCD takes one (sequence, key head)
-    // after the other, whose K and V stay in its L2.
-    const int j = blockIdx.x >> 3, n = p.by_nqb.quot(j);
-    bh = n * 8 + (blockIdx.x & 7);
-    qb = p.by_nqb.rem(j, n);
-  } else {
-    const int r = p.by_nbh.quot(blockIdx.x);
-    bh = p.by_nbh.rem(blockIdx.x, r);
-    qb = p.by_split.quot(r);
-    split = p.by_split.rem(r, qb);
-  }
-  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
-
-  // this lane's row: queries (B operand of S^T) in registers
-  const int i = qb * 32 * QW + 32 * w + col;
-  const int ic = min(i, R - 1), sq = p.by_g.quot(ic);
-  const int64_t tq = (int64_t)b * p.Sq + sq;
-  const int head = kvh * p.G + p.by_g.rem(ic, sq);
-  bf16x8 qf[8];
-  {
-    const uint16_t* qrow = p.Q + tq * p.ldq + head * DH + 8 * h;
-#pragma unroll
-    for (int ds = 0; ds < 8; ++ds) qf[ds] = *(const bf16x8*)(qrow + 16 * ds);
-  }
-  const CrossRange range = cross_range(key_count(p, b), p.by_split, split);
-  if (p.nsplit > 1 && split >= range.parts) return;   // the combine does not read it
-
-  const uint16_t* kbase = p.K + (int64_t)b * p.Sk * p.ldk + kvh * DH;
-  const uint16_t* vbase = p.V + (int64_t)b * p.Sk * p.ldv + kvh * DH;
-  char* const stages = smem + kg * NS * STAGE;
-  // K or V of key block kb of the part into a stage; the addresses are 64-bit, so
-  // a part may hold any number of bytes
-  auto kload = [&](int kb, int buf) {
-    const int64_t k0 = range.begin + (int64_t)kb * BKV;
-    tile_load<BKV, QW>(kbase + k0 * p.ldk, p.ldk, (int)min((int64_t)BKV, range.end - k0), stages + buf * STAGE, w, lane);
-  };
-  auto vload = [&](int kb, int buf) {
-    const int64_t k0 = range.begin + (int64_t)kb * BKV;
-    tile_load<BKV, QW>(vbase + k0 * p.ldv, p.ldv, (int)min((int64_t)BKV, range.end - k0), stages + buf * STAGE + T_BYTES, w,
-                       lane);
-  };
-
-  f32x16 oacc[4];
-#pragma unroll
-  for (int d = 0; d < 4; ++d) zero(oacc[d]);
-  float m_run = kNoMax, l_run = 0.0f;
-  TileTr tr;
-  tr.init(lane);
-  const int nkb = (range.end - range.begin + BKV - 1) / BKV;
-  const float sl2 = p.scale_log2;
-
-  // Rings of NS stages for K and for V: loads run ahead, and blocks behind the
-  // last are loaded too (no row of them is read: zeros), which keeps the counts
-  // of loads in flight constant.  Where a wave has its stages to itself (QW = 1)
-  // nothing but its own loads is waited for, and a stage is loaded anew as soon
-  // as its products are done; else a barrier a block says that everyone's loads
-  // have landed and that the stage loaded next is done with.
-  constexpr bool ALONE = QW == 1;
-  static_assert(!ALONE || NS == 2, "two blocks in flight");
-#pragma unroll
-  for (int n = 0; n < NS - !ALONE; ++n) {
-    kload(n * KG + kg, n);
-    vload(n * KG + kg, n);
-  }
-  auto block = [&](auto stage_c, int kb) {
-    constexpr int cur = decltype(stage_c)::value;
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (ALONE) {
-      WAIT_VMCNT(3 * LPB / 2);             // after this K: its V, the next K and V
-      asm volatile("" ::: "memory");
-    } else {
-      WAIT_VMCNT(LPB * (NS - 2));
-      asm volatile("s_barrier" ::: "memory");
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (!ALONE) {
-      kload(kb + KG * (NS - 1), (cur + NS - 1) % NS);
-      vload(kb + KG * (NS - 1), (cur + NS - 1) % NS);
-    }
-    if (!ALONE && KG > 1 && kb >= nkb) return;
-    const char* ks = stages + cur * STAGE;
-    const char* vs = ks + T_BYTES;
-    __builtin_amdgcn_s_setprio(1);
-    f32x16 sacc[NSUB];
-#pragma unroll
-    for (int t = 0; t < NSUB; ++t) {
-      zero(sacc[t]);
-#pragma unroll
-      for (int ds = 0; ds < 8; ++ds) sacc[t] = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], sacc[t]);
-    }
-    __builtin_amdgcn_s_setprio(0);
-    if constexpr (ALONE) {
-      __builtin_amdgcn_sched_barrier(0);   // the products hold what they read of the stage
-      WAIT_LGKMCNT(0);
-      asm volatile("" ::: "memory");
-      kload(kb + KG * NS, cur);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    const int left = range.end - (range.begin + kb * BKV);   // keys from this block on
-    if (left < BKV) {
-#pragma unroll
-      for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= left) sacc[t][v] = -__builtin_inff();
-    }
-    float lsum = 0.0f;
-    bf16x8 pf[2 * NSUB], pl[2 * NSUB];   // the weights in bf16, and what is left of them (few rows)
-    f32x16 ef[NSUB];                     // the weights (few rows)
-    auto weights = [&]() {
-      lsum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][v], sl2, -m_run));
-          lsum += e;
-          if constexpr (ALONE)
-            ef[t][v] = e;
-          else
-            pf[2 * t + (v >> 3)][v & 7] = (__bf16)e;
-        }
-    };
-    // m moves only where the block's maximum is more than 8 (log2 units)
-    // above it: weights stay below 2^8, exact range in float32 and bf16, and
-    // O is rescaled in few blocks.  A lane whose weights sum to at most 2^8
-    // has none above, so the maximum is taken only where some lane's sum is
-    // larger (or inf / NaN, as on the first block, where m is kNoMax).
-    weights();
-    if (__builtin_amdgcn_ballot_w64(!(lsum <= 256.0f)) != 0) {
-      float mloc = -__builtin_inff();
-#pragma unroll
-      for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) mloc = fmaxf(mloc, sacc[t][v]);
-      mloc = fmaxf(mloc, __shfl_xor(mloc, 32));   // the partner lane holds the row's other keys
-      const float m_blk = mloc * sl2;
-      const bool move = m_blk > m_run + 8.0f;
-      if (__builtin_amdgcn_ballot_w64(move) != 0) {
-        const float m_new = move ? m_blk : m_run;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= alpha;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) oacc[d] *= alpha;
-        m_run = m_new;
-        weights();
-      }
-    }
-    l_run += lsum;
-    if constexpr (ALONE) {
-#pragma unroll
-      for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const __bf16 hi = (__bf16)ef[t][v];
-          pf[2 * t + (v >> 3)][v & 7] = hi;
-          pl[2 * t + (v >> 3)][v & 7] = (__bf16)(ef[t][v] - (float)hi);
-        }
-      __builtin_amdgcn_sched_barrier(0);
-      WAIT_VMCNT(3 * LPB / 2);             // after this V: the next K and V, the K after
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int u = 0; u < BKV / 16; ++u)
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const bf16x8 v = tr.read(vs, u, d);
-        oacc[d] = mfma(v, pf[u], oacc[d]);
-        if constexpr (ALONE) oacc[d] = mfma(v, pl[u], oacc[d]);
-      }
-    if constexpr (ALONE) {
-      __builtin_amdgcn_sched_barrier(0);
-      WAIT_LGKMCNT(0);
-      asm volatile("" ::: "memory");
-      vload(kb + KG * NS, cur);
-    }
-  };
-  // NS blocks a trip, so that a block's stage is a constant and folds into the
-  // reads' offsets.  With barriers the trip count is the workgroup's, not the
-  // group's.
-  for (int kb = 0; kb < nkb; kb += NS * KG) {
-    if (!ALONE || kb + kg < nkb) block(std::integral_constant<int, 0>{}, kb + kg);
-    if (ALONE ? kb + KG + kg < nkb : kb + KG < nkb) block(std::integral_constant<int, 1>{}, kb + KG + kg);
-    if constexpr (NS > 2) {
-      if (kb + 2 * KG < nkb) block(std::integral_constant<int, 2>{}, kb + 2 * KG + kg);
-    }
-  }
-  WAIT_VMCNT(0);   // no LDS write is in flight behind the loop
-  __syncthreads();
-
-  float l_tot = l_run + __shfl_xor(l_run, 32);
-  if constexpr (KG > 1) {
-    // The groups' (m, l, O) together, in order.  Group g finishes the ND blocks
-    // of O from g ND on: it hands the others theirs and takes what they hold of
-    // its own.
-    auto box = [&](int to, int from, int d) {   // from != to
-      return (f32x4*)(smem + (((to * (KG - 1) + (from < to ? from : from - 1)) * ND + d) * PER + w * 64 + lane) * 16);
-    };
-    constexpr int STEP = KG * (KG - 1) * ND * PER;   // between the four quarters of a block
-    float2* const ml = (float2*)(smem + MERGE) + w * 64 + lane;
-    ml[kg * PER] = make_float2(m_run, l_tot);
-#pragma unroll
-    for (int g = 0; g < KG; ++g)
-      if (g != kg) {
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            box(g, kg, d)[q * STEP] = f32x4{oacc[g * ND + d][4 * q + 0], oacc[g * ND + d][4 * q + 1],
-                                            oacc[g * ND + d][4 * q + 2], oacc[g * ND + d][4 * q + 3]};
-      }
-    __syncthreads();
-    float2 st[KG];
-    m_run = kNoMax;
-#pragma unroll
-    for (int g = 0; g < KG; ++g) {
-      st[g] = ml[g * PER];
-      m_run = fmaxf(m_run, st[g].x);   // a group without keys holds (kNoMax, 0, 0)
-    }
-    f32x16 own[ND];
-#pragma unroll
-    for (int g = 0; g < KG; ++g)       // this group's own blocks (a constant index for every g)
-      if (g == kg) {
-#pragma unroll
-        for (int d = 0; d < ND; ++d) own[d] = oacc[g * ND + d];
-      }
-    f32x16 sum[ND];
-#pragma unroll
-    for (int d = 0; d < ND; ++d) zero(sum[d]);
-    l_tot = 0.0f;
-#pragma unroll
-    for (int g = 0; g < KG; ++g) {
-      const float a = __builtin_amdgcn_exp2f(st[g].x - m_run);
-      l_tot += a * st[g].y;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        f32x16 v = own[d];
-        if (g != kg) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4 x = box(kg, g, d)[q * STEP];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
-          }
-        }
-        sum[d] += a * v;
-      }
-    }
-#pragma unroll
-    for (int d = 0; d < ND; ++d) oacc[d] = sum[d];
-    __syncthreads();   // the boxes are read: their memory takes the rows
-  }
-  const int row0 = qb * 32 * QW + 32 * w;        // this wave's first row
-  const int64_t row = tq * p.Hq + head;          // this lane's
-  if (p.nsplit > 1) {
-    if constexpr (KG > 1) {   // cross_choice takes parts with several key groups only
-      const int64_t at = (int64_t)split * p.B * p.Sq * p.Hq + row;
-      store_rows<ND>(smem + wave * row_area<ND, float>(), p.Opart, at * DH + kg * ND * 32, R - row0, oacc, 1.0f, lane);
-      if (kg == 0 && h == 0 && i < R) p.MLpart[at] = make_float2(m_run, l_tot);
-    }
-    return;
-  }
-  if (p.lse && kg == 0 && h == 0 && i < R) p.lse[row] = nkb > 0 ? m_run + __builtin_amdgcn_logf(l_tot) : -__builtin_inff();
-  // O times 1 / l of its row (the lane's own)
-  store_rows<ND>(smem + wave * row_area<ND, __bf16>(), (__bf16*)p.O, tq * p.ldo + head * DH + kg * ND * 32, R - row0, oacc,
-                 nkb > 0 ? 1.0f / l_tot : 0.0f, lane);
-}
 
 // O = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - M), M = max m_s.  A row of
 // 128 takes 32 threads, 4 columns each, in each of 8 groups that share the
@@ -348,7 +50,7 @@ __global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams p) {
   const int grp = threadIdx.x >> 5, c4 = threadIdx.x & 31;
   const int64_t tq = row / p.Hq;
   const int head = (int)(row - tq * p.Hq), b = (int)(tq / p.Sq);
-  const int parts = cross_range(key_count(p, b), p.by_split, 0).parts;
+  const int parts = cross_range(clamp_len(p.lens, b, p.Sk), p.by_split, 0).parts;
   float M = kNoMax;
   for (int s = c4; s < parts; s += 32) M = fmaxf(M, p.MLpart[s * rows + row].x);
 #pragma unroll
@@ -412,11 +114,11 @@ hipError_t launch_cross_attention(const CrossParams& p, const CrossChoice& c, hi
   const int64_t rows = (int64_t)p.G * p.Sq, nqb = (rows + 32 * c.qw - 1) / (32 * c.qw);
   const dim3 grid((unsigned)(nqb * p.B * p.Hk * p.nsplit));
   if (c.qw == 1)
-    hipLaunchKernelGGL((cross_attention_kernel<1, 4, 32, 2, 1>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((cross_attention_kernel<1, 4, 32, 2, 1, 0>), grid, dim3(256), 0, s, p);
   else if (c.kg == 2)
-    hipLaunchKernelGGL((cross_attention_kernel<4, 2, 64, 2, 2>), grid, dim3(512), 0, s, p);
+    hipLaunchKernelGGL((cross_attention_kernel<4, 2, 64, 2, 2, 0>), grid, dim3(512), 0, s, p);
   else
-    hipLaunchKernelGGL((cross_attention_kernel<4, 1, 32, 3, 3>), grid, dim3(256), 0, s, p);
+    hipLaunchKernelGGL((cross_attention_kernel<4, 1, 32, 3, 3, 0>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -126,6 +126,30 @@ __device__ __forceinline__ CrossRange cross_range(int len, const Div& by_split, 
   return r;
 }
 
+// ---- masked attention (masked_attention.hip) --------------------------------
+// Attention to a sequence's own keys or to a cache, by the same kernels.
+struct MaskArgs {
+  const int32_t *q_lens, *q_starts, *prefix;   // [B] each, or NULL: Sq, Sk - Sq, 0
+  const int32_t *q_docs, *k_docs;              // [B Sq], [B Sk], or both NULL: one document
+  const int2 *q_table, *k_table;               // their least and largest of every 64 positions, [B][blocks]
+  int q_blocks, k_blocks;
+  const float* slopes;                         // [Hq]
+  float cap_log2, cap_rate;                    // cap log2 e, 2 scale log2 e / cap
+  int causal;
+};
+struct MaskedParams : CrossParams {
+  MaskArgs mask;
+};
+hipError_t launch_masked_attention(const MaskedParams& p, int form, const CrossChoice& c, hipStream_t s);
+hipError_t launch_masked_combine(const MaskedParams& p, hipStream_t s);
+// The tables of both sequences' documents, into q_table and k_table.
+struct DocTables {
+  const int32_t *docs[2], *lens[2];
+  int2* table[2];
+  int S[2], blocks[2], B;
+};
+hipError_t launch_doc_tables(const DocTables& t, hipStream_t s);
+
 // Gradients (cross_attention_bwd.hip).  Up to 128 keys a sequence: one pass.
 // Above: a dq pass, which takes the key axis in q_parts parts, and one for dk and
 // dv.  A pass that yields dk and dv takes the query rows in k_parts; more than
@@ -144,13 +168,18 @@ struct CrossBwdParams {
   Div by_g, by_hk, by_nbh, by_nqb, by_q_parts, by_k_parts;
   float scale, scale_log2;
 };
+struct MaskedBwdParams : CrossBwdParams {
+  MaskArgs mask;
+};
 struct CrossBwdChoice {
   bool one_pass;
   int q_parts, k_parts;
 };
-CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
+// may_one_pass: up to 128 keys in one pass (not with masks)
+CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, bool may_one_pass = true);
 enum CrossBwdPass { CROSS_ALL, CROSS_DQ, CROSS_DKV };
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s);
+hipError_t launch_masked_backward(const MaskedBwdParams& p, int form, CrossBwdPass pass, hipStream_t s);
 // Sums of parts of up to two matrices [rows, cols] with as many columns: out
 // (bf16, leading dim ld) = sum over the parts, in order.
 struct PartSum {

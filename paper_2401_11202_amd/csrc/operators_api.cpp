@@ -1,5 +1,6 @@
 // Host side of the operators around the loop nests: rotary positions, the
-// norms of queries and keys, cross attention, the global norm of gradients.
+// norms of queries and keys, cross attention, masked attention, the global norm of
+// gradients.
 // As in partir_api.cpp a call validates its arguments, plans its launches and
 // enqueues them on the caller's stream; nothing is enqueued before every
 // argument has passed, and no exception leaves an entry point.
@@ -121,7 +122,7 @@ struct Span {
 // Every written range is apart from every other and from every read range but
 // its own input's, which it is or is apart from: a value scaled twice, or
 // scaled before it is read, would depend on timing.
-int check_apart(const void* const* in, void* const* out, const int64_t* numel, const int* dtypes, int n, const float* norm) {
+int check_spans_apart(const void* const* in, void* const* out, const int64_t* numel, const int* dtypes, int n, const float* norm) {
   std::vector<Span> w, r;
   w.reserve(n + 1);
   auto span = [&](const void* p, int i) {
@@ -197,7 +198,7 @@ int run_grads(const void* const* in, void* const* out, const int64_t* numel, con
   if (!aligned(norm, 4)) return fail(PARTIR_E_LAYOUT, "norm must be 4-byte aligned");
   if (int st = check_ws(grad_ws(n), ws, ws_bytes)) return st;
   if (clip)
-    if (int st = check_apart(in, out, numel, dtypes, n, norm)) return st;
+    if (int st = check_spans_apart(in, out, numel, dtypes, n, norm)) return st;
   std::vector<GradLaunch> all;
   all.reserve((size_t)cdiv(n, kGradTensors));
   grad_launches(in, out, numel, dtypes, n, all);
@@ -339,6 +340,123 @@ PartSum part_sum(int n, int parts, int64_t rows, int64_t cols) {
   r.n = n; r.parts = parts; r.rows = rows; r.cols = (int)cols;
   r.by_cols4 = Div::by((uint32_t)(cols / 4));
   return r;
+}
+
+// ---------------------------------------------------------------------------
+// masked attention
+// ---------------------------------------------------------------------------
+constexpr int kFormCap = 2, kFormBias = 4;   // bits of a kernel's form
+
+// The checks of a mask, and what the kernels take of it.
+int resolve_mask(MaskArgs& m, int& form, const partir_attention_mask* mask, float scale) {
+  if (!mask) return fail(PARTIR_E_NULL, "mask must be non-NULL");
+  if (!(mask->cap == 0.0f || (mask->cap >= 0.0009765625f && mask->cap <= 1024.0f)))
+    return fail(PARTIR_E_UNSUPPORTED, "cap must be 0 or within 2^-10 .. 2^10");
+  if (mask->prefix_lens && !mask->causal) return fail(PARTIR_E_UNSUPPORTED, "prefix_lens without causal");
+  if (!mask->q_docs != !mask->k_docs) return fail(PARTIR_E_NULL, "q_docs and k_docs must be given together");
+  const struct { const char* name; const void* p; } all[] = {
+      {"slopes", mask->slopes}, {"k_lens", mask->k_lens}, {"q_lens", mask->q_lens}, {"q_starts", mask->q_starts},
+      {"prefix_lens", mask->prefix_lens}, {"q_docs", mask->q_docs}, {"k_docs", mask->k_docs}};
+  for (const auto& a : all)
+    if (!aligned(a.p, 4)) return fail(PARTIR_E_LAYOUT, "%s must be 4-byte aligned", a.name);
+  m.q_lens = mask->q_lens; m.q_starts = mask->q_starts; m.prefix = mask->prefix_lens;
+  m.q_docs = mask->q_docs; m.k_docs = mask->k_docs;
+  m.slopes = mask->slopes;
+  m.causal = mask->causal != 0;
+  form = (mask->cap > 0.0f ? kFormCap : 0) | (mask->slopes ? kFormBias : 0);
+  if (mask->cap > 0.0f) {
+    m.cap_log2 = mask->cap * kLog2e;
+    m.cap_rate = 2.0f * scale * kLog2e / mask->cap;
+    if (!(m.cap_rate > 1e-30f && m.cap_rate < 1e30f)) return fail(PARTIR_E_UNSUPPORTED, "scale / cap outside 1e-30 .. 1e30");
+  }
+  return PARTIR_OK;
+}
+
+// Documents' tables, at the front of the workspace.
+struct DocPlan {
+  int q_blocks = 0, k_blocks = 0;
+  size_t q_bytes = 0, k_bytes = 0;
+  size_t ws() const { return q_bytes + k_bytes; }
+};
+DocPlan plan_docs(const CrossSizes& z, const partir_attention_mask& mask) {
+  DocPlan d;
+  if (!mask.k_docs) return d;
+  d.q_blocks = (int)cdiv(z.Sq, 64);
+  d.k_blocks = (int)cdiv(z.Sk, 64);
+  d.q_bytes = align_up((size_t)z.B * d.q_blocks * 8);
+  d.k_bytes = align_up((size_t)z.B * d.k_blocks * 8);
+  return d;
+}
+
+int run_doc_tables(MaskArgs& m, const DocPlan& d, const CrossSizes& z, const int32_t* k_lens, void* ws, hipStream_t s) {
+  if (!d.ws()) return PARTIR_OK;
+  m.q_blocks = d.q_blocks; m.k_blocks = d.k_blocks;
+  m.q_table = (const int2*)ws;
+  m.k_table = (const int2*)((char*)ws + d.q_bytes);
+  DocTables t{};
+  t.B = (int)z.B;
+  t.docs[0] = m.q_docs; t.lens[0] = m.q_lens; t.table[0] = (int2*)ws; t.S[0] = (int)z.Sq; t.blocks[0] = d.q_blocks;
+  t.docs[1] = m.k_docs; t.lens[1] = k_lens; t.table[1] = (int2*)((char*)ws + d.q_bytes); t.S[1] = (int)z.Sk; t.blocks[1] = d.k_blocks;
+  return launched(launch_doc_tables(t, s), "doc_tables");
+}
+
+// What forward and backward kernels share of their parameters.
+template <typename P>
+void fill_sizes(P& p, const CrossSizes& z) {
+  p.B = (int)z.B; p.Sq = (int)z.Sq; p.Sk = (int)z.Sk; p.Hq = (int)z.Hq; p.Hk = (int)z.Hk; p.G = (int)(z.Hq / z.Hk);
+  p.by_g = Div::by(p.G);
+  p.by_hk = Div::by(p.Hk);
+  p.by_nbh = Div::by((uint32_t)(z.B * z.Hk));
+}
+
+int run_masked(const void* Q, const void* K, const void* V, void* O, float* lse, bool train, const CrossSizes& z, int64_t ldq,
+               int64_t ldk, int64_t ldv, int64_t ldo, const partir_attention_mask* mask, float scale, void* ws, size_t ws_bytes,
+               void* stream) {
+  if (int st = validate_cross(z)) return st;
+  if (int st = resolve_scale(scale, z.dh)) return st;
+  MaskedParams p{};
+  int form = 0;
+  if (int st = resolve_mask(p.mask, form, mask, scale)) return st;
+  const int64_t Tq = z.B * z.Sq, Tk = z.B * z.Sk;
+  const Matrix q{"Q", Q, Tq, z.Hq * z.dh, ldq, 2}, k{"K", K, Tq ? Tk : 0, z.Hk * z.dh, ldk, 2};
+  const Matrix v{"V", V, Tq ? Tk : 0, z.Hk * z.dh, ldv, 2}, o{"O", O, Tq, z.Hq * z.dh, ldo, 2};
+  const Matrix l{"lse", lse, lse ? Tq : 0, z.Hq, z.Hq, 4};
+  for (const Matrix* m : {&q, &k, &v, &o})
+    if (int st = check(*m)) return st;
+  if (train && Tq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
+  if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
+  if (Tq == 0) return PARTIR_OK;
+  if (int st = check_apart(o, &q, {&k, &v, &l})) return st;   // a workgroup holds its rows of Q before it stores those of O
+  if (int st = check_apart(l, nullptr, {&q, &k, &v})) return st;
+  const CrossPlan plan = plan_cross(z);
+  const DocPlan docs = plan_docs(z, *mask);
+  if (int st = check_ws(docs.ws() + plan.ws(), ws, ws_bytes)) return st;
+  p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)K; p.V = (const uint16_t*)V; p.O = (uint16_t*)O;
+  p.lse = lse; p.lens = mask->k_lens;
+  p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo;
+  fill_sizes(p, z);
+  p.scale_log2 = scale * kLog2e;
+  p.nsplit = plan.c.nsplit;
+  p.by_nqb = Div::by((uint32_t)cdiv((int64_t)p.G * z.Sq, 32 * plan.c.qw));
+  p.by_split = Div::by(p.nsplit);
+  if (p.nsplit > 1) {
+    p.Opart = (float*)((char*)ws + docs.ws());
+    p.MLpart = (float2*)((char*)ws + docs.ws() + plan.o_bytes);
+  }
+  if (int st = begin_launches()) return st;
+  hipStream_t s = (hipStream_t)stream;
+  if (int st = run_doc_tables(p.mask, docs, z, mask->k_lens, ws, s)) return st;
+  if (int st = launched(launch_masked_attention(p, form, plan.c, s), "masked_attention")) return st;
+  return p.nsplit == 1 ? PARTIR_OK : launched(launch_masked_combine(p, s), "masked_combine");
+}
+
+CrossBwdPlan plan_masked_bwd(const CrossSizes& z) {
+  CrossBwdPlan p;
+  p.c = cross_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk, false);
+  p.d_bytes = align_up((size_t)z.B * z.Sq * z.Hq * 4);
+  if (p.c.q_parts > 1) p.q_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
+  if (p.c.k_parts > 1) p.k_bytes = align_up((size_t)p.c.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
+  return p;
 }
 
 void fill_info(partir_plan_info* info, int shards, int launches, size_t ws, double flops) {
@@ -598,6 +716,143 @@ int partir_cross_attention_backward(const void* Q, const void* K, const void* V,
     r.part[0] = p.dKpart; r.out[0] = p.dK; r.ld[0] = lddk;
     r.part[1] = p.dVpart; r.out[1] = p.dV; r.ld[1] = lddv;
     return launched(launch_part_sum(r, s), "cross_bwd_dkv.sum");
+  });
+}
+
+// ---- masked attention ---------------------------------------------------------------
+size_t partir_masked_attention_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                         int64_t d_head, const partir_attention_mask* mask) {
+  const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+  if (guarded([&]() -> int {
+        if (!mask) return fail(PARTIR_E_NULL, "mask must be non-NULL");
+        return validate_cross(z);
+      }))
+    return (size_t)-1;
+  return B * Sq ? plan_docs(z, *mask).ws() + plan_cross(z).ws() : 0;
+}
+
+int partir_plan_masked_attention(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head,
+                                 const partir_attention_mask* mask, partir_plan_info* info) {
+  return guarded([&]() -> int {
+    const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+    if (int st = validate_cross(z)) return st;
+    if (!mask || !info) return fail(PARTIR_E_NULL, "mask and info must be non-NULL");
+    const CrossPlan p = plan_cross(z);
+    const size_t docs = plan_docs(z, *mask).ws();
+    const bool any = B * Sq > 0;
+    fill_info(info, p.c.nsplit, any ? (docs > 0) + 1 + (p.c.nsplit > 1) : 0, any ? docs + p.ws() : 0,
+              4.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
+    return PARTIR_OK;
+  });
+}
+
+int partir_masked_attention(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t Sq, int64_t Sk,
+                            int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk, int64_t ldv,
+                            int64_t ldo, const partir_attention_mask* mask, float scale, void* ws, size_t ws_bytes,
+                            void* stream) {
+  return guarded([&]() -> int {
+    return run_masked(Q, K, V, O, nullptr, false, {B, Sq, Sk, n_heads, n_kv_heads, d_head}, ldq, ldk, ldv, ldo, mask, scale,
+                      ws, ws_bytes, stream);
+  });
+}
+
+int partir_masked_attention_train(const void* Q, const void* K, const void* V, void* O, float* lse, int64_t B, int64_t Sq,
+                                  int64_t Sk, int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                  int64_t ldv, int64_t ldo, const partir_attention_mask* mask, float scale, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    return run_masked(Q, K, V, O, lse, true, {B, Sq, Sk, n_heads, n_kv_heads, d_head}, ldq, ldk, ldv, ldo, mask, scale, ws,
+                      ws_bytes, stream);
+  });
+}
+
+size_t partir_masked_attention_backward_workspace(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                                  int64_t d_head, const partir_attention_mask* mask) {
+  const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+  if (guarded([&]() -> int {
+        if (!mask) return fail(PARTIR_E_NULL, "mask must be non-NULL");
+        return validate_cross(z);
+      }))
+    return (size_t)-1;
+  return B * (Sq + Sk) ? plan_docs(z, *mask).ws() + plan_masked_bwd(z).ws() : 0;
+}
+
+int partir_plan_masked_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
+                                          int64_t d_head, const partir_attention_mask* mask, partir_plan_info* info) {
+  return guarded([&]() -> int {
+    const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+    if (int st = validate_cross(z)) return st;
+    if (!mask || !info) return fail(PARTIR_E_NULL, "mask and info must be non-NULL");
+    const CrossBwdPlan p = plan_masked_bwd(z);
+    const size_t docs = plan_docs(z, *mask).ws();
+    const int launches = (docs > 0) + (B * Sq ? 1 + (p.c.q_parts > 1) : 0) + (B * Sk ? 1 + (p.c.k_parts > 1) : 0);
+    fill_info(info, std::max(p.c.q_parts, p.c.k_parts), launches, B * (Sq + Sk) ? docs + p.ws() : 0,
+              10.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
+    return PARTIR_OK;
+  });
+}
+
+int partir_masked_attention_backward(const void* Q, const void* K, const void* V, const void* O, const void* dO,
+                                     const float* lse, void* dQ, void* dK, void* dV, int64_t B, int64_t Sq, int64_t Sk,
+                                     int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk,
+                                     int64_t ldv, int64_t ldo, int64_t lddo, int64_t lddq, int64_t lddk, int64_t lddv,
+                                     const partir_attention_mask* mask, float scale, void* ws, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
+    if (int st = validate_cross(z)) return st;
+    if (int st = resolve_scale(scale, d_head)) return st;
+    MaskedBwdParams p{};
+    int form = 0;
+    if (int st = resolve_mask(p.mask, form, mask, scale)) return st;
+    const int64_t Tq = B * Sq, Tk = B * Sk, cq = n_heads * d_head, ck = n_kv_heads * d_head;
+    const Matrix q{"Q", Q, Tq, cq, ldq, 2}, k{"K", K, Tk, ck, ldk, 2}, v{"V", V, Tk, ck, ldv, 2}, o{"O", O, Tq, cq, ldo, 2};
+    const Matrix g{"dO", dO, Tq, cq, lddo, 2}, l{"lse", lse, Tq, n_heads, n_heads, 4};
+    const Matrix dq{"dQ", dQ, Tq, cq, lddq, 2}, dk{"dK", dK, Tk, ck, lddk, 2}, dv{"dV", dV, Tk, ck, lddv, 2};
+    for (const Matrix* m : {&q, &k, &v, &o, &g, &dq, &dk, &dv})
+      if (int st = check(*m)) return st;
+    if (int st = check_apart(dq, nullptr, {&q, &k, &v, &o, &g, &l, &dk, &dv})) return st;
+    if (int st = check_apart(dk, nullptr, {&q, &k, &v, &o, &g, &l, &dv})) return st;
+    if (int st = check_apart(dv, nullptr, {&q, &k, &v, &o, &g, &l})) return st;
+    if (Tq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
+    if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
+    if (Tq == 0 && Tk == 0) return PARTIR_OK;
+    const CrossBwdPlan plan = plan_masked_bwd(z);
+    const DocPlan docs = plan_docs(z, *mask);
+    if (int st = check_ws(docs.ws() + plan.ws(), ws, ws_bytes)) return st;
+    p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)K; p.V = (const uint16_t*)V; p.O = (const uint16_t*)O;
+    p.dO = (const uint16_t*)dO; p.lse = lse; p.lens = mask->k_lens;
+    p.dQ = (uint16_t*)dQ; p.dK = (uint16_t*)dK; p.dV = (uint16_t*)dV;
+    char* base = (char*)ws + docs.ws();
+    p.Dstat = (float*)base;
+    p.dQpart = (float*)(base + plan.d_bytes);
+    p.dKpart = (float*)(base + plan.d_bytes + plan.q_bytes);
+    p.dVpart = (float*)(base + plan.d_bytes + plan.q_bytes + plan.k_bytes);
+    p.ldq = ldq; p.ldk = ldk; p.ldv = ldv; p.ldo = ldo; p.ldg = lddo; p.lddq = lddq; p.lddk = lddk; p.lddv = lddv;
+    fill_sizes(p, z);
+    p.q_parts = plan.c.q_parts; p.k_parts = plan.c.k_parts;
+    p.by_nqb = Div::by((uint32_t)std::max<int64_t>(cdiv((int64_t)p.G * Sq, 128), 1));
+    p.by_q_parts = Div::by(p.q_parts);
+    p.by_k_parts = Div::by(p.k_parts);
+    p.scale = scale;
+    p.scale_log2 = scale * kLog2e;
+    if (int st = begin_launches()) return st;
+    hipStream_t s = (hipStream_t)stream;
+    if (int st = run_doc_tables(p.mask, docs, z, mask->k_lens, ws, s)) return st;
+    if (Tq > 0) {
+      if (int st = launched(launch_masked_backward(p, form, CROSS_DQ, s), "masked_bwd_dq")) return st;
+      if (p.q_parts > 1) {
+        PartSum r = part_sum(1, p.q_parts, Tq, cq);
+        r.part[0] = p.dQpart; r.out[0] = p.dQ; r.ld[0] = lddq;
+        if (int st = launched(launch_part_sum(r, s), "masked_bwd_dq.sum")) return st;
+      }
+    }
+    if (Tk == 0) return PARTIR_OK;
+    if (int st = launched(launch_masked_backward(p, form, CROSS_DKV, s), "masked_bwd_dkv")) return st;
+    if (p.k_parts == 1) return PARTIR_OK;
+    PartSum r = part_sum(2, p.k_parts, Tk, ck);
+    r.part[0] = p.dKpart; r.out[0] = p.dK; r.ld[0] = lddk;
+    r.part[1] = p.dVpart; r.out[1] = p.dV; r.ld[1] = lddv;
+    return launched(launch_part_sum(r, s), "masked_bwd_dkv.sum");
   });
 }
 

@@ -5,7 +5,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <initializer_list>
 
 #include "host_checks.h"
 #include "operators.h"
@@ -27,42 +26,6 @@ int resolve_dropout(Dropout& d, double p, const uint64_t* seed, int64_t row0, in
   d.seed = d.kept == 65536 ? nullptr : seed;
   d.row0 = (uint32_t)row0;
   d.factor = d.kept ? 65536.0f / (float)d.kept : 0.0f;
-  return PARTIR_OK;
-}
-
-struct Matrix {
-  const char* name;
-  const void* p;
-  int64_t rows, cols, ld;
-  int es;
-  int64_t bytes() const { return rows && cols ? ((rows - 1) * ld + cols) * es : 0; }
-};
-
-int check(const Matrix& m) { return check_matrix(m.name, m.p, m.rows, m.cols, m.ld, m.es); }
-
-// Whether two matrices share a byte.  Column blocks of one array lie between one
-// another's rows: with one pitch it is told row for row.
-bool overlap(const Matrix& a, const Matrix& b) {
-  const int64_t na = a.bytes(), nb = b.bytes();
-  if (!na || !nb || !a.p || !b.p) return false;
-  const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p);
-  if (d >= na || -d >= nb) return false;
-  const int64_t pitch = a.ld * a.es;
-  if (pitch != b.ld * b.es || a.rows == 1 || b.rows == 1) return true;
-  // a's row r and b's row r + k are d + k pitch apart
-  for (int64_t k = -d / pitch - 1; k <= -d / pitch + 1; ++k)
-    if (k > -a.rows && k < b.rows && d + k * pitch < a.cols * a.es && -(d + k * pitch) < b.cols * b.es) return true;
-  return false;
-}
-
-bool same(const Matrix& a, const Matrix& b) { return a.p == b.p && a.es == b.es && (a.ld == b.ld || a.rows <= 1); }
-
-// Output o is `in`, or apart from it; and apart from every other matrix.
-int check_apart(const Matrix& o, const Matrix* in, std::initializer_list<const Matrix*> others) {
-  if (in && overlap(o, *in) && !same(o, *in))
-    return fail(PARTIR_E_LAYOUT, "%s must be %s, with its type and leading dim, or apart from it", o.name, in->name);
-  for (const Matrix* m : others)
-    if (m->p && overlap(o, *m)) return fail(PARTIR_E_LAYOUT, "%s overlaps %s", o.name, m->name);
   return PARTIR_OK;
 }
 

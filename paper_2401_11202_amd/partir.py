@@ -46,7 +46,10 @@ EXPORTS = ("partir_loop_matmul", "partir_loop_matmul_workspace", "partir_mlp_blo
            "partir_cross_attention_workspace", "partir_cross_attention_train", "partir_cross_attention_backward",
            "partir_cross_attention_backward_workspace", "partir_plan_cross_attention",
            "partir_plan_cross_attention_backward", "partir_dropout", "partir_residual_norm",
-           "partir_residual_norm_backward", "partir_residual_norm_backward_workspace")
+           "partir_residual_norm_backward", "partir_residual_norm_backward_workspace", "partir_masked_attention",
+           "partir_masked_attention_workspace", "partir_masked_attention_train", "partir_masked_attention_backward",
+           "partir_masked_attention_backward_workspace", "partir_plan_masked_attention",
+           "partir_plan_masked_attention_backward")
 
 
 class PartirError(RuntimeError):
@@ -65,6 +68,11 @@ class PlanInfo(ctypes.Structure):
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "reserved"}
 
 
+class AttentionMask(ctypes.Structure):
+    _fields_ = [("causal", ctypes.c_int), ("cap", ctypes.c_float),
+                *((n, ctypes.c_void_p) for n in ("slopes", "k_lens", "q_lens", "q_starts", "prefix_lens", "q_docs", "k_docs"))]
+
+
 class TraceEntry(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", ctypes.c_int64), ("total_ms", ctypes.c_double)]
 
@@ -75,6 +83,7 @@ _SUM_IMPL = {"auto": SUM_AUTO, "fused": SUM_FUSED, "splitk": SUM_SPLITK}
 I64, I32, P, SZ, F = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
 D = ctypes.c_double
 PP = ctypes.POINTER(ctypes.c_void_p)   # a host array of device pointers
+MP = ctypes.POINTER(AttentionMask)
 ROTARY_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
 
@@ -159,6 +168,13 @@ def lib():
         "partir_residual_norm": (I32, [P] * 7 + [I64] * 8 + [I32, I32, I32, F, D, P, I64, F, P]),
         "partir_residual_norm_backward": (I32, [P] * 12 + [I64] * 10 + [I32, I32, I32, F, D, P, I64, F, P, SZ, P]),
         "partir_residual_norm_backward_workspace": (SZ, [I64, I64, I64]),
+        "partir_masked_attention": (I32, [P] * 4 + [I64] * 10 + [MP, F, P, SZ, P]),
+        "partir_masked_attention_train": (I32, [P] * 5 + [I64] * 10 + [MP, F, P, SZ, P]),
+        "partir_masked_attention_workspace": (SZ, [I64] * 6 + [MP]),
+        "partir_masked_attention_backward": (I32, [P] * 9 + [I64] * 14 + [MP, F, P, SZ, P]),
+        "partir_masked_attention_backward_workspace": (SZ, [I64] * 6 + [MP]),
+        "partir_plan_masked_attention": (I32, [I64] * 6 + [MP, ctypes.POINTER(PlanInfo)]),
+        "partir_plan_masked_attention_backward": (I32, [I64] * 6 + [MP, ctypes.POINTER(PlanInfo)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -1130,6 +1146,125 @@ def _plan_sizes(fn, *args):
     info = PlanInfo()
     _check(fn(*args, ctypes.byref(info)))
     return info.as_dict()
+
+
+def _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal, cap, slopes, k_lens, q_lens, q_starts,
+                 prefix_lens, q_docs, k_docs):
+    """Checked sizes of a masked attention call, its mask and the mask's tensors."""
+    Hk, Tq, Tk, ldq, ldk, ldv = _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens)
+    i32 = _torch.int32
+    _opt(slopes, "slopes", (n_heads,), _torch.float32)
+    _opt(q_lens, "q_lens", (B,), i32)
+    _opt(q_starts, "q_starts", (B,), i32)
+    _opt(prefix_lens, "prefix_lens", (B,), i32)
+    _opt(q_docs, "q_docs", (Tq,), i32)
+    _opt(k_docs, "k_docs", (Tk,), i32)
+    mask = AttentionMask(bool(causal), float(cap), _ptr(slopes), _ptr(k_lens), _ptr(q_lens), _ptr(q_starts), _ptr(prefix_lens),
+                         _ptr(q_docs), _ptr(k_docs))
+    tensors = (("slopes", slopes), ("k_lens", k_lens), ("q_lens", q_lens), ("q_starts", q_starts),
+               ("prefix_lens", prefix_lens), ("q_docs", q_docs), ("k_docs", k_docs))
+    return Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors
+
+
+def masked_attention(Q, K, V, *, B: int, Sq: int, Sk: int, n_heads: int, n_kv_heads: Optional[int] = None,
+                     d_head: int = 128, causal: bool = True, cap: float = 0.0, slopes=None, k_lens=None, q_lens=None,
+                     q_starts=None, prefix_lens=None, q_docs=None, k_docs=None, scale: float = 0.0, out=None,
+                     workspace=None, stream=None):
+    """O = softmax(z) V over the keys that a query sees, per head.  Q [B*Sq, n_heads *
+    d_head], K, V [B*Sk, n_kv_heads * d_head] bf16 (views with a leading dim allowed),
+    n_kv_heads dividing n_heads.  z = scale q k, with cap cap * tanh(z / cap), with
+    slopes [n_heads] f32 less slopes[h] * |p - j| for the query's position p and key
+    j; p = q_starts[b] + s (None: Sk - Sq + s).  A query sees j < k_lens[b] (None: Sk);
+    causal: j <= p or j < prefix_lens[b]; q_docs [B*Sq], k_docs [B*Sk]: keys of its
+    own document.  Queries at and behind q_lens[b], and those that see no key, get 0.
+    All of these int32.  out: O to write into, Q itself allowed."""
+    return _masked_forward(Q, K, V, scale, out, None, False, workspace, stream, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal,
+                           cap, slopes, k_lens, q_lens, q_starts, prefix_lens, q_docs, k_docs)
+
+
+def masked_attention_train(Q, K, V, *, B: int, Sq: int, Sk: int, n_heads: int, n_kv_heads: Optional[int] = None,
+                           d_head: int = 128, causal: bool = True, cap: float = 0.0, slopes=None, k_lens=None, q_lens=None,
+                           q_starts=None, prefix_lens=None, q_docs=None, k_docs=None, scale: float = 0.0, out=None, lse=None,
+                           workspace=None, stream=None):
+    """masked_attention that also returns the base-2 log-sum-exp [B*Sq, n_heads] f32
+    for masked_attention_backward (-inf for a query that gets 0).  Returns (O, lse)."""
+    return _masked_forward(Q, K, V, scale, out, lse, True, workspace, stream, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal,
+                           cap, slopes, k_lens, q_lens, q_starts, prefix_lens, q_docs, k_docs)
+
+
+def _masked_forward(Q, K, V, scale, out, lse, train, workspace, stream, B, Sq, Sk, n_heads, n_kv_heads, d_head, *mask_args):
+    torch = _th()
+    Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors = _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, *mask_args)
+    ldo = n_heads * d_head
+    fresh_o, fresh_l = out is None, train and lse is None
+    if not fresh_o:
+        ldo = _matrix(out, "out", Tq, n_heads * d_head, torch.bfloat16)
+    _opt(lse, "lse", (Tq, n_heads), torch.float32)
+    _same_device(("Q", Q), ("K", K), ("V", V), *tensors, ("out", out), ("lse", lse))
+    dev = Q.device
+    if fresh_o:
+        out = Q.new_empty((Tq, n_heads * d_head))
+    if fresh_l:
+        lse = torch.empty((Tq, n_heads), dtype=torch.float32, device=dev)
+    ws, wsb = _workspace(dev, workspace, lib().partir_masked_attention_workspace, B, Sq, Sk, n_heads, Hk, d_head, mask)
+    _on_stream(stream, ws if workspace is None else None, out if fresh_o else None, lse if fresh_l else None)
+    sizes = (B, Sq, Sk, n_heads, Hk, d_head, ldq, ldk, ldv, ldo, mask, float(scale), _ptr(ws), wsb)
+    if train:
+        _launch(dev, lib().partir_masked_attention_train, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(lse), *sizes, stream=stream)
+        return out, lse
+    _launch(dev, lib().partir_masked_attention, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), *sizes, stream=stream)
+    return out
+
+
+def masked_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, n_heads: int,
+                              n_kv_heads: Optional[int] = None, d_head: int = 128, causal: bool = True, cap: float = 0.0,
+                              slopes=None, k_lens=None, q_lens=None, q_starts=None, prefix_lens=None, q_docs=None,
+                              k_docs=None, scale: float = 0.0, out=None, workspace=None, stream=None):
+    """Gradients (dQ, dK, dV) of masked_attention for the cotangent dO of O, from the
+    forward's O and lse; dK and dV are summed over the query heads of a key head.  The
+    slopes have none.  out: (dQ, dK, dV) to write into."""
+    torch = _th()
+    bf = torch.bfloat16
+    Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors = _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal, cap, slopes,
+                                                            k_lens, q_lens, q_starts, prefix_lens, q_docs, k_docs)
+    cq, ck = n_heads * d_head, Hk * d_head
+    ldo, lddo = _matrix(O, "O", Tq, cq, bf), _matrix(dO, "dO", Tq, cq, bf)
+    _req(lse, "lse", (Tq, n_heads), torch.float32)
+    lds = (cq, ck, ck)
+    fresh = out is None
+    if not fresh:
+        if len(out) != 3:
+            _bad("PARTIR_E_SHAPE", "out must hold (dQ, dK, dV)")
+        lds = (_matrix(out[0], "dQ", Tq, cq, bf), _matrix(out[1], "dK", Tk, ck, bf), _matrix(out[2], "dV", Tk, ck, bf))
+    _same_device(("Q", Q), ("K", K), ("V", V), ("O", O), ("dO", dO), ("lse", lse), *tensors,
+                 *(() if fresh else zip(("dQ", "dK", "dV"), out)))
+    dev = Q.device
+    if fresh:
+        out = (Q.new_empty((Tq, cq)), Q.new_empty((Tk, ck)), Q.new_empty((Tk, ck)))
+    ws, wsb = _workspace(dev, workspace, lib().partir_masked_attention_backward_workspace, B, Sq, Sk, n_heads, Hk, d_head, mask)
+    _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()))
+    _launch(dev, lib().partir_masked_attention_backward, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(lse),
+            _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), B, Sq, Sk, n_heads, Hk, d_head, ldq, ldk, ldv, ldo, lddo, *lds, mask,
+            float(scale), _ptr(ws), wsb, stream=stream)
+    return out
+
+
+def plan_masked_attention(B, Sq, Sk, n_heads, n_kv_heads=None, d_head=128, causal=True, docs=False):
+    return _plan_sizes(lib().partir_plan_masked_attention, B, Sq, Sk, n_heads,
+                       n_heads if n_kv_heads is None else n_kv_heads, d_head, _plan_mask(causal, docs))
+
+
+def plan_masked_attention_backward(B, Sq, Sk, n_heads, n_kv_heads=None, d_head=128, causal=True, docs=False):
+    return _plan_sizes(lib().partir_plan_masked_attention_backward, B, Sq, Sk, n_heads,
+                       n_heads if n_kv_heads is None else n_kv_heads, d_head, _plan_mask(causal, docs))
+
+
+def _plan_mask(causal, docs):
+    """A mask for a plan, which looks at no tensor: only at whether there are documents."""
+    m = AttentionMask(bool(causal))
+    if docs:
+        m.q_docs = m.k_docs = 16
+    return m
 
 
 def _rows(t, name, rows, cols):
