@@ -4,13 +4,13 @@
 // F, the form of a kernel: 0 attention to another sequence (every key below the
 // sequence's length), else kMasked, with kCap and kBias as the call has them.
 //
-// Position p = q_start + s of query s of a sequence, key j.  It sees
-//   j < lim = min(k_len, causal ? max(p + 1, prefix) : k_len)
-// of its own document.  lim does not fall from a row to the next, so that a tile's
-// first row tells whether a block of keys needs the comparison at all, and its last
-// row whether the block is seen.  Documents are arbitrary numbers: a table of the
-// least and largest of every 64 positions tells which blocks can hold a row's;
-// where documents are contiguous, as in packed rows, that leaves the blocks that do.
+// A query sees the keys of an interval [lo, lim): position p = q_start + s sees
+//   j < min(k_len, causal ? max(p + 1, prefix) : k_len),
+// and where there are documents those of its own, a run of keys that a launch
+// before has found (doc_rows_kernel).  So masks are two comparisons, which a block
+// of keys needs only where it crosses an end of a row's interval; blocks outside of
+// every row's are not read.  Documents that lie in pieces have no interval: their
+// sequence's keys are compared by number (by_id).
 #pragma once
 #include "attention_tiles.h"
 #include "operators.h"
@@ -18,17 +18,16 @@
 namespace partir {
 
 constexpr int kMasked = 1, kCap = 2, kBias = 4;
+constexpr int kNowhere = 2147483647;   // lo of a row that sees no key
 
-// What a kernel of form F takes.
+// What the forward kernel of form F takes.
 template <int F>
 struct FormParams {
   typedef MaskedParams fwd;
-  typedef MaskedBwdParams bwd;
 };
 template <>
 struct FormParams<0> {
   typedef CrossParams fwd;
-  typedef CrossBwdParams bwd;
 };
 
 __device__ __forceinline__ int clamp_len(const int32_t* lens, int b, int most) {
@@ -46,68 +45,73 @@ struct SeqMask {
     prefix = p.mask.prefix ? min(max(p.mask.prefix[b], 0), klen) : 0;
     causal = p.mask.causal;
   }
+  // end of what query s may see, documents aside; it does not fall with s
   __device__ __forceinline__ int lim(int s) const {
     return causal ? min(max(start + s + 1, prefix), klen) : klen;   // s < 2^30
   }
 };
 
-struct IntRange {
-  int lo, hi;
+// The keys [begin, end) that queries s0 .. s1 (below q_len) of a sequence may see,
+// from a multiple of 64 on.
+template <typename P>
+__device__ __forceinline__ int2 key_range(const P& p, const SeqMask& m, int b, int s0, int s1) {
+  int lo = 0, hi = m.lim(s1);
+  if (p.mask.rows) {
+    const int2* blocks = p.mask.blocks + (int64_t)b * p.mask.q_blocks;
+    int from = kNowhere, to = 0;
+    for (int i = s0 >> 6; i <= s1 >> 6; ++i) {
+      const int2 e = blocks[i];
+      from = min(from, e.x);
+      to = max(to, e.y);
+    }
+    lo = from == kNowhere ? 0 : from & ~63;
+    hi = min(hi, to);
+  }
+  return make_int2(lo, max(lo, hi));
+}
+
+// A lane's row of a wave's 32 (lane & 31), and what they have in common.
+struct RowMask {
+  int lo, lim;               // this lane's row sees [lo, lim); none: [kNowhere, 0)
+  int lo0, lo1, lim0, lim1;  // least and largest of the wave's
+  int pos;                   // the row's position
+  template <typename P>
+  __device__ __forceinline__ RowMask(const P& p, const SeqMask& m, int64_t tq, int s) {
+    pos = m.start + s;
+    lo = 0;
+    lim = s < m.qlen ? m.lim(s) : 0;
+    if (!p.mask.rows) {      // the rows ascend, and so do their limits
+      if (lim <= 0) lo = kNowhere;
+      lo0 = 0;
+      lo1 = __builtin_amdgcn_readlane(lo, 0);
+      lim0 = __builtin_amdgcn_readlane(lim, 0);
+      lim1 = __builtin_amdgcn_readlane(lim, 31);
+      return;
+    }
+    const int2 e = p.mask.rows[tq];
+    lo = e.x;
+    lim = min(lim, e.y);
+    if (lim <= lo) {
+      lo = kNowhere;
+      lim = 0;
+    }
+    int a = lo, b = lo, c = lim, d = lim;
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+      a = min(a, __shfl_xor(a, o));
+      b = max(b, __shfl_xor(b, o));
+      c = min(c, __shfl_xor(c, o));
+      d = max(d, __shfl_xor(d, o));
+    }
+    lo0 = __builtin_amdgcn_readfirstlane(a);
+    lo1 = __builtin_amdgcn_readfirstlane(b);
+    lim0 = __builtin_amdgcn_readfirstlane(c);
+    lim1 = __builtin_amdgcn_readfirstlane(d);
+  }
+  // whether no row of the wave sees any of n keys from key0 on; and whether all rows see all of them
+  __device__ __forceinline__ bool none(int key0, int n) const { return key0 >= lim1 || key0 + n <= lo0; }
+  __device__ __forceinline__ bool all(int key0, int n) const { return key0 >= lo1 && key0 + n <= lim0; }
 };
-
-// The least and largest document of positions [s0, s1] of a sequence, by its table.
-__device__ __forceinline__ IntRange doc_span(const int2* table, int s0, int s1) {
-  IntRange r = {2147483647, -2147483647 - 1};
-  for (int i = s0 >> 6; i <= s1 >> 6; ++i) {
-    const int2 e = table[i];
-    r.lo = min(r.lo, e.x);
-    r.hi = max(r.hi, e.y);
-  }
-  return r;
-}
-
-// The positions [lo, hi) within [from, to) (from a multiple of 64) whose blocks may
-// hold a document of `docs`; {from, from} if none does.  Every lane of the wave.
-__device__ __forceinline__ IntRange doc_range(const int2* table, IntRange docs, int from, int to, int lane) {
-  int lo = -1, hi = -1;
-  for (int i0 = from >> 6; 64 * i0 < to; i0 += 64) {
-    const int i = i0 + lane;
-    bool in = 64 * i < to;
-    if (in) {
-      const int2 e = table[i];
-      in = e.x <= docs.hi && e.y >= docs.lo;
-    }
-    const uint64_t any = __builtin_amdgcn_ballot_w64(in);
-    if (any) {
-      if (lo < 0) lo = i0 + __builtin_ctzll(any);
-      hi = i0 + 63 - __builtin_clzll(any);
-    }
-  }
-  if (lo < 0) return {from, from};
-  return {64 * lo, min(to, 64 * hi + 64)};
-}
-
-// A run [lo, hi) of positions within [from, to) whose blocks hold document `doc`
-// alone: the first such run.
-__device__ __forceinline__ IntRange doc_run(const int2* table, int doc, int from, int to, int lane) {
-  int lo = -1;
-  for (int i0 = from >> 6; 64 * i0 < to; i0 += 64) {
-    const int i = i0 + lane;
-    bool full = 64 * i < to;
-    if (full) {
-      const int2 e = table[i];
-      full = e.x == doc && e.y == doc;
-    }
-    uint64_t yes = __builtin_amdgcn_ballot_w64(full);
-    if (lo < 0) {
-      if (!yes) continue;
-      lo = i0 + __builtin_ctzll(yes);
-      yes |= ((uint64_t)1 << (lo - i0)) - 1;   // those before it do not end the run
-    }
-    if (~yes) return {64 * lo, 64 * (i0 + __builtin_ctzll(~yes))};
-  }
-  return lo < 0 ? IntRange{0, 0} : IntRange{64 * lo, to};
-}
 
 // Score s = q k, in units of log2: z = cap tanh(scale s / cap) log2 e with
 // tanh x = 1 - 2 / (1 + e^(2x)); r = 1 / (1 + e^(2x)) gives its derivative too,

@@ -29,11 +29,316 @@
 // units are busy 58 and 49 % of the time; in dkv on three quarters of the compute
 // units only, as a workgroup behind its sequence's end has nothing to do.
 #include <algorithm>
+#include <type_traits>
 
-#include "cross_attention_bwd_kernels.h"
+#include "attention_row_tiles.h"
 
 namespace partir {
 namespace {
+
+__device__ __forceinline__ int key_count(const CrossBwdParams& p, int b) {
+  return p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
+}
+
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void cross_bwd_dq_kernel(CrossBwdParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+
+  const int R = p.G * p.Sq;
+  int qb, bh, part = 0;
+  if (p.q_parts == 1 && (p.by_nbh.d & 7) == 0) {
+    // as in the forward pass an XCD takes one (sequence, key head) after the other,
+    // whose K and V stay in its L2 (four at a time in its 4 MiB: 818 MB read and
+    // 700 us at 4 x 4096 queries over 2048 keys, 32 / 8 heads; 535 MB and 640 us so)
+    const int j = blockIdx.x >> 3, n = p.by_nqb.quot(j);
+    bh = n * 8 + (blockIdx.x & 7);
+    qb = p.by_nqb.rem(j, n);
+  } else {
+    const int rest = p.by_nbh.quot(blockIdx.x);
+    bh = p.by_nbh.rem(blockIdx.x, rest);
+    qb = p.by_q_parts.quot(rest);
+    part = p.by_q_parts.rem(rest, qb);
+  }
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
+  const int i = qb * 128 + 32 * w + col;
+  const int ic = min(i, R - 1), sq = p.by_g.quot(ic);
+  const int64_t tq = (int64_t)b * p.Sq + sq;
+  const int head = kvh * p.G + p.by_g.rem(ic, sq);
+
+  // Q and dO of this lane's row (B operands), D = rowsum(dO * O)
+  bf16x8 qf[8], gf[8];
+  float dsum = 0.0f;
+  {
+    const uint16_t* qrow = p.Q + tq * p.ldq + head * DH + 8 * h;
+    const uint16_t* grow = p.dO + tq * p.ldg + head * DH + 8 * h;
+    const uint16_t* orow = p.O + tq * p.ldo + head * DH + 8 * h;
+#pragma unroll
+    for (int ds = 0; ds < 8; ++ds) {
+      qf[ds] = *(const bf16x8*)(qrow + 16 * ds);
+      gf[ds] = *(const bf16x8*)(grow + 16 * ds);
+      const bf16x8 of = *(const bf16x8*)(orow + 16 * ds);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dsum += (float)gf[ds][e] * (float)of[e];
+    }
+  }
+  const float lse = p.lse[tq * p.Hq + head];
+  const int len = key_count(p, b);
+  const CrossRange range = cross_range(len, p.by_q_parts, part);
+  TileTr tr;
+  tr.init(lane);
+  const float c = p.scale_log2;
+  if (len <= 256) {
+    // With few keys O's rounding to bf16 would be of the size of the others in
+    // D: up to four tiles more give it as sum_j P_j dP_j.  (The error of dQ at 129
+    // keys, in roundings of the result alone: 1.51 from O, 1.45 so.)
+    dsum = 0.0f;
+    for (int key = 0; key < len; key += TR) {
+      const int64_t tk = (int64_t)b * p.Sk + key;
+      tile_load<TR, 4>(p.K + tk * p.ldk + kvh * DH, p.ldk, min(TR, len - key), smem, w, lane);
+      tile_load<TR, 4>(p.V + tk * p.ldv + kvh * DH, p.ldv, min(TR, len - key), smem + TILE, w, lane);
+      WAIT_VMCNT(0);
+      __syncthreads();
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        f32x16 s, dp;
+        zero(s);
+        zero(dp);
+#pragma unroll
+        for (int ds = 0; ds < 8; ++ds) {
+          s = mfma(tile_rows(smem, 32 * t, col, h, ds), qf[ds], s);
+          dp = mfma(tile_rows(smem + TILE, 32 * t, col, h, ds), gf[ds], dp);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (key + 32 * t + 8 * (v >> 2) + 4 * h + (v & 3) < len)
+            dsum += __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse)) * dp[v];
+      }
+      __syncthreads();
+    }
+  }
+  const float Dq = dsum + __shfl_xor(dsum, 32);
+  if (part == 0 && h == 0 && i < R) p.Dstat[tq * p.Hq + head] = Dq;
+
+  const uint16_t* kbase = p.K + ((int64_t)b * p.Sk + range.begin) * p.ldk + kvh * DH;
+  const uint16_t* vbase = p.V + ((int64_t)b * p.Sk + range.begin) * p.ldv + kvh * DH;
+  const int nkeys = range.end - range.begin, nkb = (nkeys + TR - 1) / TR;
+  auto gload = [&](int kb, int buf) {
+    char* t = smem + buf * 2 * TILE;
+    const int rows = min(TR, nkeys - kb * TR);
+    tile_load<TR, 4>(kbase + (int64_t)kb * TR * p.ldk, p.ldk, rows, t, w, lane);
+    tile_load<TR, 4>(vbase + (int64_t)kb * TR * p.ldv, p.ldv, rows, t + TILE, w, lane);
+  };
+  f32x16 dq[4], nD;   // dP starts at -D: its first product reads it, where a subtraction would follow
+#pragma unroll
+  for (int d = 0; d < 4; ++d) zero(dq[d]);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) nD[v] = -Dq;
+  auto iter = [&](int kb, auto stage) {
+    constexpr int cur = decltype(stage)::value;
+    if (kb + 1 < nkb) gload(kb + 1, cur ^ 1);
+    const char* ks = smem + cur * 2 * TILE;
+    const char* vs = ks + TILE;
+    const int left = nkeys - kb * TR;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 s, dp = nD;
+      zero(s);
+#pragma unroll
+      for (int ds = 0; ds < 8; ++ds) {
+        s = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], s);
+        dp = mfma(tile_rows(vs, 32 * t, col, h, ds), gf[ds], dp);
+      }
+      float pr[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) pr[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse));
+      if (left < 32 * t + 32) {   // keys past the end
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= left) pr[v] = 0.0f;
+      }
+      bf16x8 dsf[2];
+#pragma unroll
+      for (int v = 0; v < 16; v += 2)
+        put2(dsf[v >> 3], v & 7, pr[v] * dp[v], pr[v + 1] * dp[v + 1]);
+#pragma unroll
+      for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) dq[d] = mfma(tr.read(ks, 2 * t + uu, d), dsf[uu], dq[d]);
+    }
+    WAIT_VMCNT(0);
+    __syncthreads();
+  };
+  if (nkb > 0) gload(0, 0);
+  WAIT_VMCNT(0);
+  __syncthreads();
+  for (int kb = 0; kb < nkb; kb += 2) {
+    iter(kb, std::integral_constant<int, 0>{});
+    if (kb + 1 < nkb) iter(kb + 1, std::integral_constant<int, 1>{});
+  }
+  const int rows = R - qb * 128 - 32 * w;
+  if (p.q_parts > 1)
+    store(smem, w, p.dQpart, (((int64_t)part * p.B * p.Sq + tq) * p.Hq + head) * DH, rows, dq, p.scale, lane);
+  else
+    store(smem, w, p.dQ, tq * p.lddq + head * DH, rows, dq, p.scale, lane);
+}
+
+// dK and dV: eight waves of 32 keys, K as an operand in registers, V in LDS (both
+// as registers would leave one wave a SIMD); rows in tiles of 64.  Per 32 rows a
+// wave forms S and P, dP, dV^T += dO^T P, then dS and dK^T += Q^T dS.  One pass for
+// both gradients forms S, P and dP once, 4 products where a pass for each takes
+// 5, and three quarters of their time at the size above.  Two scheduling barriers keep phases
+// apart where the compiler would otherwise hold the operands of several at once;
+// one at every phase costs their overlap (24 % more).  Eight registers (nine
+// without EVEN) are spilled still, addresses of the tiles' loads and of the
+// statistics, of which a tile reads four or five back.
+template <bool EVEN>
+__global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams p) {
+  constexpr int STAGES = 0, VT = 2 * 2 * TILE, STAT = VT + 256 * ROWB;
+  // one object: with several, the compiler tells them apart, takes every tile
+  // read for one of the tiles being loaded and waits for those
+  __shared__ __attribute__((aligned(1024))) char smem[STAT + 2 * 2 * TR * 4];
+  static_assert(8 * row_area<4, __bf16>() <= STAT && 8 * row_area<2, float>() <= STAT, "the end goes through the stages and V");
+  float (*const stat)[2][TR] = (float (*)[2][TR])(smem + STAT);   // [stage][-lse / c, -D][row]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, col = lane & 31;
+
+  const int rest = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, rest);
+  const int kblk = p.by_k_parts.quot(rest), part = p.by_k_parts.rem(rest, kblk);
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
+  const int len = key_count(p, b), R = p.G * p.Sq;
+  const int k0 = kblk * 256, kw = k0 + 32 * w;       // the workgroup's first key, the wave's
+  const int kj = kw + col;                           // this lane's
+  const int64_t tk = (int64_t)b * p.Sk + kj;
+
+  f32x16 dk[4], dv[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    zero(dk[d]);
+    zero(dv[d]);
+  }
+  // workgroup-uniform: keys behind len_b get zeros
+  if (k0 < len) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {   // 256 rows of 2^24 values are more than a descriptor spans
+      const int64_t t0 = (int64_t)b * p.Sk + k0 + 128 * half;
+      tile_load<128, 8>(p.V + t0 * p.ldv + kvh * DH, p.ldv, min(128, len - k0 - 128 * half), smem + VT + 128 * half * ROWB, w,
+                        lane);
+    }
+    bf16x8 kf[8];
+    {
+      const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, len - 1)) * p.ldk + kvh * DH + 8 * h;
+#pragma unroll
+      for (int ds = 0; ds < 8; ++ds) kf[ds] = *(const bf16x8*)(krow + 16 * ds);
+    }
+    const int tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
+    const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
+    const RowTiles<EVEN, 8> rt(p, b, kvh, p.G * p.Sq, w, lane);
+    const float inv_c = 1.0f / p.scale_log2;
+    float st_l = 0.0f, st_d = 0.0f;
+    auto gload = [&](int it, int buf) {
+      rt.load(it, smem + STAGES + buf * 2 * TILE);
+      if (tid < TR) {
+        // nothing looks at the loaded values before sstore: a use here would wait
+        // for the tiles' loads too
+        const int i = min(it * TR + tid, R - 1), sq = p.by_g.quot(i);
+        const int64_t at = ((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq);
+        st_l = p.lse[at];
+        st_d = p.Dstat[at];
+      }
+    };
+    auto sstore = [&](int it, int buf) {
+      if (tid < TR) {
+        const bool row = it * TR + tid < R;   // a missing row: P = 2^-inf
+        lds_write((char*)&stat[buf][0][tid], row ? -st_l * inv_c : -__builtin_inff());
+        lds_write((char*)&stat[buf][1][tid], row ? -st_d : 0.0f);
+      }
+    };
+    TileTr tr;
+    tr.init(lane);
+    const float c = p.scale_log2;
+    auto iter = [&](int it, auto stage) {
+      constexpr int cur = decltype(stage)::value;
+      if (it + 1 < it1) gload(it + 1, cur ^ 1);
+      const char* qs = smem + STAGES + cur * 2 * TILE;
+      const char* gs = qs + TILE;
+      if (kw < len) {   // wave-uniform
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t) {
+          // the accumulators start at -lse / c and -D of their rows
+          auto start = [&](f32x16& x, int which) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 v = lds_read<f32x4>((const char*)&stat[cur][which][32 * t + 8 * q + 4 * h]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[4 * q + j] = v[j];
+            }
+          };
+          f32x16 s;
+          start(s, 0);
+#pragma unroll
+          for (int ds = 0; ds < 8; ++ds) s = mfma(tile_rows(qs, 32 * t, col, h, ds), kf[ds], s);
+          __builtin_amdgcn_sched_barrier(0);
+          bf16x8 pf[2];
+#pragma unroll
+          for (int v = 0; v < 16; v += 2) {
+            s[v] = __builtin_amdgcn_exp2f(s[v] * c);
+            s[v + 1] = __builtin_amdgcn_exp2f(s[v + 1] * c);
+            put2(pf[v >> 3], v & 7, s[v], s[v + 1]);
+          }
+          f32x16 dp;
+          start(dp, 1);
+#pragma unroll
+          for (int ds = 0; ds < 8; ++ds)
+            dp = mfma(tile_rows(gs, 32 * t, col, h, ds), tile_rows(smem + VT, 32 * w, col, h, ds), dp);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * t + uu, d), pf[uu], dv[d]);
+#pragma unroll
+          for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[v] * dp[v], s[v + 1] * dp[v + 1]);
+#pragma unroll
+          for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, 2 * t + uu, d), pf[uu], dk[d]);
+        }
+      }
+      if (it + 1 < it1) sstore(it + 1, cur ^ 1);
+      WAIT_VMCNT(0);
+      __syncthreads();
+    };
+    if (it0 < it1) {
+      gload(it0, 0);
+      sstore(it0, 0);
+    }
+    WAIT_VMCNT(0);
+    __syncthreads();
+    for (int it = it0; it < it1; it += 2) {
+      iter(it, std::integral_constant<int, 0>{});
+      if (it + 1 < it1) iter(it + 1, std::integral_constant<int, 1>{});
+    }
+    if (kj >= len) {   // a lane's key is its own column: what its sums hold goes nowhere else
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        zero(dk[d]);
+        zero(dv[d]);
+      }
+    }
+  }
+  const int rows = p.Sk - kw;
+  if (p.k_parts > 1) {
+    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH;
+    store(smem, w, p.dKpart, at, rows, dk, p.scale, lane);
+    store(smem, w, p.dVpart, at, rows, dv, 1.0f, lane);
+  } else {
+    store(smem, w, p.dK, tk * p.lddk + kvh * DH, rows, dk, p.scale, lane);
+    store(smem, w, p.dV, tk * p.lddv + kvh * DH, rows, dv, 1.0f, lane);
+  }
+}
 
 // All three gradients in one pass where a sequence has at most 128 keys: S and
 // dP are formed once (5 products instead of 8), and D = sum_j P_j dP_j comes
@@ -72,13 +377,13 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdP
   const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
   const int R = p.G * p.Sq, tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
   const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
-  const int len = clamp_len(p.lens, b, p.Sk);
+  const int len = key_count(p, b);
 
   // K for good, V through the first stage (rows behind len are zeros)
   const int64_t tk0 = (int64_t)b * p.Sk;
   tile_load<128, 8>(p.K + tk0 * p.ldk + kvh * DH, p.ldk, len, smem + KT, w, lane);
   tile_load<128, 8>(p.V + tk0 * p.ldv + kvh * DH, p.ldv, len, smem + STAGES, w, lane);
-  const RowTiles<EVEN, 8> rt(p, b, kvh, R, w, lane);
+  const RowTiles<EVEN, 8> rt(p, b, kvh, p.G * p.Sq, w, lane);
   TileTr tr;
   tr.init(lane);
   WAIT_VMCNT(0);
@@ -224,7 +529,7 @@ constexpr int64_t kCUs = 256;
 
 }  // namespace
 
-CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, bool may_one_pass) {
+CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk) {
   // A tile of 64 streamed rows takes a workgroup 2.8 us in the one pass, 1.45 us in
   // dq and 3 us in dkv; 1000 rows of a part cost 0.15 us.  One part / these: 2 x 4096
   // queries over 77 keys, 8 heads 187 / 30 us; 200 queries over 2048 keys, 4 heads
@@ -234,7 +539,7 @@ CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, i
   auto most = [](int64_t grid, int64_t tiles) { return grid > 0 ? std::min(kCUs / grid, tiles) : 1; };
   const double q_us = 1.5e-4 * (double)(B * Sq * Hq), k_us = 2 * 1.5e-4 * (double)(B * Sk * Hk);
   // without keys the dq pass alone runs, and writes zeros
-  if (may_one_pass && Sk > 0 && Sk <= 128) return {true, 1, best_parts(most(B * Hk, rows), rows, 2.8, k_us)};
+  if (Sk > 0 && Sk <= 128) return {true, 1, best_parts(most(B * Hk, rows), rows, 2.8, k_us)};
   return {false, best_parts(most(B * Hk * ((R + 127) / 128), keys), keys, 1.45, q_us),
           best_parts(most(B * Hk * ((Sk + 255) / 256), rows), rows, 3.0, k_us)};
 }
@@ -244,13 +549,13 @@ hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hip
   const bool even = 16 % p.G == 0;
   if (pass == CROSS_DQ) {
     const int64_t blocks = ((int64_t)p.G * p.Sq + 127) / 128;
-    hipLaunchKernelGGL(cross_bwd_dq_kernel<0>, dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
+    hipLaunchKernelGGL(cross_bwd_dq_kernel, dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
   } else if (pass == CROSS_ALL) {
     hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>,
                        dim3((unsigned)(nbh * p.k_parts)), dim3(2 * NT), 0, s, p);
   } else {
     const int64_t blocks = ((int64_t)p.Sk + 255) / 256;
-    hipLaunchKernelGGL((even ? cross_bwd_dkv_kernel<true, 0> : cross_bwd_dkv_kernel<false, 0>),
+    hipLaunchKernelGGL(even ? cross_bwd_dkv_kernel<true> : cross_bwd_dkv_kernel<false>,
                        dim3((unsigned)(blocks * nbh * p.k_parts)), dim3(2 * NT), 0, s, p);
   }
   return hipGetLastError();

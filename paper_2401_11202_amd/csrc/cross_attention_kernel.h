@@ -75,35 +75,25 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
     for (int ds = 0; ds < 8; ++ds) qf[ds] = *(const bf16x8*)(qrow + 16 * ds);
   }
   CrossRange range;
-  // masked: the keys that this lane's row sees end at lim (lim0, lim1: of the wave's
-  // first and last row), and blocks within [full.lo, full.hi) need no look at documents
-  int lim = 0, lim0 = 0, lim1 = 0, pos = 0, doc = 0;
-  IntRange full = {0, 2147483647};
-  float slope = 0.0f;
   if constexpr (F == 0) {
     range = cross_range(clamp_len(p.lens, b, p.Sk), p.by_split, split);
     if (p.nsplit > 1 && split >= range.parts) return;   // the combine does not read it
-  } else {
-    const SeqMask m(p, b);
-    pos = m.start + sq;
-    lim = m.lim(sq);
-    lim0 = __builtin_amdgcn_readlane(lim, 0);
-    lim1 = __builtin_amdgcn_readlane(lim, 31);
-    const int r0 = min(qb * 32 * QW, last), r1 = min(qb * 32 * QW + 32 * QW - 1, last);   // the workgroup's rows
-    const int s0 = p.by_g.quot(r0), s1 = p.by_g.quot(r1);
-    IntRange keys = {0, max(m.qlen > 0 && qb * 32 * QW <= last ? m.lim(s1) : 0, 0)};
-    if (p.mask.k_docs) {
-      const int2* table = p.mask.k_table + (int64_t)b * p.mask.k_blocks;
-      doc = p.mask.q_docs[tq];
-      keys = doc_range(table, doc_span(p.mask.q_table + (int64_t)b * p.mask.q_blocks, s0, s1), 0, keys.hi, lane);
-      const int first = __builtin_amdgcn_readfirstlane(doc);
-      full = __builtin_amdgcn_ballot_w64(doc != first) == 0 ? doc_run(table, first, keys.lo, keys.hi, lane) : IntRange{0, 0};
-    }
-    range = cross_range(keys.hi - keys.lo, p.by_split, split);
-    range.begin += keys.lo;
-    range.end += keys.lo;
-    if constexpr ((F & kBias) != 0) slope = p.mask.slopes[head] * 1.4426950408889634f;
   }
+  const auto mask = [&] {
+    if constexpr (F == 0)
+      return 0;
+    else {
+      const SeqMask m(p, b);
+      const int r0 = qb * 32 * QW, r1 = min(r0 + 32 * QW - 1, last);   // the workgroup's rows
+      const int2 keys = r0 <= last && m.qlen > 0 ? key_range(p, m, b, p.by_g.quot(r0), p.by_g.quot(r1)) : make_int2(0, 0);
+      range = cross_range(keys.y - keys.x, p.by_split, split);
+      range.begin += keys.x;
+      range.end += keys.x;
+      return RowMask(p, m, tq, sq);
+    }
+  }();
+  float slope = 0.0f;
+  if constexpr ((F & kBias) != 0) slope = p.mask.slopes[head] * 1.4426950408889634f;
 
   const uint16_t* kbase = p.K + (int64_t)b * p.Sk * p.ldk + kvh * DH;
   const uint16_t* vbase = p.V + (int64_t)b * p.Sk * p.ldv + kvh * DH;
@@ -159,7 +149,9 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
     }
     if (!ALONE && KG > 1 && kb >= nkb) return;
     const int key0 = range.begin + kb * BKV;
-    if (F != 0 && !ALONE && key0 >= lim1) return;   // no row of the wave sees the block
+    if constexpr (F != 0 && !ALONE) {
+      if (mask.none(key0, BKV)) return;
+    }
     const char* ks = stages + cur * STAGE;
     const char* vs = ks + T_BYTES;
     __builtin_amdgcn_s_setprio(1);
@@ -179,7 +171,7 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr ((F & (kCap | kBias)) != 0) {
-      const float far = (float)(pos - key0 - 4 * h);
+      const float far = (float)(mask.pos - key0 - 4 * h);
 #pragma unroll
       for (int t = 0; t < NSUB; ++t)
 #pragma unroll
@@ -192,23 +184,25 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
             sacc[t][v] = __builtin_fmaf(-slope, __builtin_fabsf(far - (float)(32 * t + 8 * (v >> 2) + (v & 3))), sacc[t][v]);
         }
     }
-    int left = range.end - key0;   // keys from this block on
+    const int left = range.end - key0;   // keys from this block on
     if constexpr (F != 0) {
-      if (key0 < full.lo || key0 + BKV > full.hi) {   // a border of documents
+      if (!mask.all(key0, BKV)) {
+        // [lo, lim) of the row, in keys from this lane's first of the block on
+        const uint32_t lo = (uint32_t)(mask.lo - key0 - 4 * h), len = (uint32_t)max(mask.lim - mask.lo, 0);
+#pragma unroll
+        for (int t = 0; t < NSUB; ++t)
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if ((uint32_t)(32 * t + 8 * (v >> 2) + (v & 3)) - lo >= len) sacc[t][v] = -__builtin_inff();
+      }
+      if (p.mask.rows && p.mask.by_id[b]) {
         const int32_t* ids = p.mask.k_docs + (int64_t)b * p.Sk;
+        const int doc = p.mask.q_docs[tq];
 #pragma unroll
         for (int t = 0; t < NSUB; ++t)
 #pragma unroll
           for (int v = 0; v < 16; ++v)
             if (ids[min(key0 + 32 * t + 8 * (v >> 2) + 4 * h + (v & 3), p.Sk - 1)] != doc) sacc[t][v] = -__builtin_inff();
-      }
-      if (key0 + BKV > lim0 || left < BKV) {
-        left = min(left, lim - key0);
-#pragma unroll
-        for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (32 * t + 8 * (v >> 2) + 4 * h + (v & 3) >= left) sacc[t][v] = -__builtin_inff();
       }
     } else if (left < BKV) {
 #pragma unroll

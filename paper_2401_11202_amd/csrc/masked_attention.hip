@@ -4,7 +4,7 @@
 // kernel is that of attention to another sequence (cross_attention_kernel.h) in its
 // masked forms: a workgroup takes the keys from the first to the last block that a
 // row of it may see, a wave passes blocks that none of its rows sees, and only
-// blocks across a limit or a border of documents compare keys one by one.
+// blocks across an end of some row's interval compare keys one by one.
 #include <algorithm>
 
 #include "cross_attention_kernel.h"
@@ -50,22 +50,87 @@ __global__ __launch_bounds__(256) void masked_combine_kernel(MaskedParams p) {
       bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
 }
 
-// The least and largest document of every 64 valid positions of a sequence: a wave
-// a block.  A block without valid positions meets none.
-__global__ __launch_bounds__(256) void doc_table_kernel(DocTables t) {
-  const int which = blockIdx.y, lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int blocks = t.blocks[which];
-  if (n >= (int64_t)t.B * blocks) return;
-  const int b = (int)(n / blocks), s = (int)(n - (int64_t)b * blocks) * 64 + lane;
-  int lo = 2147483647, hi = -2147483647 - 1;
-  if (s < clamp_len(t.lens[which], b, t.S[which])) lo = hi = t.docs[which][(int64_t)b * t.S[which] + s];
+// The keys of every query's document.  A workgroup takes 1024 queries of a sequence:
+// it lists the runs of equal numbers of the sequence's valid keys, and where no
+// number has two runs, and there are at most kRuns, a query's keys are the run of
+// its number.  The run at the query's own position is looked at first, which is the
+// one where queries and keys are the same tokens.
+constexpr int kRuns = 4096, kDocThreads = 1024;
+__global__ __launch_bounds__(kDocThreads) void doc_rows_kernel(DocRows t) {
+  __shared__ __attribute__((aligned(16))) int id[kRuns];
+  __shared__ int first[kRuns + 1];
+  __shared__ int wave_sum[17];
+  __shared__ int in_pieces;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int chunks = (t.Sq + kDocThreads - 1) / kDocThreads, b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
+  const int klen = clamp_len(t.k_lens, b, t.Sk), qlen = clamp_len(t.q_lens, b, t.Sq);
+  const int32_t* kd = t.k_docs + (int64_t)b * t.Sk;
+  // starts of runs among this thread's keys, and how many lie before them
+  const int per = (klen + kDocThreads - 1) / kDocThreads;
+  const int j0 = min(tid * per, klen), j1 = min(j0 + per, klen);
+  int count = 0;
+  for (int j = j0; j < j1; ++j) count += j == 0 || kd[j] != kd[j - 1];
+  int before = count;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(before, o);
+    if (lane >= o) before += x;
+  }
+  if (lane == 63) wave_sum[wave] = before;
+  if (tid == 0) in_pieces = 0;
+  __syncthreads();
+  int runs = 0, base = 0;
+  for (int w = 0; w < kDocThreads / 64; ++w) {
+    if (w == wave) base = runs;
+    runs += wave_sum[w];
+  }
+  before += base - count;
+  const bool listed = runs <= kRuns;   // the same in every thread
+  if (listed) {
+    for (int j = j0; j < j1; ++j)
+      if (j == 0 || kd[j] != kd[j - 1]) {
+        id[before] = kd[j];
+        first[before++] = j;
+      }
+    if (tid == 0) first[runs] = klen;
+    __syncthreads();
+    for (int r = tid; r < runs; r += kDocThreads) {
+      const int mine = id[r];
+      bool twice = false;
+      for (int k = 0; k < runs; ++k) twice |= id[k] == mine && k != r;
+      if (twice) in_pieces = 1;
+    }
+  } else if (tid == 0) {
+    in_pieces = 1;
+  }
+  __syncthreads();
+  const bool by_id = in_pieces != 0;
+  if (chunk == 0 && tid == 0) t.by_id[b] = by_id;
+  const int s = chunk * kDocThreads + tid;
+  int2 e = make_int2(0, 0);
+  if (s < qlen) {
+    if (by_id) {
+      e = make_int2(0, klen);
+    } else if (runs > 0) {
+      const int mine = t.q_docs[(int64_t)b * t.Sq + s];
+      int a = 0, z = runs;             // the run that holds position s, if any does
+      while (z - a > 1) {
+        const int mid = (a + z) >> 1;
+        (first[mid] <= s ? a : z) = mid;
+      }
+      if (id[a] != mine)
+        for (a = 0; a < runs && id[a] != mine; ++a) {}
+      if (a < runs) e = make_int2(first[a], first[a + 1]);
+    }
+  }
+  if (s < t.Sq) t.rows[(int64_t)b * t.Sq + s] = e;
+  int lo = e.y > e.x ? e.x : kNowhere, hi = e.y;
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     lo = min(lo, __shfl_xor(lo, o));
     hi = max(hi, __shfl_xor(hi, o));
   }
-  if (lane == 0) t.table[which][n] = make_int2(lo, hi);
+  if (lane == 0 && s < t.Sq) t.blocks[(int64_t)b * t.q_blocks + (s >> 6)] = make_int2(lo, hi);
 }
 
 template <int F>
@@ -98,9 +163,9 @@ hipError_t launch_masked_combine(const MaskedParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_doc_tables(const DocTables& t, hipStream_t s) {
-  const int64_t most = (int64_t)t.B * std::max(t.blocks[0], t.blocks[1]);
-  hipLaunchKernelGGL(doc_table_kernel, dim3((unsigned)((most + 3) / 4), 2), dim3(256), 0, s, t);
+hipError_t launch_doc_rows(const DocRows& t, hipStream_t s) {
+  const int64_t chunks = ((int64_t)t.Sq + kDocThreads - 1) / kDocThreads;
+  hipLaunchKernelGGL(doc_rows_kernel, dim3((unsigned)(chunks * t.B)), dim3(kDocThreads), 0, s, t);
   return hipGetLastError();
 }
 

@@ -1,31 +1,520 @@
-// Gradients of masked attention: the two passes of cross_attention_bwd_kernels.h
-// in their masked forms.  With t = tanh(scale q k / cap), P = 2^(z - lse):
-//   dS = P (dP - D) (1 - t^2)   (without a cap the last factor is 1)
-// and the rest as there; the bias has no gradient.  D is the rowsum of dO * O.
+// Gradients of masked attention, d_head = 128, bf16.
+//
+// With t = tanh(scale q k / cap), z the changed score in log2 units, P = 2^(z - lse):
+//     D  = rowsum(P * dP)             dV = P^T dO        dP = dO V^T
+//     dS = P * (dP - D) * (1 - t^2)   dQ = scale dS K    dK = scale dS^T Q
+// (without a cap the last factor is 1; the bias has no gradient).  Two passes, each
+// with one writer of a gradient and a fixed order of its sums, no atomics:
+//  * dq: workgroup = 128 of the G Sq query rows of a (sequence, key head), 4 waves x
+//    32, keys in tiles of 64; S^T = K Q^T and dP^T = V dO^T put one row on a lane,
+//    dQ^T += K^T dS^T.
+//  * dkv: workgroup = 128 keys of a (sequence, key head), 8 waves: four of 32 keys, two
+//    of the 32 rows of a tile of 64; S = Q K^T and dP = dO V^T put one key on a lane,
+//    dV^T += dO^T P, dK^T += Q^T dS; the two row halves are added at the end.
+// Both take the range of the other axis that their rows or keys may see, and a wave
+// passes blocks of 32 in which it sees nothing.
+//
+// D.  rowsum(dO * O) has the rounding of O to bf16, which with few keys is of the size
+// of the other errors.  The dq pass starts from it, and adds the sum over its keys of
+// P (dP - D), which is what it was off by (the weights sum to 1), so that dkv takes D
+// with float32's error; where a workgroup's rows see 256 keys at most, two tiles' time
+// more give the dq pass itself that D.
 #include <algorithm>
+#include <type_traits>
 
-#include "cross_attention_bwd_kernels.h"
+#include "attention_mask.h"
+#include "attention_row_tiles.h"
 
 namespace partir {
 namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <int F>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void masked_bwd_dq_kernel(MaskedBwdParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * 2 * TILE];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = lane >> 5, col = lane & 31;
+
+  int qb, bh, part = 0;
+  if (p.q_parts == 1 && (p.by_nbh.d & 7) == 0) {
+    // an XCD takes one (sequence, key head) after the other, whose K and V stay in its L2
+    const int j = blockIdx.x >> 3, n = p.by_nqb.quot(j);
+    bh = n * 8 + (blockIdx.x & 7);
+    qb = p.by_nqb.rem(j, n);
+  } else {
+    const int rest = p.by_nbh.quot(blockIdx.x);
+    bh = p.by_nbh.rem(blockIdx.x, rest);
+    qb = p.by_q_parts.quot(rest);
+    part = p.by_q_parts.rem(rest, qb);
+  }
+  qb = (int)p.by_nqb.d - 1 - qb;       // the longest rows of a causal mask first
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
+  const SeqMask m(p, b);
+  const int R = p.G * p.Sq, last = max(p.G * m.qlen - 1, 0);   // the last row that is read: those behind it repeat it
+  const int r0 = qb * 128, i = r0 + 32 * w + col;
+  const int ic = min(i, last), sq = p.by_g.quot(ic);
+  const int64_t tq = (int64_t)b * p.Sq + sq;
+  const int head = kvh * p.G + p.by_g.rem(ic, sq);
+
+  // Q and dO of this lane's row (B operands), and a first D = rowsum(dO * O)
+  bf16x8 qf[8], gf[8];
+  float dsum = 0.0f;
+  {
+    const uint16_t* qrow = p.Q + tq * p.ldq + head * DH + 8 * h;
+    const uint16_t* grow = p.dO + tq * p.ldg + head * DH + 8 * h;
+    const uint16_t* orow = p.O + tq * p.ldo + head * DH + 8 * h;
+#pragma unroll
+    for (int ds = 0; ds < 8; ++ds) {
+      qf[ds] = *(const bf16x8*)(qrow + 16 * ds);
+      gf[ds] = *(const bf16x8*)(grow + 16 * ds);
+      const bf16x8 of = *(const bf16x8*)(orow + 16 * ds);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) dsum += (float)gf[ds][e] * (float)of[e];
+    }
+  }
+  float lse = p.lse[tq * p.Hq + head];
+  // a row without keys, or behind the last: its weights are 2^-inf
+  const bool live = lse != -__builtin_inff() && i <= last && m.qlen > 0;
+  if (!live) lse = __builtin_inff();
+  float slope = 0.0f;
+  if constexpr ((F & kBias) != 0) slope = p.mask.slopes[head] * kLog2e;
+  const RowMask mask(p, m, tq, sq);
+  const int2 keys = r0 <= last && m.qlen > 0 ? key_range(p, m, b, p.by_g.quot(r0), p.by_g.quot(min(r0 + 127, last))) : make_int2(0, 0);
+  CrossRange range = cross_range(keys.y - keys.x, p.by_q_parts, part);
+  range.begin += keys.x;
+  range.end += keys.x;
+  const bool by_id = p.mask.rows && p.mask.by_id[b];
+  TileTr tr;
+  tr.init(lane);
+  const float c = p.scale_log2;
+
+  // Weights of 32 keys from key0 on (element v: key 8 (v / 4) + 4 h + v % 4), with the
+  // cap's derivative in sl.
+  auto weights = [&](f32x16& s, f32x16& sl, int key0) {
+    if constexpr ((F & (kCap | kBias)) == 0) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, -lse);
+    } else {
+      const float far = (float)(mask.pos - key0 - 4 * h);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        if constexpr ((F & kCap) != 0) {
+          const Capped z = capped(s[v], p.mask.cap_rate, p.mask.cap_log2);
+          s[v] = z.z - lse;
+          sl[v] = z.slope;
+        } else {
+          s[v] = __builtin_fmaf(s[v], c, -lse);
+        }
+        if constexpr ((F & kBias) != 0)
+          s[v] = __builtin_fmaf(-slope, __builtin_fabsf(far - (float)(8 * (v >> 2) + (v & 3))), s[v]);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(s[v]);
+    if (!mask.all(key0, 32)) {
+      const uint32_t lo = (uint32_t)(mask.lo - key0 - 4 * h), len = (uint32_t)max(mask.lim - mask.lo, 0);
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if ((uint32_t)(8 * (v >> 2) + (v & 3)) - lo >= len) s[v] = 0.0f;
+    }
+    if (by_id) {
+      const int32_t* ids = p.mask.k_docs + (int64_t)b * p.Sk;
+      const int doc = p.mask.q_docs[tq];
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (ids[min(key0 + 8 * (v >> 2) + 4 * h + (v & 3), p.Sk - 1)] != doc) s[v] = 0.0f;
+    }
+  };
+  if (keys.y - keys.x <= 256) {
+    dsum = 0.0f;
+    for (int key = keys.x; key < keys.y; key += TR) {
+      const int64_t tk = (int64_t)b * p.Sk + key;
+      tile_load<TR, 4>(p.K + tk * p.ldk + kvh * DH, p.ldk, min(TR, m.klen - key), smem, w, lane);
+      tile_load<TR, 4>(p.V + tk * p.ldv + kvh * DH, p.ldv, min(TR, m.klen - key), smem + TILE, w, lane);
+      WAIT_VMCNT(0);
+      __syncthreads();
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        if (mask.none(key + 32 * t, 32)) continue;
+        f32x16 s, dp, sl;
+        zero(s);
+        zero(dp);
+#pragma unroll
+        for (int ds = 0; ds < 8; ++ds) {
+          s = mfma(tile_rows(smem, 32 * t, col, h, ds), qf[ds], s);
+          dp = mfma(tile_rows(smem + TILE, 32 * t, col, h, ds), gf[ds], dp);
+        }
+        weights(s, sl, key + 32 * t);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dsum = __builtin_fmaf(s[v], dp[v], dsum);
+      }
+      __syncthreads();
+    }
+  }
+  const float Dq = dsum + __shfl_xor(dsum, 32);
+
+  const uint16_t* kbase = p.K + ((int64_t)b * p.Sk + range.begin) * p.ldk + kvh * DH;
+  const uint16_t* vbase = p.V + ((int64_t)b * p.Sk + range.begin) * p.ldv + kvh * DH;
+  const int nkeys = range.end - range.begin, nkb = (nkeys + TR - 1) / TR;
+  auto gload = [&](int kb, int buf) {
+    char* t = smem + buf * 2 * TILE;
+    const int rows = min(TR, nkeys - kb * TR);
+    tile_load<TR, 4>(kbase + (int64_t)kb * TR * p.ldk, p.ldk, rows, t, w, lane);
+    tile_load<TR, 4>(vbase + (int64_t)kb * TR * p.ldv, p.ldv, rows, t + TILE, w, lane);
+  };
+  f32x16 dq[4], nD;   // dP starts at -D: its first product reads it, where a subtraction would follow
+#pragma unroll
+  for (int d = 0; d < 4; ++d) zero(dq[d]);
+#pragma unroll
+  for (int v = 0; v < 16; ++v) nD[v] = -Dq;
+  float off = 0.0f;   // sum of P (dP - D)
+  auto iter = [&](int kb, auto stage) {
+    constexpr int cur = decltype(stage)::value;
+    if (kb + 1 < nkb) gload(kb + 1, cur ^ 1);
+    const char* ks = smem + cur * 2 * TILE;
+    const char* vs = ks + TILE;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key0 = range.begin + kb * TR + 32 * t;
+      if (mask.none(key0, 32)) continue;
+      f32x16 s, dp = nD, sl;
+      zero(s);
+#pragma unroll
+      for (int ds = 0; ds < 8; ++ds) {
+        s = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], s);
+        dp = mfma(tile_rows(vs, 32 * t, col, h, ds), gf[ds], dp);
+      }
+      weights(s, sl, key0);
+      bf16x8 dsf[2];
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) {
+        float x = s[v] * dp[v], y = s[v + 1] * dp[v + 1];
+        off += x + y;
+        if constexpr ((F & kCap) != 0) {
+          x *= sl[v];
+          y *= sl[v + 1];
+        }
+        put2(dsf[v >> 3], v & 7, x, y);
+      }
+#pragma unroll
+      for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) dq[d] = mfma(tr.read(ks, 2 * t + uu, d), dsf[uu], dq[d]);
+    }
+    WAIT_VMCNT(0);
+    __syncthreads();
+  };
+  if (nkb > 0) gload(0, 0);
+  WAIT_VMCNT(0);
+  __syncthreads();
+  for (int kb = 0; kb < nkb; kb += 2) {
+    iter(kb, std::integral_constant<int, 0>{});
+    if (kb + 1 < nkb) iter(kb + 1, std::integral_constant<int, 1>{});
+  }
+  off += __shfl_xor(off, 32);
+  const int io = min(i, R - 1), so = p.by_g.quot(io);
+  const int64_t tqo = (int64_t)b * p.Sq + so;
+  const int ho = kvh * p.G + p.by_g.rem(io, so);
+  if (h == 0 && i < R)
+    p.Dstat[((int64_t)part * p.B * p.Sq + tqo) * p.Hq + ho] = live ? (part == 0 ? Dq + off : off) : 0.0f;
+  if (!live) {   // whatever Q, dO and O hold there
+#pragma unroll
+    for (int d = 0; d < 4; ++d) zero(dq[d]);
+  }
+  const int rows = R - qb * 128 - 32 * w;
+  if (p.q_parts > 1)
+    store(smem, w, p.dQpart, (((int64_t)part * p.B * p.Sq + tqo) * p.Hq + ho) * DH, rows, dq, p.scale, lane);
+  else
+    store(smem, w, p.dQ, tqo * p.lddq + ho * DH, rows, dq, p.scale, lane);
+}
+
+constexpr int KW = 128;   // keys of a dkv workgroup
+
+template <bool EVEN, int F>
+__global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdParams p) {
+  constexpr int NS = 3, NSTAT = 6;                               // stages; numbers of a row
+  constexpr int VT = NS * 2 * TILE, STAT = VT + KW * ROWB;       // Q and dO tiles, V, the rows' numbers
+  // one object: with several, the compiler tells them apart, takes every tile
+  // read for one of the tiles being loaded and waits for those
+  __shared__ __attribute__((aligned(1024))) char smem[STAT + NS * NSTAT * TR * 4];
+  static_assert(8 * 16 * 64 * 16 <= STAT, "the row halves are added through the stages and V");
+  enum { LSE, NEG_D, LO, LIM, POS, SLOPE };
+  auto stat = [&](int buf, int which, int row) { return smem + STAT + ((buf * NSTAT + which) * TR + row) * 4; };
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = w & 3, rh = w >> 2;                             // the wave's keys and rows
+  const int h = lane >> 5, col = lane & 31;
+
+  const int rest = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, rest);
+  const int kblk = p.by_k_parts.quot(rest), part = p.by_k_parts.rem(rest, kblk);
+  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
+  const SeqMask m(p, b);
+  const int R = p.G * m.qlen;                                    // rows behind it are not read
+  const int k0 = kblk * KW, kw = k0 + 32 * kg, kj = kw + col;
+  const int64_t tk = (int64_t)b * p.Sk + kj;
+
+  f32x16 dk[4], dv[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    zero(dk[d]);
+    zero(dv[d]);
+  }
+  int first = 0, tiles = k0 < m.klen ? (R + TR - 1) / TR : 0;    // the tiles whose rows may see the workgroup's keys
+  if (m.causal && k0 >= m.prefix) first = (int)max((int64_t)0, min((int64_t)k0 - m.start, (int64_t)m.qlen)) * p.G / TR;
+  if (p.mask.rows && tiles > 0) {
+    const int2* blocks = p.mask.blocks + (int64_t)b * p.mask.q_blocks;
+    int lo = -1, hi = -1;
+    for (int i0 = 0; 64 * i0 < m.qlen; i0 += 64) {               // every wave for itself
+      bool in = 64 * (i0 + lane) < m.qlen;
+      if (in) {
+        const int2 e = blocks[i0 + lane];
+        in = e.x < k0 + KW && e.y > k0;
+      }
+      const uint64_t any = __builtin_amdgcn_ballot_w64(in);
+      if (any) {
+        if (lo < 0) lo = i0 + __builtin_ctzll(any);
+        hi = i0 + 63 - __builtin_clzll(any);
+      }
+    }
+    first = max(first, lo < 0 ? tiles : 64 * lo * p.G / TR);
+    if (hi >= 0) tiles = min(tiles, (int)(((int64_t)64 * (hi + 1) * p.G + TR - 1) / TR));
+  }
+  first = min(first, tiles);
+  const int per = p.by_k_parts.quot(tiles - first + p.k_parts - 1);
+  const int it0 = min(tiles, first + part * per), it1 = min(tiles, it0 + per);
+  if (it0 < it1) {                                               // workgroup-uniform
+    tile_load<KW, 8>(p.V + ((int64_t)b * p.Sk + k0) * p.ldv + kvh * DH, p.ldv, m.klen - k0, smem + VT, w, lane);
+    bf16x8 kf[8];
+    {
+      const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, m.klen - 1)) * p.ldk + kvh * DH + 8 * h;
+#pragma unroll
+      for (int ds = 0; ds < 8; ++ds) kf[ds] = *(const bf16x8*)(krow + 16 * ds);
+    }
+    const bool by_id = p.mask.rows && p.mask.by_id[b];
+    const RowTiles<EVEN, 8> rt(p, b, kvh, R, w, lane);
+    const float c = p.scale_log2, inv_c = 1.0f / p.scale_log2;
+    float st = 0.0f;
+    // Wave w < 6 provides one number of every row of a tile, a lane its row's.  The
+    // load goes out before the tile's, and is not looked at before sstore, so that
+    // waiting for it leaves the tile's in flight.
+    auto gload = [&](int it, int buf) {
+      const int i = min(it * TR + lane, R - 1), sq = p.by_g.quot(i), head = kvh * p.G + p.by_g.rem(i, sq);
+      const int64_t tq = (int64_t)b * p.Sq + sq, at = tq * p.Hq + head;
+      if (w == LSE) st = p.lse[at];
+      if (w == NEG_D) {
+        st = p.Dstat[at];
+        for (int q = 1; q < p.q_parts; ++q) st += p.Dstat[q * ((int64_t)p.B * p.Sq * p.Hq) + at];
+      }
+      if (p.mask.rows) {
+        if (w == LO) st = __builtin_bit_cast(float, p.mask.rows[tq].x);
+        if (w == LIM) st = __builtin_bit_cast(float, p.mask.rows[tq].y);
+      }
+      if constexpr ((F & kBias) != 0) {
+        if (w == SLOPE) st = p.mask.slopes[head];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      rt.load(it, smem + buf * 2 * TILE);
+    };
+    auto sstore = [&](int it, int buf) {
+      const int i = it * TR + lane, sq = p.by_g.quot(min(i, R - 1));
+      float x = st;
+      if (w == LSE) {   // a missing row, or one without keys: P = 2^-inf
+        x = i < R && x != -__builtin_inff() ? x : __builtin_inff();
+        if constexpr ((F & kCap) == 0) x = -x * inv_c;
+      }
+      if (w == NEG_D) x = i < R ? -x : 0.0f;
+      if (w == LO && !p.mask.rows) x = 0.0f;
+      if (w == LIM) {
+        int lim = m.lim(sq);
+        if (p.mask.rows) lim = min(lim, __builtin_bit_cast(int, x));
+        x = __builtin_bit_cast(float, i < R ? lim : 0);
+      }
+      if (w == POS) x = (float)(m.start + sq);
+      if (w == SLOPE) x *= kLog2e;
+      if (w < NSTAT) lds_write(stat(buf, w, lane), x);
+    };
+    TileTr tr;
+    tr.init(lane);
+    gload(it0, 0);
+    sstore(it0, 0);
+    if (it0 + 1 < it1) {
+      gload(it0 + 1, 1);
+      sstore(it0 + 1, 1);
+    }
+    // The stage is a number, not a constant: three copies of the body would each keep
+    // their addresses in registers (45 of them read back from memory a tile).
+    int cur = 0, vt = VT + 32 * kg * ROWB;
+#pragma unroll 1
+    for (int it = it0; it < it1; ++it) {
+      const int nxt = cur == 0 ? NS - 1 : cur - 1;   // the stage of tile it + 2
+      asm volatile("" : "+s"(vt));                   // V's addresses are formed here
+      __builtin_amdgcn_sched_barrier(0);
+      if (it + 1 < it1)                // the next tile may be in flight: four loads of this wave
+        WAIT_VMCNT(4);
+      else
+        WAIT_VMCNT(0);
+      lds_barrier();                   // everyone's tile has landed, and everyone is done with the stage loaded next
+      if (it + 2 < it1) gload(it + 2, nxt);
+      __builtin_amdgcn_sched_barrier(0);
+      const char* qs = smem + cur * 2 * TILE;
+      const char* gs = qs + TILE;
+      // which of the wave's 32 rows see its keys, by the lanes of both halves alike
+      const int lo = lds_read<int>(stat(cur, LO, 32 * rh + col)), lim = lds_read<int>(stat(cur, LIM, 32 * rh + col));
+      if (__builtin_amdgcn_ballot_w64(lo < kw + 32 && lim > kw && lim > lo) != 0) {
+        const bool some = __builtin_amdgcn_ballot_w64(lo > kw || lim < kw + 32) != 0;
+        auto row4 = [&](int which, int q) { return lds_read<f32x4>(stat(cur, which, 32 * rh + 8 * q + 4 * h)); };
+        f32x16 s, dp;
+        if constexpr ((F & kCap) != 0) {
+          zero(s);
+        } else {                       // the accumulators start at -lse / c, and at -D
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 x = row4(LSE, q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[4 * q + j] = x[j];
+          }
+        }
+#pragma unroll
+        for (int ds = 0; ds < 8; ++ds) s = mfma(tile_rows(qs, 32 * rh, col, h, ds), kf[ds], s);
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 pf[2];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f32x4 z, sl;
+          if constexpr ((F & kCap) != 0) {
+            const f32x4 lse = row4(LSE, q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const Capped x = capped(s[4 * q + j], p.mask.cap_rate, p.mask.cap_log2);
+              z[j] = x.z - lse[j];
+              sl[j] = x.slope;
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = s[4 * q + j] * c;
+          }
+          if constexpr ((F & kBias) != 0) {
+            const f32x4 at = row4(POS, q), slope = row4(SLOPE, q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = __builtin_fmaf(-slope[j], __builtin_fabsf(at[j] - (float)kj), z[j]);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) z[j] = __builtin_amdgcn_exp2f(z[j]);
+          if (some) {
+            const f32x4 lo4 = row4(LO, q), lim4 = row4(LIM, q);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (kj < __builtin_bit_cast(int, (float)lo4[j]) || kj >= __builtin_bit_cast(int, (float)lim4[j])) z[j] = 0.0f;
+          }
+          if (by_id) {
+            const int doc = p.mask.k_docs[(int64_t)b * p.Sk + min(kj, m.klen - 1)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int i = min(it * TR + 32 * rh + 8 * q + 4 * h + j, R - 1);
+              if (p.mask.q_docs[(int64_t)b * p.Sq + p.by_g.quot(i)] != doc) z[j] = 0.0f;
+            }
+          }
+          put2(pf[q >> 1], 4 * (q & 1), z[0], z[1]);
+          put2(pf[q >> 1], 4 * (q & 1) + 2, z[2], z[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[4 * q + j] = (F & kCap) != 0 ? z[j] * sl[j] : z[j];
+          if constexpr ((F & (kCap | kBias)) != 0) __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = row4(NEG_D, q);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dp[4 * q + j] = x[j];
+        }
+#pragma unroll
+        for (int ds = 0; ds < 8; ++ds)
+          dp = mfma(tile_rows(gs, 32 * rh, col, h, ds), tile_rows(smem + vt, 0, col, h, ds), dp);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * rh + uu, d), pf[uu], dv[d]);
+#pragma unroll
+        for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[v] * dp[v], s[v + 1] * dp[v + 1]);
+#pragma unroll
+        for (int uu = 0; uu < 2; ++uu)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, 2 * rh + uu, d), pf[uu], dk[d]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (it + 2 < it1) sstore(it + 2, nxt);
+      cur = cur == NS - 1 ? 0 : cur + 1;
+    }
+    // The row halves are added: the first takes dK of both, the second dV.
+    __syncthreads();
+    f32x4* const box = (f32x4*)(smem + w * 16 * 64 * 16) + lane;
+    const f32x4* const other = (const f32x4*)(smem + (w ^ 4) * 16 * 64 * 16) + lane;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float k = dk[d][4 * q + j], v = dv[d][4 * q + j];
+          x[j] = rh == 0 ? v : k;
+          dk[d][4 * q + j] = rh == 0 ? k : v;                    // from here on the wave's own sum
+        }
+        box[(4 * d + q) * 64] = x;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = other[(4 * d + q) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dk[d][4 * q + j] += x[j];
+      }
+    __syncthreads();
+    if (kj >= m.klen) {   // a lane's key is its own column: what its sums hold goes nowhere else
+#pragma unroll
+      for (int d = 0; d < 4; ++d) zero(dk[d]);
+    }
+  }
+  const int rows = p.Sk - kw;
+  const float f = rh == 0 ? p.scale : 1.0f;
+  if (p.k_parts > 1)
+    store(smem, w, rh == 0 ? p.dKpart : p.dVpart, (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH, rows, dk, f, lane);
+  else
+    store(smem, w, rh == 0 ? p.dK : p.dV, tk * (rh == 0 ? p.lddk : p.lddv) + kvh * DH, rows, dk, f, lane);
+}
+
+constexpr int64_t kCUs = 256;
 
 template <int F>
 void launch_form(const MaskedBwdParams& p, CrossBwdPass pass, hipStream_t s) {
   const int64_t nbh = (int64_t)p.B * p.Hk;
   if (pass == CROSS_DQ) {
     const int64_t blocks = ((int64_t)p.G * p.Sq + 127) / 128;
-    hipLaunchKernelGGL((cross_bwd_dq_kernel<F>), dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
+    hipLaunchKernelGGL((masked_bwd_dq_kernel<F>), dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
   } else {
-    const int64_t blocks = ((int64_t)p.Sk + 255) / 256;
+    const int64_t blocks = ((int64_t)p.Sk + KW - 1) / KW;
     const dim3 grid((unsigned)(blocks * nbh * p.k_parts));
     if (16 % p.G == 0)
-      hipLaunchKernelGGL((cross_bwd_dkv_kernel<true, F>), grid, dim3(2 * NT), 0, s, p);
+      hipLaunchKernelGGL((masked_bwd_dkv_kernel<true, F>), grid, dim3(2 * NT), 0, s, p);
     else
-      hipLaunchKernelGGL((cross_bwd_dkv_kernel<false, F>), grid, dim3(2 * NT), 0, s, p);
+      hipLaunchKernelGGL((masked_bwd_dkv_kernel<false, F>), grid, dim3(2 * NT), 0, s, p);
   }
 }
 
 }  // namespace
+
+CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk) {
+  const int64_t R = Hq / Hk * Sq, rows = (R + 63) / 64, keys = (Sk + 63) / 64;
+  auto most = [](int64_t grid, int64_t tiles) { return grid > 0 ? std::min(kCUs / grid, tiles) : 1; };
+  const double q_us = 1.5e-4 * (double)(B * Sq * Hq), k_us = 2 * 1.5e-4 * (double)(B * Sk * Hk);
+  return {false, best_parts(most(B * Hk * ((R + 127) / 128), keys), keys, 1.45, q_us),
+          best_parts(most(B * Hk * ((Sk + KW - 1) / KW), rows), rows, 1.5, k_us)};
+}
 
 hipError_t launch_masked_backward(const MaskedBwdParams& p, int form, CrossBwdPass pass, hipStream_t s) {
   switch (form & (kCap | kBias)) {

@@ -131,8 +131,12 @@ __device__ __forceinline__ CrossRange cross_range(int len, const Div& by_split, 
 struct MaskArgs {
   const int32_t *q_lens, *q_starts, *prefix;   // [B] each, or NULL: Sq, Sk - Sq, 0
   const int32_t *q_docs, *k_docs;              // [B Sq], [B Sk], or both NULL: one document
-  const int2 *q_table, *k_table;               // their least and largest of every 64 positions, [B][blocks]
-  int q_blocks, k_blocks;
+  // with documents: the keys [x, y) of every query's, the least x and largest y of
+  // every 64 queries that have any, [B][q_blocks], and whether documents of a sequence
+  // lie in pieces, [B]: then its intervals are all of its keys, and numbers are compared
+  const int2 *rows, *blocks;
+  const int32_t* by_id;
+  int q_blocks;
   const float* slopes;                         // [Hq]
   float cap_log2, cap_rate;                    // cap log2 e, 2 scale log2 e / cap
   int causal;
@@ -142,13 +146,14 @@ struct MaskedParams : CrossParams {
 };
 hipError_t launch_masked_attention(const MaskedParams& p, int form, const CrossChoice& c, hipStream_t s);
 hipError_t launch_masked_combine(const MaskedParams& p, hipStream_t s);
-// The tables of both sequences' documents, into q_table and k_table.
-struct DocTables {
-  const int32_t *docs[2], *lens[2];
-  int2* table[2];
-  int S[2], blocks[2], B;
+// rows, blocks and by_id of MaskArgs
+struct DocRows {
+  const int32_t *q_docs, *k_docs, *q_lens, *k_lens;
+  int2 *rows, *blocks;
+  int32_t* by_id;
+  int B, Sq, Sk, q_blocks;
 };
-hipError_t launch_doc_tables(const DocTables& t, hipStream_t s);
+hipError_t launch_doc_rows(const DocRows& t, hipStream_t s);
 
 // Gradients (cross_attention_bwd.hip).  Up to 128 keys a sequence: one pass.
 // Above: a dq pass, which takes the key axis in q_parts parts, and one for dk and
@@ -157,7 +162,7 @@ hipError_t launch_doc_tables(const DocTables& t, hipStream_t s);
 struct CrossBwdParams {
   const uint16_t *Q, *K, *V, *O, *dO;
   const float* lse;
-  float* Dstat;            // [B Sq][Hq] rowsums of dO * O, from the dq pass for the other
+  float* Dstat;            // [B Sq][Hq] D of the rows, from the dq pass for the other (masked: in q_parts parts)
   uint16_t *dQ, *dK, *dV;
   float *dQpart, *dKpart, *dVpart;   // [parts][rows][heads * 128]
   const int32_t* lens;
@@ -175,8 +180,8 @@ struct CrossBwdChoice {
   bool one_pass;
   int q_parts, k_parts;
 };
-// may_one_pass: up to 128 keys in one pass (not with masks)
-CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, bool may_one_pass = true);
+CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
+CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
 enum CrossBwdPass { CROSS_ALL, CROSS_DQ, CROSS_DKV };
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s);
 hipError_t launch_masked_backward(const MaskedBwdParams& p, int form, CrossBwdPass pass, hipStream_t s);

@@ -372,32 +372,32 @@ int resolve_mask(MaskArgs& m, int& form, const partir_attention_mask* mask, floa
   return PARTIR_OK;
 }
 
-// Documents' tables, at the front of the workspace.
+// The intervals of documents, at the front of the workspace.
 struct DocPlan {
-  int q_blocks = 0, k_blocks = 0;
-  size_t q_bytes = 0, k_bytes = 0;
-  size_t ws() const { return q_bytes + k_bytes; }
+  int q_blocks = 0;
+  size_t row_bytes = 0, block_bytes = 0, id_bytes = 0;
+  size_t ws() const { return row_bytes + block_bytes + id_bytes; }
 };
 DocPlan plan_docs(const CrossSizes& z, const partir_attention_mask& mask) {
   DocPlan d;
-  if (!mask.k_docs) return d;
+  if (!mask.k_docs || z.B * z.Sq == 0) return d;
   d.q_blocks = (int)cdiv(z.Sq, 64);
-  d.k_blocks = (int)cdiv(z.Sk, 64);
-  d.q_bytes = align_up((size_t)z.B * d.q_blocks * 8);
-  d.k_bytes = align_up((size_t)z.B * d.k_blocks * 8);
+  d.row_bytes = align_up((size_t)z.B * z.Sq * 8);
+  d.block_bytes = align_up((size_t)z.B * d.q_blocks * 8);
+  d.id_bytes = align_up((size_t)z.B * 4);
   return d;
 }
 
-int run_doc_tables(MaskArgs& m, const DocPlan& d, const CrossSizes& z, const int32_t* k_lens, void* ws, hipStream_t s) {
+int run_doc_rows(MaskArgs& m, const DocPlan& d, const CrossSizes& z, const int32_t* k_lens, void* ws, hipStream_t s) {
   if (!d.ws()) return PARTIR_OK;
-  m.q_blocks = d.q_blocks; m.k_blocks = d.k_blocks;
-  m.q_table = (const int2*)ws;
-  m.k_table = (const int2*)((char*)ws + d.q_bytes);
-  DocTables t{};
-  t.B = (int)z.B;
-  t.docs[0] = m.q_docs; t.lens[0] = m.q_lens; t.table[0] = (int2*)ws; t.S[0] = (int)z.Sq; t.blocks[0] = d.q_blocks;
-  t.docs[1] = m.k_docs; t.lens[1] = k_lens; t.table[1] = (int2*)((char*)ws + d.q_bytes); t.S[1] = (int)z.Sk; t.blocks[1] = d.k_blocks;
-  return launched(launch_doc_tables(t, s), "doc_tables");
+  DocRows t{};
+  t.q_docs = m.q_docs; t.k_docs = m.k_docs; t.q_lens = m.q_lens; t.k_lens = k_lens;
+  t.rows = (int2*)ws;
+  t.blocks = (int2*)((char*)ws + d.row_bytes);
+  t.by_id = (int32_t*)((char*)ws + d.row_bytes + d.block_bytes);
+  t.B = (int)z.B; t.Sq = (int)z.Sq; t.Sk = (int)z.Sk; t.q_blocks = d.q_blocks;
+  m.rows = t.rows; m.blocks = t.blocks; m.by_id = t.by_id; m.q_blocks = d.q_blocks;
+  return launched(launch_doc_rows(t, s), "doc_rows");
 }
 
 // What forward and backward kernels share of their parameters.
@@ -445,15 +445,15 @@ int run_masked(const void* Q, const void* K, const void* V, void* O, float* lse,
   }
   if (int st = begin_launches()) return st;
   hipStream_t s = (hipStream_t)stream;
-  if (int st = run_doc_tables(p.mask, docs, z, mask->k_lens, ws, s)) return st;
+  if (int st = run_doc_rows(p.mask, docs, z, mask->k_lens, ws, s)) return st;
   if (int st = launched(launch_masked_attention(p, form, plan.c, s), "masked_attention")) return st;
   return p.nsplit == 1 ? PARTIR_OK : launched(launch_masked_combine(p, s), "masked_combine");
 }
 
 CrossBwdPlan plan_masked_bwd(const CrossSizes& z) {
   CrossBwdPlan p;
-  p.c = cross_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk, false);
-  p.d_bytes = align_up((size_t)z.B * z.Sq * z.Hq * 4);
+  p.c = masked_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk);
+  p.d_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * 4);
   if (p.c.q_parts > 1) p.q_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
   if (p.c.k_parts > 1) p.k_bytes = align_up((size_t)p.c.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
   return p;
@@ -837,7 +837,7 @@ int partir_masked_attention_backward(const void* Q, const void* K, const void* V
     p.scale_log2 = scale * kLog2e;
     if (int st = begin_launches()) return st;
     hipStream_t s = (hipStream_t)stream;
-    if (int st = run_doc_tables(p.mask, docs, z, mask->k_lens, ws, s)) return st;
+    if (int st = run_doc_rows(p.mask, docs, z, mask->k_lens, ws, s)) return st;
     if (Tq > 0) {
       if (int st = launched(launch_masked_backward(p, form, CROSS_DQ, s), "masked_bwd_dq")) return st;
       if (p.q_parts > 1) {
