@@ -115,15 +115,12 @@ struct RowMask {
 
 // Score s = q k, in units of log2: z = cap tanh(scale s / cap) log2 e with
 // tanh x = 1 - 2 / (1 + e^(2x)); r = 1 / (1 + e^(2x)) gives its derivative too,
-// 1 - tanh^2 = 4 r (1 - r).  z is off by 2^-20 of the cap at most (the roundings of
+// 1 - tanh^2 = 4 (r - r^2).  z is off by 2^-20 of the cap at most (the roundings of
 // exp2, of the sum and of the reciprocal, each of numbers up to 1), which for caps up
 // to 1024, the most that a call takes, stays below a weight's rounding to bf16.
-struct Capped {
-  float z, slope;
-};
-__device__ __forceinline__ Capped capped(float s, float rate, float cap_log2) {
-  const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * rate));
-  return {__builtin_fmaf(-2.0f * cap_log2, r, cap_log2), 4.0f * r * (1.0f - r)};
+// z = a - 2 cap log2 e r for a = cap log2 e, or less what the caller subtracts anyway.
+__device__ __forceinline__ float cap_r(float s, float rate) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * rate));
 }
 
 }  // namespace partir

@@ -11,13 +11,13 @@ constexpr int NT = 256;
 constexpr int TR = 64;                 // rows of a streamed tile
 constexpr int TILE = TR * ROWB;
 
-// The 64-row tiles of the first `rows` of the G Sq query rows of a (sequence, key head), Q and dO
+// The ROWS-row tiles of the first `rows` of the G Sq query rows of a (sequence, key head), Q and dO
 // side by side: row i is position i / G of head i mod G.  Addresses ascend with
 // the rows, so a descriptor that ends with the tile's last row makes those
 // behind it zeros.  Where G divides 16, a lane's rows lie at one offset from a
 // tile's first position and a fixed step apart; else each is divided by G (8 %
 // of dkv's time).
-template <bool EVEN, int WAVES = 4>
+template <bool EVEN, int WAVES = 4, int ROWS = TR>
 struct RowTiles {
   const uint16_t *q, *g;
   int64_t ldq, ldg;
@@ -34,22 +34,22 @@ struct RowTiles {
     og = (uint32_t)s * (uint32_t)(ldg * 2) + in;
   }
   __device__ __forceinline__ void load(int it, char* tile) const {
-    const int i0 = it * TR, s0 = by_g.quot(i0), last = min(i0 + TR, R) - 1, sl = by_g.quot(last);
+    const int i0 = it * ROWS, s0 = by_g.quot(i0), last = min(i0 + ROWS, R) - 1, sl = by_g.quot(last);
     const uint32_t tail = (uint32_t)by_g.rem(last, sl) * ROWB + ROWB;
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(q + s0 * ldq, (uint32_t)((sl - s0) * ldq * 2) + tail);
     const __amdgpu_buffer_rsrc_t rg = make_rsrc(g + s0 * ldg, (uint32_t)((sl - s0) * ldg * 2) + tail);
     auto put = [&](int j, uint32_t a, uint32_t b) {
       char* const t = tile + (WAVES * j + w) * 1024;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void*)t, 16, a, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, (lds_void*)(t + TILE), 16, b, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rg, (lds_void*)(t + ROWS * ROWB), 16, b, 0, 0, 0);
     };
     if constexpr (EVEN) {
       const uint32_t n = by_g.quot(4 * WAVES), sq = n * (uint32_t)(ldq * 2), sg = n * (uint32_t)(ldg * 2);
 #pragma unroll
-      for (int j = 0; j < TR / (4 * WAVES); ++j) put(j, oq + j * sq, og + j * sg);
+      for (int j = 0; j < ROWS / (4 * WAVES); ++j) put(j, oq + j * sq, og + j * sg);
     } else {
 #pragma unroll
-      for (int j = 0; j < TR / (4 * WAVES); ++j) {
+      for (int j = 0; j < ROWS / (4 * WAVES); ++j) {
         const int i = i0 + 4 * (WAVES * j + w) + (lane >> 4), s = by_g.quot(i);
         const uint32_t in = (uint32_t)by_g.rem(i, s) * ROWB + chunk;
         put(j, (uint32_t)(s - s0) * (uint32_t)(ldq * 2) + in, (uint32_t)(s - s0) * (uint32_t)(ldg * 2) + in);

@@ -177,7 +177,7 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           if constexpr ((F & kCap) != 0)
-            sacc[t][v] = capped(sacc[t][v], p.mask.cap_rate, p.mask.cap_log2).z;
+            sacc[t][v] = __builtin_fmaf(-2.0f * p.mask.cap_log2, cap_r(sacc[t][v], p.mask.cap_rate), p.mask.cap_log2);
           else
             sacc[t][v] *= p.scale_log2;
           if constexpr ((F & kBias) != 0)

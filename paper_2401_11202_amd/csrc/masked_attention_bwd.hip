@@ -8,9 +8,8 @@
 //  * dq: workgroup = 128 of the G Sq query rows of a (sequence, key head), 4 waves x
 //    32, keys in tiles of 64; S^T = K Q^T and dP^T = V dO^T put one row on a lane,
 //    dQ^T += K^T dS^T.
-//  * dkv: workgroup = 128 keys of a (sequence, key head), 8 waves: four of 32 keys, two
-//    of the 32 rows of a tile of 64; S = Q K^T and dP = dO V^T put one key on a lane,
-//    dV^T += dO^T P, dK^T += Q^T dS; the two row halves are added at the end.
+//  * dkv: workgroup = 128 keys of a (sequence, key head), 4 waves x 32, rows in tiles of
+//    32; S = Q K^T and dP = dO V^T put one key on a lane, dV^T += dO^T P, dK^T += Q^T dS.
 // Both take the range of the other axis that their rows or keys may see, and a wave
 // passes blocks of 32 in which it sees nothing.
 //
@@ -91,8 +90,9 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
   tr.init(lane);
   const float c = p.scale_log2;
 
-  // Weights of 32 keys from key0 on (element v: key 8 (v / 4) + 4 h + v % 4), with the
-  // cap's derivative in sl.
+  // Weights of 32 keys from key0 on (element v: key 8 (v / 4) + 4 h + v % 4), with a
+  // quarter of the cap's derivative in sl.
+  const float top = p.mask.cap_log2 - lse;
   auto weights = [&](f32x16& s, f32x16& sl, int key0) {
     if constexpr ((F & (kCap | kBias)) == 0) {
 #pragma unroll
@@ -102,9 +102,9 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         if constexpr ((F & kCap) != 0) {
-          const Capped z = capped(s[v], p.mask.cap_rate, p.mask.cap_log2);
-          s[v] = z.z - lse;
-          sl[v] = z.slope;
+          const float r = cap_r(s[v], p.mask.cap_rate);
+          s[v] = __builtin_fmaf(-2.0f * p.mask.cap_log2, r, top);
+          sl[v] = __builtin_fmaf(-r, r, r);
         } else {
           s[v] = __builtin_fmaf(s[v], c, -lse);
         }
@@ -114,18 +114,18 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
     }
 #pragma unroll
     for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(s[v]);
-    if (!mask.all(key0, 32)) {
+    if (by_id || !mask.all(key0, 32)) {
       const uint32_t lo = (uint32_t)(mask.lo - key0 - 4 * h), len = (uint32_t)max(mask.lim - mask.lo, 0);
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         if ((uint32_t)(8 * (v >> 2) + (v & 3)) - lo >= len) s[v] = 0.0f;
-    }
-    if (by_id) {
-      const int32_t* ids = p.mask.k_docs + (int64_t)b * p.Sk;
-      const int doc = p.mask.q_docs[tq];
+      if (by_id) {
+        const int32_t* ids = p.mask.k_docs + (int64_t)b * p.Sk;
+        const int doc = p.mask.q_docs[tq];
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (ids[min(key0 + 8 * (v >> 2) + 4 * h + (v & 3), p.Sk - 1)] != doc) s[v] = 0.0f;
+        for (int v = 0; v < 16; ++v)
+          if (ids[min(key0 + 8 * (v >> 2) + 4 * h + (v & 3), p.Sk - 1)] != doc) s[v] = 0.0f;
+      }
     }
   };
   if (keys.y - keys.x <= 256) {
@@ -225,27 +225,29 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
     for (int d = 0; d < 4; ++d) zero(dq[d]);
   }
   const int rows = R - qb * 128 - 32 * w;
+  const float f = (F & kCap) != 0 ? 4.0f * p.scale : p.scale;
   if (p.q_parts > 1)
-    store(smem, w, p.dQpart, (((int64_t)part * p.B * p.Sq + tqo) * p.Hq + ho) * DH, rows, dq, p.scale, lane);
+    store(smem, w, p.dQpart, (((int64_t)part * p.B * p.Sq + tqo) * p.Hq + ho) * DH, rows, dq, f, lane);
   else
-    store(smem, w, p.dQ, tqo * p.lddq + ho * DH, rows, dq, p.scale, lane);
+    store(smem, w, p.dQ, tqo * p.lddq + ho * DH, rows, dq, f, lane);
 }
 
 constexpr int KW = 128;   // keys of a dkv workgroup
+constexpr int QT = 32;    // rows of its tiles
 
 template <bool EVEN, int F>
-__global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdParams p) {
-  constexpr int NS = 3, NSTAT = 6;                               // stages; numbers of a row
-  constexpr int VT = NS * 2 * TILE, STAT = VT + KW * ROWB;       // Q and dO tiles, V, the rows' numbers
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void masked_bwd_dkv_kernel(MaskedBwdParams p) {
+  constexpr int NS = 2, NSTAT = 6, STAGE = 2 * QT * ROWB;        // stages; numbers of a row
+  constexpr int VT = NS * STAGE, STAT = VT + KW * ROWB;          // Q and dO tiles, V, the rows' numbers
   // one object: with several, the compiler tells them apart, takes every tile
   // read for one of the tiles being loaded and waits for those
-  __shared__ __attribute__((aligned(1024))) char smem[STAT + NS * NSTAT * TR * 4];
-  static_assert(8 * 16 * 64 * 16 <= STAT, "the row halves are added through the stages and V");
+  __shared__ __attribute__((aligned(1024))) char smem[STAT + NS * NSTAT * QT * 4];
+  static_assert(4 * row_area<4, __bf16>() <= STAT && 4 * row_area<2, float>() <= STAT, "the end goes through the stages and V");
   enum { LSE, NEG_D, LO, LIM, POS, SLOPE };
-  auto stat = [&](int buf, int which, int row) { return smem + STAT + ((buf * NSTAT + which) * TR + row) * 4; };
+  auto stat = [&](int buf, int which, int row) { return smem + STAT + ((buf * NSTAT + which) * QT + row) * 4; };
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kg = w & 3, rh = w >> 2;                             // the wave's keys and rows
   const int h = lane >> 5, col = lane & 31;
 
   const int rest = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, rest);
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdPara
   const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
   const SeqMask m(p, b);
   const int R = p.G * m.qlen;                                    // rows behind it are not read
-  const int k0 = kblk * KW, kw = k0 + 32 * kg, kj = kw + col;
+  const int k0 = kblk * KW, kw = k0 + 32 * w, kj = kw + col;
   const int64_t tk = (int64_t)b * p.Sk + kj;
 
   f32x16 dk[4], dv[4];
@@ -262,8 +264,8 @@ __global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdPara
     zero(dk[d]);
     zero(dv[d]);
   }
-  int first = 0, tiles = k0 < m.klen ? (R + TR - 1) / TR : 0;    // the tiles whose rows may see the workgroup's keys
-  if (m.causal && k0 >= m.prefix) first = (int)max((int64_t)0, min((int64_t)k0 - m.start, (int64_t)m.qlen)) * p.G / TR;
+  int first = 0, tiles = k0 < m.klen ? (R + QT - 1) / QT : 0;    // the tiles whose rows may see the workgroup's keys
+  if (m.causal && k0 >= m.prefix) first = (int)max((int64_t)0, min((int64_t)k0 - m.start, (int64_t)m.qlen)) * p.G / QT;
   if (p.mask.rows && tiles > 0) {
     const int2* blocks = p.mask.blocks + (int64_t)b * p.mask.q_blocks;
     int lo = -1, hi = -1;
@@ -279,14 +281,14 @@ __global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdPara
         hi = i0 + 63 - __builtin_clzll(any);
       }
     }
-    first = max(first, lo < 0 ? tiles : 64 * lo * p.G / TR);
-    if (hi >= 0) tiles = min(tiles, (int)(((int64_t)64 * (hi + 1) * p.G + TR - 1) / TR));
+    first = max(first, lo < 0 ? tiles : 64 * lo * p.G / QT);
+    if (hi >= 0) tiles = min(tiles, (int)(((int64_t)64 * (hi + 1) * p.G + QT - 1) / QT));
   }
   first = min(first, tiles);
   const int per = p.by_k_parts.quot(tiles - first + p.k_parts - 1);
   const int it0 = min(tiles, first + part * per), it1 = min(tiles, it0 + per);
   if (it0 < it1) {                                               // workgroup-uniform
-    tile_load<KW, 8>(p.V + ((int64_t)b * p.Sk + k0) * p.ldv + kvh * DH, p.ldv, m.klen - k0, smem + VT, w, lane);
+    tile_load<KW, 4>(p.V + ((int64_t)b * p.Sk + k0) * p.ldv + kvh * DH, p.ldv, m.klen - k0, smem + VT, w, lane);
     bf16x8 kf[8];
     {
       const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, m.klen - 1)) * p.ldk + kvh * DH + 8 * h;
@@ -294,78 +296,68 @@ __global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdPara
       for (int ds = 0; ds < 8; ++ds) kf[ds] = *(const bf16x8*)(krow + 16 * ds);
     }
     const bool by_id = p.mask.rows && p.mask.by_id[b];
-    const RowTiles<EVEN, 8> rt(p, b, kvh, R, w, lane);
+    const RowTiles<EVEN, 4, QT> rt(p, b, kvh, R, w, lane);
     const float c = p.scale_log2, inv_c = 1.0f / p.scale_log2;
+    const int which = 2 * w + h;       // the number that this half of a wave provides, a lane its row's
     float st = 0.0f;
-    // Wave w < 6 provides one number of every row of a tile, a lane its row's.  The
-    // load goes out before the tile's, and is not looked at before sstore, so that
-    // waiting for it leaves the tile's in flight.
+    // nothing looks at the loaded number before sstore: a use here would wait for the tile
     auto gload = [&](int it, int buf) {
-      const int i = min(it * TR + lane, R - 1), sq = p.by_g.quot(i), head = kvh * p.G + p.by_g.rem(i, sq);
+      const int i = min(it * QT + col, R - 1), sq = p.by_g.quot(i), head = kvh * p.G + p.by_g.rem(i, sq);
       const int64_t tq = (int64_t)b * p.Sq + sq, at = tq * p.Hq + head;
-      if (w == LSE) st = p.lse[at];
-      if (w == NEG_D) {
+      if (which == LSE) st = p.lse[at];
+      if (which == NEG_D) {
         st = p.Dstat[at];
         for (int q = 1; q < p.q_parts; ++q) st += p.Dstat[q * ((int64_t)p.B * p.Sq * p.Hq) + at];
       }
       if (p.mask.rows) {
-        if (w == LO) st = __builtin_bit_cast(float, p.mask.rows[tq].x);
-        if (w == LIM) st = __builtin_bit_cast(float, p.mask.rows[tq].y);
+        if (which == LO) st = __builtin_bit_cast(float, p.mask.rows[tq].x);
+        if (which == LIM) st = __builtin_bit_cast(float, p.mask.rows[tq].y);
       }
       if constexpr ((F & kBias) != 0) {
-        if (w == SLOPE) st = p.mask.slopes[head];
+        if (which == SLOPE) st = p.mask.slopes[head];
       }
-      __builtin_amdgcn_sched_barrier(0);
-      rt.load(it, smem + buf * 2 * TILE);
+      rt.load(it, smem + buf * STAGE);
     };
     auto sstore = [&](int it, int buf) {
-      const int i = it * TR + lane, sq = p.by_g.quot(min(i, R - 1));
+      const int i = it * QT + col, sq = p.by_g.quot(min(i, R - 1));
       float x = st;
-      if (w == LSE) {   // a missing row, or one without keys: P = 2^-inf
+      if (which == LSE) {   // a missing row, or one without keys: P = 2^-inf
         x = i < R && x != -__builtin_inff() ? x : __builtin_inff();
-        if constexpr ((F & kCap) == 0) x = -x * inv_c;
+        x = (F & kCap) != 0 ? p.mask.cap_log2 - x : -x * inv_c;
       }
-      if (w == NEG_D) x = i < R ? -x : 0.0f;
-      if (w == LO && !p.mask.rows) x = 0.0f;
-      if (w == LIM) {
+      if (which == NEG_D) x = i < R ? -x : 0.0f;
+      if (which == LO && !p.mask.rows) x = 0.0f;
+      if (which == LIM) {
         int lim = m.lim(sq);
         if (p.mask.rows) lim = min(lim, __builtin_bit_cast(int, x));
         x = __builtin_bit_cast(float, i < R ? lim : 0);
       }
-      if (w == POS) x = (float)(m.start + sq);
-      if (w == SLOPE) x *= kLog2e;
-      if (w < NSTAT) lds_write(stat(buf, w, lane), x);
+      if (which == POS) x = (float)(m.start + sq);
+      if (which == SLOPE) x *= kLog2e;
+      if (which < NSTAT) lds_write(stat(buf, which, col), x);
     };
     TileTr tr;
     tr.init(lane);
     gload(it0, 0);
     sstore(it0, 0);
-    if (it0 + 1 < it1) {
-      gload(it0 + 1, 1);
-      sstore(it0 + 1, 1);
-    }
-    // The stage is a number, not a constant: three copies of the body would each keep
-    // their addresses in registers (45 of them read back from memory a tile).
-    int cur = 0, vt = VT + 32 * kg * ROWB;
+    // The stage is a number, not a constant: copies of the body would each keep their
+    // addresses in registers.  (Eight waves with three stages and three copies read 45
+    // of them back from memory a tile.)
+    int cur = 0, vt = VT + 32 * w * ROWB;
 #pragma unroll 1
     for (int it = it0; it < it1; ++it) {
-      const int nxt = cur == 0 ? NS - 1 : cur - 1;   // the stage of tile it + 2
-      asm volatile("" : "+s"(vt));                   // V's addresses are formed here
+      asm volatile("" : "+s"(vt));     // V's addresses are formed here
       __builtin_amdgcn_sched_barrier(0);
-      if (it + 1 < it1)                // the next tile may be in flight: four loads of this wave
-        WAIT_VMCNT(4);
-      else
-        WAIT_VMCNT(0);
+      WAIT_VMCNT(0);
       lds_barrier();                   // everyone's tile has landed, and everyone is done with the stage loaded next
-      if (it + 2 < it1) gload(it + 2, nxt);
+      if (it + 1 < it1) gload(it + 1, cur ^ 1);
       __builtin_amdgcn_sched_barrier(0);
-      const char* qs = smem + cur * 2 * TILE;
-      const char* gs = qs + TILE;
-      // which of the wave's 32 rows see its keys, by the lanes of both halves alike
-      const int lo = lds_read<int>(stat(cur, LO, 32 * rh + col)), lim = lds_read<int>(stat(cur, LIM, 32 * rh + col));
+      const char* qs = smem + cur * STAGE;
+      const char* gs = qs + QT * ROWB;
+      // which of the rows see the wave's keys, by the lanes of both halves alike
+      const int lo = lds_read<int>(stat(cur, LO, col)), lim = lds_read<int>(stat(cur, LIM, col));
       if (__builtin_amdgcn_ballot_w64(lo < kw + 32 && lim > kw && lim > lo) != 0) {
-        const bool some = __builtin_amdgcn_ballot_w64(lo > kw || lim < kw + 32) != 0;
-        auto row4 = [&](int which, int q) { return lds_read<f32x4>(stat(cur, which, 32 * rh + 8 * q + 4 * h)); };
+        auto row4 = [&](int which, int q) { return lds_read<f32x4>(stat(cur, which, 8 * q + 4 * h)); };
         f32x16 s, dp;
         if constexpr ((F & kCap) != 0) {
           zero(s);
@@ -378,50 +370,56 @@ __global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdPara
           }
         }
 #pragma unroll
-        for (int ds = 0; ds < 8; ++ds) s = mfma(tile_rows(qs, 32 * rh, col, h, ds), kf[ds], s);
-        __builtin_amdgcn_sched_barrier(0);
-        bf16x8 pf[2];
+        for (int ds = 0; ds < 8; ++ds) s = mfma(tile_rows(qs, 0, col, h, ds), kf[ds], s);
+        f32x16 sl;                     // a quarter of the cap's derivative
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          f32x4 z, sl;
           if constexpr ((F & kCap) != 0) {
-            const f32x4 lse = row4(LSE, q);
+            const f32x4 top = row4(LSE, q);   // cap log2 e - lse
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const Capped x = capped(s[4 * q + j], p.mask.cap_rate, p.mask.cap_log2);
-              z[j] = x.z - lse[j];
-              sl[j] = x.slope;
+              const float r = cap_r(s[4 * q + j], p.mask.cap_rate);
+              s[4 * q + j] = __builtin_fmaf(-2.0f * p.mask.cap_log2, r, top[j]);
+              sl[4 * q + j] = __builtin_fmaf(-r, r, r);
             }
           } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) z[j] = s[4 * q + j] * c;
+            for (int j = 0; j < 4; ++j) s[4 * q + j] *= c;
           }
           if constexpr ((F & kBias) != 0) {
             const f32x4 at = row4(POS, q), slope = row4(SLOPE, q);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) z[j] = __builtin_fmaf(-slope[j], __builtin_fabsf(at[j] - (float)kj), z[j]);
+            for (int j = 0; j < 4; ++j)
+              s[4 * q + j] = __builtin_fmaf(-slope[j], __builtin_fabsf(at[j] - (float)kj), s[4 * q + j]);
           }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) z[j] = __builtin_amdgcn_exp2f(z[j]);
-          if (some) {
+          for (int j = 0; j < 4; ++j) s[4 * q + j] = __builtin_amdgcn_exp2f(s[4 * q + j]);
+        }
+        if (by_id || __builtin_amdgcn_ballot_w64(lo > kw || lim < kw + 32) != 0) {   // some row does not see some key
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
             const f32x4 lo4 = row4(LO, q), lim4 = row4(LIM, q);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (kj < __builtin_bit_cast(int, (float)lo4[j]) || kj >= __builtin_bit_cast(int, (float)lim4[j])) z[j] = 0.0f;
+              if (kj < __builtin_bit_cast(int, (float)lo4[j]) || kj >= __builtin_bit_cast(int, (float)lim4[j])) s[4 * q + j] = 0.0f;
           }
           if (by_id) {
             const int doc = p.mask.k_docs[(int64_t)b * p.Sk + min(kj, m.klen - 1)];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int i = min(it * TR + 32 * rh + 8 * q + 4 * h + j, R - 1);
-              if (p.mask.q_docs[(int64_t)b * p.Sq + p.by_g.quot(i)] != doc) z[j] = 0.0f;
+            for (int v = 0; v < 16; ++v) {
+              const int i = min(it * QT + 8 * (v >> 2) + 4 * h + (v & 3), R - 1);
+              if (p.mask.q_docs[(int64_t)b * p.Sq + p.by_g.quot(i)] != doc) s[v] = 0.0f;
             }
           }
-          put2(pf[q >> 1], 4 * (q & 1), z[0], z[1]);
-          put2(pf[q >> 1], 4 * (q & 1) + 2, z[2], z[3]);
+        }
+        bf16x8 pf[2];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) s[4 * q + j] = (F & kCap) != 0 ? z[j] * sl[j] : z[j];
-          if constexpr ((F & (kCap | kBias)) != 0) __builtin_amdgcn_sched_barrier(0);
+        for (int v = 0; v < 16; v += 2) {
+          put2(pf[v >> 3], v & 7, s[v], s[v + 1]);
+          if constexpr ((F & kCap) != 0) {
+            s[v] *= sl[v];
+            s[v + 1] *= sl[v + 1];
+          }
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -430,62 +428,41 @@ __global__ __launch_bounds__(2 * NT, 2) void masked_bwd_dkv_kernel(MaskedBwdPara
           for (int j = 0; j < 4; ++j) dp[4 * q + j] = x[j];
         }
 #pragma unroll
-        for (int ds = 0; ds < 8; ++ds)
-          dp = mfma(tile_rows(gs, 32 * rh, col, h, ds), tile_rows(smem + vt, 0, col, h, ds), dp);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int ds = 0; ds < 8; ++ds) dp = mfma(tile_rows(gs, 0, col, h, ds), tile_rows(smem + vt, 0, col, h, ds), dp);
 #pragma unroll
         for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, 2 * rh + uu, d), pf[uu], dv[d]);
+          for (int d = 0; d < 4; ++d) dv[d] = mfma(tr.read(gs, uu, d), pf[uu], dv[d]);
 #pragma unroll
         for (int v = 0; v < 16; v += 2) put2(pf[v >> 3], v & 7, s[v] * dp[v], s[v + 1] * dp[v + 1]);
 #pragma unroll
         for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
-          for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, 2 * rh + uu, d), pf[uu], dk[d]);
+          for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, uu, d), pf[uu], dk[d]);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (it + 2 < it1) sstore(it + 2, nxt);
-      cur = cur == NS - 1 ? 0 : cur + 1;
+      if (it + 1 < it1) sstore(it + 1, cur ^ 1);
+      cur ^= 1;
     }
-    // The row halves are added: the first takes dK of both, the second dV.
-    __syncthreads();
-    f32x4* const box = (f32x4*)(smem + w * 16 * 64 * 16) + lane;
-    const f32x4* const other = (const f32x4*)(smem + (w ^ 4) * 16 * 64 * 16) + lane;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f32x4 x;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float k = dk[d][4 * q + j], v = dv[d][4 * q + j];
-          x[j] = rh == 0 ? v : k;
-          dk[d][4 * q + j] = rh == 0 ? k : v;                    // from here on the wave's own sum
-        }
-        box[(4 * d + q) * 64] = x;
-      }
-    __syncthreads();
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 x = other[(4 * d + q) * 64];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) dk[d][4 * q + j] += x[j];
-      }
-    __syncthreads();
+    __syncthreads();                   // the tiles' memory takes the rows
     if (kj >= m.klen) {   // a lane's key is its own column: what its sums hold goes nowhere else
 #pragma unroll
-      for (int d = 0; d < 4; ++d) zero(dk[d]);
+      for (int d = 0; d < 4; ++d) {
+        zero(dk[d]);
+        zero(dv[d]);
+      }
     }
   }
   const int rows = p.Sk - kw;
-  const float f = rh == 0 ? p.scale : 1.0f;
-  if (p.k_parts > 1)
-    store(smem, w, rh == 0 ? p.dKpart : p.dVpart, (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH, rows, dk, f, lane);
-  else
-    store(smem, w, rh == 0 ? p.dK : p.dV, tk * (rh == 0 ? p.lddk : p.lddv) + kvh * DH, rows, dk, f, lane);
+  const float f = (F & kCap) != 0 ? 4.0f * p.scale : p.scale;    // a quarter of the cap's derivative is in dS
+  if (p.k_parts > 1) {
+    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH;
+    store(smem, w, p.dKpart, at, rows, dk, f, lane);
+    store(smem, w, p.dVpart, at, rows, dv, 1.0f, lane);
+  } else {
+    store(smem, w, p.dK, tk * p.lddk + kvh * DH, rows, dk, f, lane);
+    store(smem, w, p.dV, tk * p.lddv + kvh * DH, rows, dv, 1.0f, lane);
+  }
 }
 
 constexpr int64_t kCUs = 256;
@@ -500,9 +477,9 @@ void launch_form(const MaskedBwdParams& p, CrossBwdPass pass, hipStream_t s) {
     const int64_t blocks = ((int64_t)p.Sk + KW - 1) / KW;
     const dim3 grid((unsigned)(blocks * nbh * p.k_parts));
     if (16 % p.G == 0)
-      hipLaunchKernelGGL((masked_bwd_dkv_kernel<true, F>), grid, dim3(2 * NT), 0, s, p);
+      hipLaunchKernelGGL((masked_bwd_dkv_kernel<true, F>), grid, dim3(NT), 0, s, p);
     else
-      hipLaunchKernelGGL((masked_bwd_dkv_kernel<false, F>), grid, dim3(2 * NT), 0, s, p);
+      hipLaunchKernelGGL((masked_bwd_dkv_kernel<false, F>), grid, dim3(NT), 0, s, p);
   }
 }
 
