@@ -12,13 +12,20 @@
 namespace partir {
 namespace {
 
-// The joined parts of a row, as cross_combine_kernel; every part of a row has its
-// statistics, and one without a key that the row sees weighs nothing.
+// The joined parts of a row: O = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - M), M =
+// max m_s; every part of a row has its statistics, and one without a key that the row
+// sees weighs nothing.  A row of 128 takes 32 threads, 4 columns each, in each of GRP
+// groups that share the parts (s = group, group + GRP, ..) and are added in order; 8 /
+// GRP rows a workgroup.  With two parts the eight groups of a row would idle but two:
+// 16288 rows 15 us so, 6 with one group a row.
+template <int GRP>
 __global__ __launch_bounds__(256) void masked_combine_kernel(MaskedParams p) {
+  constexpr int ROWS = 8 / GRP;
   __shared__ f32x4 acc_s[8][32];
   __shared__ float l_s[8];
-  const int64_t row = blockIdx.x, rows = (int64_t)p.B * p.Sq * p.Hq;
-  const int grp = threadIdx.x >> 5, c4 = threadIdx.x & 31;
+  const int64_t rows = (int64_t)p.B * p.Sq * p.Hq;
+  const int slot = threadIdx.x >> 5, grp = slot % GRP, c4 = threadIdx.x & 31;
+  const int64_t row = min((int64_t)blockIdx.x * ROWS + slot / GRP, rows - 1);   // the last one more than once
   const int64_t tq = row / p.Hq;
   const int head = (int)(row - tq * p.Hq);
   float M = kNoMax;
@@ -28,20 +35,22 @@ __global__ __launch_bounds__(256) void masked_combine_kernel(MaskedParams p) {
   float L = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-  for (int s = grp; s < p.nsplit; s += 8) {
+  for (int s = grp; s < p.nsplit; s += GRP) {
     const float2 ml = p.MLpart[s * rows + row];
     const float f = ml.y != 0.0f ? __builtin_amdgcn_exp2f(ml.x - M) : 0.0f;
     L += f * ml.y;
     acc += f * *(const f32x4*)(p.Opart + (s * rows + row) * DH + 4 * c4);
   }
-  acc_s[grp][c4] = acc;
-  if (c4 == 0) l_s[grp] = L;
-  __syncthreads();
-  if (grp > 0) return;
+  if constexpr (GRP > 1) {
+    acc_s[slot][c4] = acc;
+    if (c4 == 0) l_s[slot] = L;
+    __syncthreads();
+    if (grp > 0) return;
 #pragma unroll
-  for (int g = 1; g < 8; ++g) {
-    acc += acc_s[g][c4];
-    L += l_s[g];
+    for (int g = 1; g < GRP; ++g) {
+      acc += acc_s[slot + g][c4];
+      L += l_s[slot + g];
+    }
   }
   const bool seen = L != 0.0f;
   if (p.lse && c4 == 0) p.lse[row] = seen ? M + __builtin_amdgcn_logf(L) : -__builtin_inff();
@@ -159,7 +168,10 @@ hipError_t launch_masked_attention(const MaskedParams& p, int form, const CrossC
 
 hipError_t launch_masked_combine(const MaskedParams& p, hipStream_t s) {
   const int64_t rows = (int64_t)p.B * p.Sq * p.Hq;
-  hipLaunchKernelGGL(masked_combine_kernel, dim3((unsigned)rows), dim3(256), 0, s, p);
+  if (p.nsplit <= 4)
+    hipLaunchKernelGGL(masked_combine_kernel<1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL(masked_combine_kernel<8>, dim3((unsigned)rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -16,8 +16,9 @@
 // D.  rowsum(dO * O) has the rounding of O to bf16, which with few keys is of the size
 // of the other errors.  The dq pass starts from it, and adds the sum over its keys of
 // P (dP - D), which is what it was off by (the weights sum to 1), so that dkv takes D
-// with float32's error; where a workgroup's rows see 256 keys at most, two tiles' time
-// more give the dq pass itself that D.
+// with float32's error; where a wave's rows see 256 keys at most, some blocks' time
+// more give the dq pass itself that D.  (Error of dQ at 4 x 2048 tokens of documents of
+// 400 on average, of its size: 2.69e-3 with rowsum(dO * O) alone.)
 #include <algorithm>
 #include <type_traits>
 
@@ -28,6 +29,7 @@ namespace partir {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kFew = 256;
 
 template <int F>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -128,14 +130,44 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
       }
     }
   };
-  if (keys.y - keys.x <= 256) {
-    dsum = 0.0f;
-    for (int key = keys.x; key < keys.y; key += TR) {
-      const int64_t tk = (int64_t)b * p.Sk + key;
-      tile_load<TR, 4>(p.K + tk * p.ldk + kvh * DH, p.ldk, min(TR, m.klen - key), smem, w, lane);
-      tile_load<TR, 4>(p.V + tk * p.ldv + kvh * DH, p.ldv, min(TR, m.klen - key), smem + TILE, w, lane);
+  // Waves whose rows lie within 256 keys (kFew) take D from the weights themselves,
+  // in tiles that the workgroup loads for all of them.
+  const bool few = mask.lim1 - mask.lo0 <= kFew;
+  int* const spans = (int*)smem;
+  if (lane == 0) {
+    spans[2 * w] = few ? mask.lo0 & ~(TR - 1) : kNowhere;
+    spans[2 * w + 1] = few ? mask.lim1 : 0;
+  }
+  __syncthreads();
+  int few0 = kNowhere, few1 = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    few0 = min(few0, spans[2 * k]);
+    few1 = max(few1, spans[2 * k + 1]);
+  }
+  __syncthreads();
+  const int nkb = (range.end - range.begin + TR - 1) / TR;
+  // keys from `key` on into a stage; those behind the range's end are of rows without weight
+  auto gload = [&](int key, int buf) {
+    char* t = smem + buf * 2 * TILE;
+    const int64_t tk = (int64_t)b * p.Sk + key;
+    const int rows = min(TR, m.klen - key);
+    tile_load<TR, 4>(p.K + tk * p.ldk + kvh * DH, p.ldk, rows, t, w, lane);
+    tile_load<TR, 4>(p.V + tk * p.ldv + kvh * DH, p.ldv, rows, t + TILE, w, lane);
+  };
+  if (few0 < few1) {
+    if (few) dsum = 0.0f;
+    int buf = (few1 - few0 + TR - 1) / TR & 1;       // so that the first tile of the loop below is in stage 0
+    gload(few0, buf);
+    for (int key = few0; key < few1; key += TR, buf ^= 1) {
       WAIT_VMCNT(0);
       __syncthreads();
+      if (key + TR < few1)
+        gload(key + TR, buf ^ 1);
+      else if (nkb > 0)
+        gload(range.begin, 0);
+      if (!few) continue;
+      const char* ks = smem + buf * 2 * TILE;
 #pragma unroll 1
       for (int t = 0; t < 2; ++t) {
         if (mask.none(key + 32 * t, 32)) continue;
@@ -144,27 +176,19 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
         zero(dp);
 #pragma unroll
         for (int ds = 0; ds < 8; ++ds) {
-          s = mfma(tile_rows(smem, 32 * t, col, h, ds), qf[ds], s);
-          dp = mfma(tile_rows(smem + TILE, 32 * t, col, h, ds), gf[ds], dp);
+          s = mfma(tile_rows(ks, 32 * t, col, h, ds), qf[ds], s);
+          dp = mfma(tile_rows(ks + TILE, 32 * t, col, h, ds), gf[ds], dp);
         }
         weights(s, sl, key + 32 * t);
 #pragma unroll
         for (int v = 0; v < 16; ++v) dsum = __builtin_fmaf(s[v], dp[v], dsum);
       }
-      __syncthreads();
     }
+  } else if (nkb > 0) {
+    gload(range.begin, 0);
   }
   const float Dq = dsum + __shfl_xor(dsum, 32);
 
-  const uint16_t* kbase = p.K + ((int64_t)b * p.Sk + range.begin) * p.ldk + kvh * DH;
-  const uint16_t* vbase = p.V + ((int64_t)b * p.Sk + range.begin) * p.ldv + kvh * DH;
-  const int nkeys = range.end - range.begin, nkb = (nkeys + TR - 1) / TR;
-  auto gload = [&](int kb, int buf) {
-    char* t = smem + buf * 2 * TILE;
-    const int rows = min(TR, nkeys - kb * TR);
-    tile_load<TR, 4>(kbase + (int64_t)kb * TR * p.ldk, p.ldk, rows, t, w, lane);
-    tile_load<TR, 4>(vbase + (int64_t)kb * TR * p.ldv, p.ldv, rows, t + TILE, w, lane);
-  };
   f32x16 dq[4], nD;   // dP starts at -D: its first product reads it, where a subtraction would follow
 #pragma unroll
   for (int d = 0; d < 4; ++d) zero(dq[d]);
@@ -173,7 +197,7 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
   float off = 0.0f;   // sum of P (dP - D)
   auto iter = [&](int kb, auto stage) {
     constexpr int cur = decltype(stage)::value;
-    if (kb + 1 < nkb) gload(kb + 1, cur ^ 1);
+    if (kb + 1 < nkb) gload(range.begin + (kb + 1) * TR, cur ^ 1);
     const char* ks = smem + cur * 2 * TILE;
     const char* vs = ks + TILE;
 #pragma unroll
@@ -207,7 +231,6 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
     WAIT_VMCNT(0);
     __syncthreads();
   };
-  if (nkb > 0) gload(0, 0);
   WAIT_VMCNT(0);
   __syncthreads();
   for (int kb = 0; kb < nkb; kb += 2) {
@@ -413,6 +436,7 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
           }
         }
         bf16x8 pf[2];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int v = 0; v < 16; v += 2) {
           put2(pf[v >> 3], v & 7, s[v], s[v + 1]);
@@ -439,6 +463,7 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
         for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
           for (int d = 0; d < 4; ++d) dk[d] = mfma(tr.read(qs, uu, d), pf[uu], dk[d]);
+        __builtin_amdgcn_s_setprio(0);
       }
       __builtin_amdgcn_sched_barrier(0);
       if (it + 1 < it1) sstore(it + 1, cur ^ 1);
@@ -485,12 +510,32 @@ void launch_form(const MaskedBwdParams& p, CrossBwdPass pass, hipStream_t s) {
 
 }  // namespace
 
-CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk) {
-  const int64_t R = Hq / Hk * Sq, rows = (R + 63) / 64, keys = (Sk + 63) / 64;
-  auto most = [](int64_t grid, int64_t tiles) { return grid > 0 ? std::min(kCUs / grid, tiles) : 1; };
+// Parts of an axis whose `grid` workgroups take up to `steps` steps each, and `share`
+// of those on average: the longest workgroup, or all of them on the chip's two a compute
+// unit, whichever lasts longer; from two parts on a launch that adds them (5 us) and
+// part_us for the float32 rows of each, written and read.
+static int masked_parts(int64_t grid, int64_t steps, double share, double step_us, double part_us) {
+  if (grid <= 0 || steps <= 0) return 1;
+  const double all = (double)grid * (double)steps * share / (2.0 * kCUs);
+  int best = 1;
+  double least = std::max((double)steps, all) * step_us;
+  for (int64_t n = 2; n <= 64 && n <= steps; n *= 2) {
+    const double us = std::max((double)((steps + n - 1) / n), all) * step_us + 5.0 + (double)n * part_us;
+    if (us < least) {
+      least = us;
+      best = (int)n;
+    }
+  }
+  return best;
+}
+
+CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, bool causal) {
+  const int64_t R = Hq / Hk * Sq, rows = (R + QT - 1) / QT, keys = (Sk + TR - 1) / TR;
+  // a causal mask leaves half of the pairs where the queries are as many as the keys
+  const double share = causal && Sk > 0 ? 1.0 - 0.5 * (double)std::min(Sq, Sk) / (double)Sk : 1.0;
   const double q_us = 1.5e-4 * (double)(B * Sq * Hq), k_us = 2 * 1.5e-4 * (double)(B * Sk * Hk);
-  return {false, best_parts(most(B * Hk * ((R + 127) / 128), keys), keys, 1.45, q_us),
-          best_parts(most(B * Hk * ((Sk + KW - 1) / KW), rows), rows, 1.5, k_us)};
+  return {false, masked_parts(B * Hk * ((R + 127) / 128), keys, share, 1.45, q_us),
+          masked_parts(B * Hk * ((Sk + KW - 1) / KW), rows, share, 1.5, k_us)};
 }
 
 hipError_t launch_masked_backward(const MaskedBwdParams& p, int form, CrossBwdPass pass, hipStream_t s) {

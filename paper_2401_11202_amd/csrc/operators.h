@@ -181,7 +181,7 @@ struct CrossBwdChoice {
   int q_parts, k_parts;
 };
 CrossBwdChoice cross_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
-CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk);
+CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, int64_t Hk, bool causal);
 enum CrossBwdPass { CROSS_ALL, CROSS_DQ, CROSS_DKV };
 hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hipStream_t s);
 hipError_t launch_masked_backward(const MaskedBwdParams& p, int form, CrossBwdPass pass, hipStream_t s);

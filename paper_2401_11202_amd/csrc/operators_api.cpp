@@ -450,9 +450,9 @@ int run_masked(const void* Q, const void* K, const void* V, void* O, float* lse,
   return p.nsplit == 1 ? PARTIR_OK : launched(launch_masked_combine(p, s), "masked_combine");
 }
 
-CrossBwdPlan plan_masked_bwd(const CrossSizes& z) {
+CrossBwdPlan plan_masked_bwd(const CrossSizes& z, const partir_attention_mask& mask) {
   CrossBwdPlan p;
-  p.c = masked_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk);
+  p.c = masked_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk, mask.causal != 0);
   p.d_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * 4);
   if (p.c.q_parts > 1) p.q_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
   if (p.c.k_parts > 1) p.k_bytes = align_up((size_t)p.c.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
@@ -774,7 +774,7 @@ size_t partir_masked_attention_backward_workspace(int64_t B, int64_t Sq, int64_t
         return validate_cross(z);
       }))
     return (size_t)-1;
-  return B * (Sq + Sk) ? plan_docs(z, *mask).ws() + plan_masked_bwd(z).ws() : 0;
+  return B * (Sq + Sk) ? plan_docs(z, *mask).ws() + plan_masked_bwd(z, *mask).ws() : 0;
 }
 
 int partir_plan_masked_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int64_t n_heads, int64_t n_kv_heads,
@@ -783,7 +783,7 @@ int partir_plan_masked_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int
     const CrossSizes z{B, Sq, Sk, n_heads, n_kv_heads, d_head};
     if (int st = validate_cross(z)) return st;
     if (!mask || !info) return fail(PARTIR_E_NULL, "mask and info must be non-NULL");
-    const CrossBwdPlan p = plan_masked_bwd(z);
+    const CrossBwdPlan p = plan_masked_bwd(z, *mask);
     const size_t docs = plan_docs(z, *mask).ws();
     const int launches = (docs > 0) + (B * Sq ? 1 + (p.c.q_parts > 1) : 0) + (B * Sk ? 1 + (p.c.k_parts > 1) : 0);
     fill_info(info, std::max(p.c.q_parts, p.c.k_parts), launches, B * (Sq + Sk) ? docs + p.ws() : 0,
@@ -816,7 +816,7 @@ int partir_masked_attention_backward(const void* Q, const void* K, const void* V
     if (Tq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
     if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
     if (Tq == 0 && Tk == 0) return PARTIR_OK;
-    const CrossBwdPlan plan = plan_masked_bwd(z);
+    const CrossBwdPlan plan = plan_masked_bwd(z, *mask);
     const DocPlan docs = plan_docs(z, *mask);
     if (int st = check_ws(docs.ws() + plan.ws(), ws, ws_bytes)) return st;
     p.Q = (const uint16_t*)Q; p.K = (const uint16_t*)K; p.V = (const uint16_t*)V; p.O = (const uint16_t*)O;
