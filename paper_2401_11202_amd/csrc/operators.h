@@ -248,13 +248,14 @@ struct JoinParams {
   float scale;             // the factor of what dropout keeps included
   float eps;
   Dropout drop;
-  // who takes which rows (join_choice): waves of a row, workers (workgroups, or
-  // waves where a row is one wave's); backward: worker w takes `per` rows of span
-  // w / chunks, spans being a gate's row or several whole ones
-  int waves;
+  // Who takes which rows (join_choice): waves of a row.  Forward: workers (workgroups,
+  // or waves where a row is one wave's) take every workers-th.  Backward: `workers`
+  // workgroups of `teams` teams; with chunks > 0 a workgroup has `per` rows of span
+  // workgroup / chunks, spans being a gate's rows or all; else a team has `per` rows.
+  int waves, teams;
   int64_t workers, span, chunks, per;
   float *part_post, *part_pre, *part_gate;   // backward: [workers][D] sums, each may be NULL
-  float* dgate_rows;                         // backward: dgate itself, where a worker has whole gate rows
+  float* dgate_rows;                         // backward: dgate itself, where a team has whole gate rows
 };
 void join_choice(JoinParams& p, bool backward);
 hipError_t launch_join(const JoinParams& p, bool x_bf16, bool y_bf16, hipStream_t s);

@@ -13,7 +13,7 @@
 //
 // A row is one wave's up to 512 columns, else a workgroup's of as many waves as
 // it takes at 8 columns a lane (16 from 8192 columns on).  In the gradients a
-// workgroup (or wave) keeps its columns' sums over all of its rows in registers.
+// workgroup keeps its columns' sums over all of its rows in registers.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,7 +34,7 @@ __device__ __forceinline__ float wave_sum(float v) {
 // again has met everyone at the other's barrier, behind their reads of this one.
 struct RowSum {
   float (*red)[16][8];   // [2][wave][value]
-  int waves, wave, turn;
+  int waves, wave, turn, base;   // base: the first wave of the row
   template <int N>
   __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
@@ -49,7 +49,7 @@ struct RowSum {
     for (int i = 0; i < N; ++i) v[i] = 0.0f;
     for (int w = 0; w < waves; ++w)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += red[turn][w][i];
+      for (int i = 0; i < N; ++i) v[i] += red[turn][base + w][i];
     turn ^= 1;
   }
 };
@@ -99,17 +99,6 @@ __device__ __forceinline__ void store_row(void* p, int64_t off, const Columns<C>
     if (k.on[c]) Run<T, 8>::store((T*)p + off + k.at[c], v[c]);
 }
 
-// Worker (wave or workgroup) w takes rows [first, end), all of one gate's row or
-// whole gate rows.
-struct Rows {
-  int64_t first, end;
-  __device__ __forceinline__ Rows(const JoinParams& p, int64_t w) {
-    const int64_t group = w / p.chunks, chunk = w - group * p.chunks;
-    first = group * p.span + chunk * p.per;
-    end = min(min(first + p.per, (group + 1) * p.span), p.T);
-  }
-};
-
 template <typename TX, typename TY, int C>
 __global__ __launch_bounds__(1024) void join_kernel(JoinParams p) {
   __shared__ float red[2][16][8];
@@ -117,7 +106,7 @@ __global__ __launch_bounds__(1024) void join_kernel(JoinParams p) {
   const int64_t w = p.waves == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 6) + wave : blockIdx.x;
   if (w >= p.workers) return;                        // whole waves, and only where a row is one wave's
   const Columns<C> k(p, p.waves == 1 ? lane : (int)threadIdx.x);
-  RowSum sum{red, p.waves, wave, 0};
+  RowSum sum{red, p.waves, wave, 0, 0};
   Philox rng;
   if (p.drop.seed) rng.init(p.drop.seed);
   const float inv_d = 1.0f / (float)p.D;
@@ -165,29 +154,86 @@ __global__ __launch_bounds__(1024) void join_kernel(JoinParams p) {
   }
 }
 
-template <typename TX, typename TY, int C>
-__global__ __launch_bounds__(1024) void join_bwd_kernel(JoinParams p) {
+// A row as it is stored.
+template <typename T, int C>
+struct Raw {
+  typename Run<T, 8>::raw v[C];
+  __device__ __forceinline__ void load(const void* p, int64_t off, const Columns<C>& k) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (k.on[c]) v[c] = *(const typename Run<T, 8>::raw*)((const T*)p + off + k.at[c]);
+  }
+  __device__ __forceinline__ void get(const Columns<C>& k, float (&x)[C][8]) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[c][e] = k.on[c] ? (float)v[c][e] : 0.0f;
+  }
+};
+
+// The rows of a workgroup are shared out over its teams of p.waves waves.  Where a
+// gate's row has rows enough for a workgroup, or there is no gate, a workgroup has a
+// chunk of one gate's row and its teams take every teams-th row; else a team has
+// whole gate rows, and stores each one's gradient itself.  The teams' sums are added
+// in LDS, so that a workgroup leaves one partial row of each gradient.  A row's
+// loads go out before the sums of the row before are taken.
+template <typename TX, typename TY, int C, int MOST, bool POST, bool GATE>
+__global__ __launch_bounds__(MOST) void join_bwd_kernel(JoinParams p) {
   __shared__ float red[2][16][8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t w = p.waves == 1 ? (int64_t)blockIdx.x * (blockDim.x >> 6) + wave : blockIdx.x;
-  if (w >= p.workers) return;
-  const Columns<C> k(p, p.waves == 1 ? lane : (int)threadIdx.x);
-  RowSum sum{red, p.waves, wave, 0};
+  __shared__ __attribute__((aligned(16))) float acc[8][64][8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int team = wave / p.waves, in_team = wave - team * p.waves;
+  const Columns<C> k(p, 64 * in_team + lane);
+  RowSum sum{red, p.waves, wave, 0, team * p.waves};
   Philox rng;
   if (p.drop.seed) rng.init(p.drop.seed);
   const float inv_d = 1.0f / (float)p.D;
   const bool next = p.dn != nullptr;
+  // this team's rows: t0, t0 + step, .. below end; `turns` of them in every team of the workgroup
+  int64_t t0, end, step, turns;
+  if (p.chunks > 0) {
+    const int64_t group = blockIdx.x / p.chunks, first = group * p.span + (blockIdx.x - group * p.chunks) * p.per;
+    end = min(min(first + p.per, (group + 1) * p.span), p.T);
+    t0 = first + team;
+    step = p.teams;
+    turns = (p.per + p.teams - 1) / p.teams;
+  } else {
+    t0 = ((int64_t)blockIdx.x * p.teams + team) * p.per;
+    end = min(t0 + p.per, p.T);
+    step = 1;
+    turns = p.per;
+  }
   float gpost[C][8], gpre[C][8], gate[C][8], apost[C][8], apre[C][8], agate[C][8];
-  load_gain(p.g_post, k, 1.0f, gpost);
-  load_gain(p.g_pre, k, 1.0f, gpre);
+  // 16 columns a lane leave no room for a second row's loads and for the gains
+  constexpr bool AHEAD = C == 1;
+  auto gains = [&]() {
+    load_gain(p.g_post, k, 1.0f, gpost);
+    load_gain(p.g_pre, k, 1.0f, gpre);
+  };
+  if (AHEAD) gains();
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) apost[c][e] = apre[c][e] = agate[c][e] = 0.0f;
-  const Rows rows(p, w);
-  int64_t group = -1, group_end = rows.first;        // the gate's row that the sums are of, and where it ends
-  for (int64_t t = rows.first; t < rows.end; ++t) {
-    if (t >= group_end) {
+    for (int e = 0; e < 8; ++e) {
+      apost[c][e] = apre[c][e] = agate[c][e] = 0.0f;
+      gate[c][e] = 1.0f;
+    }
+  Raw<TX, C> rx, rdh;
+  Raw<TY, C> ry, rdn;
+  auto fetch = [&](int64_t t) {
+    ry.load(p.y, t * p.ldy, k);
+    if (next) {
+      rx.load(p.x, t * p.ldx, k);
+      rdn.load(p.dn, t * p.lddn, k);
+    }
+    if (p.dh) rdh.load(p.dh, t * p.lddh, k);
+  };
+  if (AHEAD && t0 < end) fetch(t0);
+  int64_t group = -1, group_end = t0;                // the gate's row that the sums are of, and where it ends
+  for (int64_t n = 0; n < turns; ++n) {
+    const int64_t t = t0 + n * step;
+    const bool live = t < end;                       // the same in a team, not in a workgroup
+    if (GATE && live && t >= group_end) {
       if (p.dgate_rows && group >= 0) {              // whole gate rows: each is stored where it belongs
         store_row<float>(p.dgate_rows, group * p.D, k, agate);
 #pragma unroll
@@ -197,15 +243,23 @@ __global__ __launch_bounds__(1024) void join_bwd_kernel(JoinParams p) {
       }
       group = t / p.gate_rows;
       group_end = (group + 1) * p.gate_rows;
-      load_gain(p.gate ? p.gate + group * p.ldgate : nullptr, k, 1.0f, gate);
+      if (AHEAD) load_gain(p.gate + group * p.ldgate, k, 1.0f, gate);
+    }
+    if (!AHEAD) {
+      if (live) fetch(t);
+      gains();
+      if (GATE && live) load_gain(p.gate + group * p.ldgate, k, 1.0f, gate);
     }
     float x[C][8], y[C][8], dh[C][8], v[C][8];
-    load_row<TY>(p.y, t * p.ldy, k, y);
-    if (next) load_row<TX>(p.x, t * p.ldx, k, x);
-    if (p.dh) load_row<TX>(p.dh, t * p.lddh, k, dh);
-    if (next) load_row<TY>(p.dn, t * p.lddn, k, v);
+    ry.get(k, y);
+    if (next) {
+      rx.get(k, x);
+      rdn.get(k, v);
+    }
+    if (p.dh) rdh.get(k, dh);
+    if (AHEAD && t + step < end) fetch(t + step);
     float r1 = 1.0f, r2 = 0.0f;
-    if (p.post) {
+    if constexpr (POST) {
       float s[1] = {0.0f};
 #pragma unroll
       for (int c = 0; c < C; ++c)
@@ -221,69 +275,87 @@ __global__ __launch_bounds__(1024) void join_bwd_kernel(JoinParams p) {
       if (p.drop.seed && k.on[c]) keep[c] = rng.keep8((uint32_t)k.at[c] >> 3, p.drop.row0 + (uint32_t)t, p.drop.kept);
     }
     // sums of h^2, h v, and of z dh, z v, z h with z = a g_post y
-    float s[5] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    float s[POST ? 5 : 2];
+#pragma unroll
+    for (int i = 0; i < (POST ? 5 : 2); ++i) s[i] = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (!p.dh) dh[c][e] = 0.0f;
-        const float z = keep[c] >> e & 1 ? p.scale * gate[c][e] * (p.post ? gpost[c][e] * y[c][e] : y[c][e]) : 0.0f;
+        const float z = keep[c] >> e & 1 ? p.scale * gate[c][e] * (POST ? gpost[c][e] * y[c][e] : y[c][e]) : 0.0f;
         if (next) {
           x[c][e] += z * r1;                         // h
           const float gv = gpre[c][e] * v[c][e];
           s[0] += x[c][e] * x[c][e];
           s[1] += x[c][e] * gv;
-          s[3] += z * gv;
-          s[4] += z * x[c][e];
+          if constexpr (POST) {
+            s[3] += z * gv;
+            s[4] += z * x[c][e];
+          }
         }
-        s[2] += z * dh[c][e];
+        if constexpr (POST) s[2] += z * dh[c][e];
       }
-    if (next || p.post) sum(s);
-    float m = 0.0f;
+    if (next || POST) sum(s);
+    float m = 0.0f, q = 0.0f;
     if (next) {
       r2 = rsqrtf(s[0] * inv_d + p.eps);
       m = r2 * r2 * (s[1] * inv_d);
     }
-    const float q = r1 * r1 * inv_d * (s[2] + r2 * (s[3] - m * s[4]));   // r1^2 mean(y g_post du)
+    if constexpr (POST) q = r1 * r1 * inv_d * (s[2] + r2 * (s[3] - m * s[4]));   // r1^2 mean(y g_post du)
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (next) {
-          apre[c][e] += v[c][e] * x[c][e] * r2;
+          if (live) apre[c][e] += v[c][e] * x[c][e] * r2;
           dh[c][e] += r2 * (gpre[c][e] * v[c][e] - x[c][e] * m);
         }
         const bool on = keep[c] >> e & 1;
         const float kept = on ? p.scale * dh[c][e] : 0.0f;
         const float yr = y[c][e] * r1, du = gate[c][e] * kept;
-        agate[c][e] += on ? kept * (p.post ? gpost[c][e] * yr : yr) : 0.0f;
-        if (p.post) {
-          apost[c][e] += du * yr;
+        if (GATE && live) agate[c][e] += on ? kept * (POST ? gpost[c][e] * yr : yr) : 0.0f;
+        if constexpr (POST) {
+          if (live) apost[c][e] += du * yr;
           y[c][e] = r1 * (gpost[c][e] * du - y[c][e] * q);
         } else {
           y[c][e] = du;
         }
       }
-    store_row<TX>(p.dx, t * p.lddx, k, dh);
-    store_row<TY>(p.dy, t * p.lddy, k, y);
+    if (live) {
+      store_row<TX>(p.dx, t * p.lddx, k, dh);
+      store_row<TY>(p.dy, t * p.lddy, k, y);
+    }
   }
-  if (p.dgate_rows) {
-    if (group >= 0) store_row<float>(p.dgate_rows, group * p.D, k, agate);
-  } else if (p.part_gate) {
-    store_row<float>(p.part_gate, w * p.D, k, agate);
-  }
-  if (p.part_post) store_row<float>(p.part_post, w * p.D, k, apost);
-  if (p.part_pre) store_row<float>(p.part_pre, w * p.D, k, apre);
+  if (GATE && p.dgate_rows && group >= 0) store_row<float>(p.dgate_rows, group * p.D, k, agate);
+  // the teams' sums, in order, into the workgroup's row of a matrix of parts
+  auto leave = [&](float* part, float (&a)[C][8]) {
+    if (!part) return;
+    if (p.teams > 1) {                               // C = 1
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[wave & 7][lane][e] = a[0][e];
+      __syncthreads();
+      if (team == 0)
+        for (int i = 1; i < p.teams; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[0][e] += acc[i * p.waves + in_team][lane][e];
+      __syncthreads();
+    }
+    if (team == 0) store_row<float>(part, (int64_t)blockIdx.x * p.D, k, a);
+  };
+  leave(p.part_post, apost);
+  leave(p.part_pre, apre);
+  if (p.chunks > 0) leave(p.part_gate, agate);
 }
 
 // out[o][d] = sum over parts [o * parts, (o + 1) * parts) of part[.][d], for the
-// matrices of a launch; 64 columns and 4 runs of the parts a workgroup, in order.
-__global__ __launch_bounds__(256) void join_reduce_kernel(JoinSums q) {
-  __shared__ float acc[4][64];
+// matrices of a launch; 64 columns and 16 runs of the parts a workgroup, in order.
+__global__ __launch_bounds__(1024) void join_reduce_kernel(JoinSums q) {
+  __shared__ float acc[16][64];
   int o = blockIdx.y, i = 0;
   while (o >= q.outs[i]) o -= q.outs[i++];
   const int d = blockIdx.x * 64 + (threadIdx.x & 63), run = threadIdx.x >> 6;
-  const int64_t parts = q.parts[i], per = (parts + 3) / 4;
+  const int64_t parts = q.parts[i], per = (parts + 15) / 16;
   float s = 0.0f;
   if (d < q.D) {
     const float* src = q.part[i] + (int64_t)o * parts * q.D + d;
@@ -293,8 +365,11 @@ __global__ __launch_bounds__(256) void join_reduce_kernel(JoinSums q) {
   }
   acc[run][threadIdx.x & 63] = s;
   __syncthreads();
-  if (run == 0 && d < q.D)
-    q.out[i][(int64_t)o * q.D + d] = (acc[0][threadIdx.x] + acc[1][threadIdx.x]) + (acc[2][threadIdx.x] + acc[3][threadIdx.x]);
+  if (run == 0 && d < q.D) {
+#pragma unroll
+    for (int r = 1; r < 16; ++r) s += acc[r][threadIdx.x];
+    q.out[i][(int64_t)o * q.D + d] = s;
+  }
 }
 
 constexpr int64_t kCUs = 256;
@@ -319,20 +394,24 @@ void join_choice(JoinParams& p, bool backward) {
     p.workers = std::min<int64_t>(p.T, 1 << 20);   // a launch is fewer than 2^32 threads
     return;
   }
-  // rows of a worker: two workgroups of 8 to 16 waves a CU, more of smaller ones
-  const int64_t slots = kCUs * std::max(1, 16 / p.waves);
+  // Workgroups of 8 to 16 waves, two a CU (one from 9 waves on); less than 4 rows a
+  // team only where there are fewer, since each leaves a row of partial sums.
+  p.teams = p.waves >= 5 ? 1 : 8 / p.waves;
+  const int64_t most = kCUs * (p.waves * p.teams > 8 ? 1 : 2);
   const int64_t span = std::min(p.gate_rows, p.T);
-  const int64_t per = std::max<int64_t>(1, (p.T + slots - 1) / slots);
-  if (span >= per) {                     // rows of one gate's row in chunks
+  const int64_t wgs = std::max<int64_t>(1, std::min<int64_t>(most, (p.T + 4 * p.teams - 1) / (4 * p.teams)));
+  const int64_t per = (p.T + wgs - 1) / wgs;
+  if (span >= per) {                     // a workgroup: a chunk of one gate's row
     p.span = span;
     p.chunks = (span + per - 1) / per;
     p.per = (span + p.chunks - 1) / p.chunks;
     p.chunks = (span + p.per - 1) / p.per;
     p.workers = (p.T + span - 1) / span * p.chunks;
-  } else {                               // whole gate rows
-    p.per = p.span = (per + span - 1) / span * span;
-    p.chunks = 1;
-    p.workers = (p.T + p.per - 1) / p.per;
+  } else {                               // a team: whole gate rows
+    const int64_t rows = (per + p.teams - 1) / p.teams;
+    p.per = p.span = (rows + span - 1) / span * span;
+    p.chunks = 0;
+    p.workers = (p.T + p.per * p.teams - 1) / (p.per * p.teams);
   }
 }
 
@@ -346,10 +425,23 @@ hipError_t launch_join(const JoinParams& p, bool x_bf16, bool y_bf16, hipStream_
 }
 
 hipError_t launch_join_backward(const JoinParams& p, bool x_bf16, bool y_bf16, hipStream_t s) {
-  const int64_t per = p.waves == 1 ? 4 : 1;
-  const dim3 grid((unsigned)((p.workers + per - 1) / per)), block((unsigned)(64 * (p.waves == 1 ? 4 : p.waves)));
+  const dim3 grid((unsigned)p.workers), block((unsigned)(64 * p.waves * p.teams));
   by_types(x_bf16, y_bf16, p.D > 8192, [&](auto x, auto y, auto c) {
-    hipLaunchKernelGGL((join_bwd_kernel<decltype(x), decltype(y), decltype(c)::value>), grid, block, 0, s, p);
+    auto go = [&](auto post, auto gate) {
+      constexpr int C = decltype(c)::value;
+      constexpr bool P = decltype(post)::value, G = decltype(gate)::value;
+      // up to 8 waves may take twice the registers that 16 may
+      if (C == 1 && p.waves * p.teams <= 8)
+        hipLaunchKernelGGL((join_bwd_kernel<decltype(x), decltype(y), 1, 512, P, G>), grid, block, 0, s, p);
+      else
+        hipLaunchKernelGGL((join_bwd_kernel<decltype(x), decltype(y), C, 1024, P, G>), grid, block, 0, s, p);
+    };
+    typedef std::true_type yes;
+    typedef std::false_type no;
+    if (p.post)
+      p.gate ? go(yes(), yes()) : go(yes(), no());
+    else
+      p.gate ? go(no(), yes()) : go(no(), no());
   });
   return hipGetLastError();
 }
@@ -357,7 +449,7 @@ hipError_t launch_join_backward(const JoinParams& p, bool x_bf16, bool y_bf16, h
 hipError_t launch_join_reduce(const JoinSums& q, hipStream_t s) {
   int64_t outs = 0;
   for (int i = 0; i < q.n; ++i) outs += q.outs[i];
-  hipLaunchKernelGGL(join_reduce_kernel, dim3((unsigned)((q.D + 63) / 64), (unsigned)outs), dim3(256), 0, s, q);
+  hipLaunchKernelGGL(join_reduce_kernel, dim3((unsigned)((q.D + 63) / 64), (unsigned)outs), dim3(1024), 0, s, q);
   return hipGetLastError();
 }
 

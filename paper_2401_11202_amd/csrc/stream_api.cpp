@@ -212,7 +212,7 @@ int partir_residual_norm_backward(const void* X, const void* Y, const void* dH, 
       q.part_pre = part + n;
       add(q.part_pre, dg_pre, 1, q.workers);
     }
-    if (dgate && q.chunks == 1) {
+    if (dgate && q.chunks == 0) {
       q.dgate_rows = dgate;
     } else if (dgate) {
       q.part_gate = part + 2 * n;
