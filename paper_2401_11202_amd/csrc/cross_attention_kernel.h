@@ -45,7 +45,11 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
   const int h = lane >> 5, col = lane & 31;
 
   int qb, bh, split = 0;
-  if (p.nsplit == 1 && (p.by_nbh.d & 7) == 0) {
+  bool by_head = p.nsplit == 1 && (p.by_nbh.d & 7) == 0;
+  // with documents a row block sees few keys, and all heads of a row block together
+  // read whole rows (4 x 2048 tokens, 32 heads, documents of 400 on average: 108 -> 93 us)
+  if constexpr (F != 0) by_head = by_head && !p.mask.rows;
+  if (by_head) {
     // Workgroup i runs on XCD i mod 8: an XCD takes one (sequence, key head)
     // after the other, whose K and V stay in its L2.
     const int j = blockIdx.x >> 3, n = p.by_nqb.quot(j);
@@ -170,18 +174,33 @@ __global__ __launch_bounds__(64 * QW * KG, OCC) void cross_attention_kernel(type
       kload(kb + KG * NS, cur);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr ((F & (kCap | kBias)) != 0) {
+    if constexpr ((F & kCap) != 0) {
+      float big = 0.0f;   // a NaN stays one in either form
+#pragma unroll
+      for (int t = 0; t < NSUB; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) big = fmaxf(big, __builtin_fabsf(sacc[t][v]));
+      if (__builtin_amdgcn_ballot_w64(big > p.mask.cap_small) == 0) {
+#pragma unroll
+        for (int t = 0; t < NSUB; ++t)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) sacc[t][v] = cap_small(sacc[t][v], p.mask);
+      } else {
+#pragma unroll
+        for (int t = 0; t < NSUB; ++t)
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            sacc[t][v] = __builtin_fmaf(-2.0f * p.mask.cap_log2, cap_r(sacc[t][v], p.mask.cap_rate), p.mask.cap_log2);
+      }
+    }
+    if constexpr ((F & kBias) != 0) {
       const float far = (float)(mask.pos - key0 - 4 * h);
 #pragma unroll
       for (int t = 0; t < NSUB; ++t)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          if constexpr ((F & kCap) != 0)
-            sacc[t][v] = __builtin_fmaf(-2.0f * p.mask.cap_log2, cap_r(sacc[t][v], p.mask.cap_rate), p.mask.cap_log2);
-          else
-            sacc[t][v] *= p.scale_log2;
-          if constexpr ((F & kBias) != 0)
-            sacc[t][v] = __builtin_fmaf(-slope, __builtin_fabsf(far - (float)(32 * t + 8 * (v >> 2) + (v & 3))), sacc[t][v]);
+          if constexpr ((F & kCap) == 0) sacc[t][v] *= p.scale_log2;
+          sacc[t][v] = __builtin_fmaf(-slope, __builtin_fabsf(far - (float)(32 * t + 8 * (v >> 2) + (v & 3))), sacc[t][v]);
         }
     }
     const int left = range.end - key0;   // keys from this block on

@@ -139,6 +139,7 @@ struct MaskArgs {
   int q_blocks;
   const float* slopes;                         // [Hq]
   float cap_log2, cap_rate;                    // cap log2 e, 2 scale log2 e / cap
+  float cap_small, cap_c[5];                   // largest |q k| of the polynomial, its coefficients in odd powers of q k
   int causal;
 };
 struct MaskedParams : CrossParams {

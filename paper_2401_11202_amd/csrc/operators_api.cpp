@@ -368,6 +368,12 @@ int resolve_mask(MaskArgs& m, int& form, const partir_attention_mask* mask, floa
     m.cap_log2 = mask->cap * kLog2e;
     m.cap_rate = 2.0f * scale * kLog2e / mask->cap;
     if (!(m.cap_rate > 1e-30f && m.cap_rate < 1e30f)) return fail(PARTIR_E_UNSUPPORTED, "scale / cap outside 1e-30 .. 1e30");
+    // tanh x = x (c0 + c1 x^2 + ..) up to x = 5 / 8, in powers of q k; with a scale / cap
+    // whose ninth power float32 does not hold the other form takes all
+    const double c[5] = {0.9999998917, -0.3333194271, 0.133043797, -0.05181591168, 0.01504335657};
+    const double x = (double)scale / mask->cap, a = (double)mask->cap * 1.4426950408889634;
+    m.cap_small = x > 0x1p-12 && x < 0x1p4 ? (float)(0.625 / x) : -1.0f;
+    for (int i = 0; i < 5; ++i) m.cap_c[i] = m.cap_small > 0.0f ? (float)(a * c[i] * std::pow(x, 2 * i + 1)) : 0.0f;
   }
   return PARTIR_OK;
 }
