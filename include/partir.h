@@ -640,7 +640,9 @@ typedef struct partir_attention_mask {
  * mask: HOST struct, read during the call.  Queries and keys behind their lens are
  * not read, whatever they hold.  What the lens leave must be finite: a masked key's
  * values are multiplied by 0.  Blocks of 64 keys that no query of a tile sees are
- * not read either: documents in one piece each cost what their own lengths do.
+ * not read either: documents in one piece each, up to 4096 of them, cost what their
+ * own lengths do (others are compared key by key).  z is formed in float32: a bias
+ * is off by 2^-23 of itself, a cap's tanh by 2^-20 of the cap.
  * Workspace: tables of the documents, and the parts as in partir_cross_attention.
  * Errors: as partir_cross_attention; E_NULL (mask, one of q_docs and k_docs),
  * E_UNSUPPORTED (cap, prefix_lens without causal), E_LAYOUT (O or lse overlaps an
@@ -675,7 +677,7 @@ size_t partir_masked_attention_backward_workspace(int64_t B, int64_t Sq, int64_t
 /* Dropout from a counter-based generator: Y = R + (kept ? X / share kept : 0).
  * X, Y: [T, D], R: [T, D] of Y's type or NULL (none); x_dtype and y_dtype F32 or
  * BF16 each, leading dims ldx, ldr, ldy.  Y may be X (pointer, type and leading dim
- * alike) or R, else it is apart from them.
+ * alike) or R, else it is apart from them and from the seed.
  * seed: two uint64 on the DEVICE, key and stream (a layer's number, a step's), read
  * when the call runs, so that a captured graph takes what they hold at its replay.
  * Element (t, d) is kept where the 16 bits that Philox 4x32 (Salmon et al., 2011;
@@ -698,7 +700,8 @@ int partir_dropout(const void* X, const void* R, void* Y, int64_t T, int64_t D, 
  *   H = X + scale * gate * dropout(U)
  *   N = g_pre * H / sqrt(mean(H^2) + eps)
  * X, H: [T, D] x_dtype; Y, N: [T, D] y_dtype (F32 or BF16 each); means are over the
- * D values of a row, in float32, N is taken from H before it is rounded.  H may be X
+ * D values of a row, in float32 (a row of zeros with eps = 0 gives NaN), N is taken
+ * from H before it is rounded.  H may be X
  * and N may be Y (pointer and leading dim alike), else they are apart from all
  * else.  N may be NULL: no next norm.
  * g_post, g_pre: [D] f32, or NULL: 1.  gate: [ceil(T / gate_rows), D] f32, leading

@@ -358,7 +358,7 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
         if (p.mask.rows) lim = min(lim, __builtin_bit_cast(int, x));
         x = __builtin_bit_cast(float, i < R ? lim : 0);
       }
-      if (which == POS) x = (float)(m.start + sq);
+      if (which == POS) x = (float)(m.start + sq - k0);   // from the first key on: exact where it matters
       if (which == SLOPE) x *= kLog2e;
       if (which < NSTAT) lds_write(stat(buf, which, col), x);
     };
@@ -416,7 +416,7 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
             const f32x4 at = row4(POS, q), slope = row4(SLOPE, q);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              s[4 * q + j] = __builtin_fmaf(-slope[j], __builtin_fabsf(at[j] - (float)kj), s[4 * q + j]);
+              s[4 * q + j] = __builtin_fmaf(-slope[j], __builtin_fabsf(at[j] - (float)(kj - k0)), s[4 * q + j]);
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[4 * q + j] = __builtin_amdgcn_exp2f(s[4 * q + j]);

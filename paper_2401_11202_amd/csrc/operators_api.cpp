@@ -348,19 +348,23 @@ PartSum part_sum(int n, int parts, int64_t rows, int64_t cols) {
 constexpr int kFormCap = 2, kFormBias = 4;   // bits of a kernel's form
 
 // The checks of a mask, and what the kernels take of it.
-int resolve_mask(MaskArgs& m, int& form, const partir_attention_mask* mask, float scale) {
+int resolve_mask(MaskArgs& m, int& form, const partir_attention_mask* mask, const CrossSizes& z, float scale) {
   if (!mask) return fail(PARTIR_E_NULL, "mask must be non-NULL");
   if (!(mask->cap == 0.0f || (mask->cap >= 0.0009765625f && mask->cap <= 1024.0f)))
     return fail(PARTIR_E_UNSUPPORTED, "cap must be 0 or within 2^-10 .. 2^10");
   if (mask->prefix_lens && !mask->causal) return fail(PARTIR_E_UNSUPPORTED, "prefix_lens without causal");
-  if (!mask->q_docs != !mask->k_docs) return fail(PARTIR_E_NULL, "q_docs and k_docs must be given together");
+  const bool pairs = z.B * z.Sq > 0 && z.B * z.Sk > 0;   // else one of the arrays is empty, and NULL perhaps
+  if (pairs && !mask->q_docs != !mask->k_docs) return fail(PARTIR_E_NULL, "q_docs and k_docs must be given together");
   const struct { const char* name; const void* p; } all[] = {
       {"slopes", mask->slopes}, {"k_lens", mask->k_lens}, {"q_lens", mask->q_lens}, {"q_starts", mask->q_starts},
       {"prefix_lens", mask->prefix_lens}, {"q_docs", mask->q_docs}, {"k_docs", mask->k_docs}};
   for (const auto& a : all)
     if (!aligned(a.p, 4)) return fail(PARTIR_E_LAYOUT, "%s must be 4-byte aligned", a.name);
   m.q_lens = mask->q_lens; m.q_starts = mask->q_starts; m.prefix = mask->prefix_lens;
-  m.q_docs = mask->q_docs; m.k_docs = mask->k_docs;
+  if (pairs) {
+    m.q_docs = mask->q_docs;
+    m.k_docs = mask->k_docs;
+  }
   m.slopes = mask->slopes;
   m.causal = mask->causal != 0;
   form = (mask->cap > 0.0f ? kFormCap : 0) | (mask->slopes ? kFormBias : 0);
@@ -386,7 +390,7 @@ struct DocPlan {
 };
 DocPlan plan_docs(const CrossSizes& z, const partir_attention_mask& mask) {
   DocPlan d;
-  if (!mask.k_docs || z.B * z.Sq == 0) return d;
+  if (!mask.k_docs || z.B * z.Sq == 0 || z.B * z.Sk == 0) return d;
   d.q_blocks = (int)cdiv(z.Sq, 64);
   d.row_bytes = align_up((size_t)z.B * z.Sq * 8);
   d.block_bytes = align_up((size_t)z.B * d.q_blocks * 8);
@@ -422,7 +426,7 @@ int run_masked(const void* Q, const void* K, const void* V, void* O, float* lse,
   if (int st = resolve_scale(scale, z.dh)) return st;
   MaskedParams p{};
   int form = 0;
-  if (int st = resolve_mask(p.mask, form, mask, scale)) return st;
+  if (int st = resolve_mask(p.mask, form, mask, z, scale)) return st;
   const int64_t Tq = z.B * z.Sq, Tk = z.B * z.Sk;
   const Matrix q{"Q", Q, Tq, z.Hq * z.dh, ldq, 2}, k{"K", K, Tq ? Tk : 0, z.Hk * z.dh, ldk, 2};
   const Matrix v{"V", V, Tq ? Tk : 0, z.Hk * z.dh, ldv, 2}, o{"O", O, Tq, z.Hq * z.dh, ldo, 2};
@@ -809,7 +813,7 @@ int partir_masked_attention_backward(const void* Q, const void* K, const void* V
     if (int st = resolve_scale(scale, d_head)) return st;
     MaskedBwdParams p{};
     int form = 0;
-    if (int st = resolve_mask(p.mask, form, mask, scale)) return st;
+    if (int st = resolve_mask(p.mask, form, mask, z, scale)) return st;
     const int64_t Tq = B * Sq, Tk = B * Sk, cq = n_heads * d_head, ck = n_kv_heads * d_head;
     const Matrix q{"Q", Q, Tq, cq, ldq, 2}, k{"K", K, Tk, ck, ldk, 2}, v{"V", V, Tk, ck, ldv, 2}, o{"O", O, Tq, cq, ldo, 2};
     const Matrix g{"dO", dO, Tq, cq, lddo, 2}, l{"lse", lse, Tq, n_heads, n_heads, 4};

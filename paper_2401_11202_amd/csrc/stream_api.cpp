@@ -99,7 +99,8 @@ int partir_dropout(const void* X, const void* R, void* Y, int64_t T, int64_t D, 
     for (const Matrix* m : {&x, &r, &y})
       if (int st = check(*m)) return st;
     if (T == 0 || D == 0) return PARTIR_OK;
-    if (int st = check_apart(y, &x, {})) return st;
+    const Matrix sd{"seed", seed, 1, 2, 2, 8};
+    if (int st = check_apart(y, &x, {&sd})) return st;
     if (int st = check_apart(y, &r, {})) return st;
     q.cols8 = (int)cdiv(D, 8);
     if (T * q.cols8 >= (int64_t)1 << 34) return fail(PARTIR_E_SHAPE, "more than 2^32 threads of a launch");

@@ -211,11 +211,27 @@ def test_capped_scores_at_their_ends():
     assert bool(((a.float() - b.float()).abs() <= 2.0 ** -6 * (1 + b.float().abs())).all())
 
 
+def test_far_positions():
+    """Queries millions of positions behind their keys: distances that float32 does not hold as two positions."""
+    run(2, 140, 140, 2, 1, dict(causal=False, slopes=[2.0 ** -20, -(2.0 ** -21)], q_starts=[2 ** 25 + 3, -(2 ** 26) + 5]), wid=13)
+
+
+def test_many_documents():
+    """As many documents as the list of runs holds, and one more."""
+    for n in (4096, 4097):
+        ids = np.arange(n)[::-1]
+        run(1, n, n, 1, 1, dict(q_docs=ids, k_docs=ids), wid=14, backward=False)
+    ids = np.arange(1500) // 2
+    run(1, 1500, 1500, 1, 1, dict(q_docs=ids, k_docs=ids), wid=15)
+
+
 def test_nothing_to_do():
     e = torch.zeros(0, 256, device="cuda", dtype=torch.bfloat16)
     x = torch.randn(6, 256, device="cuda").to(torch.bfloat16)
+    ids = torch.zeros(6, device="cuda", dtype=torch.int32)
     O, lse = P.masked_attention_train(x, e, e, B=2, Sq=3, Sk=0, n_heads=2)
     assert not O.any() and bool((lse == -math.inf).all())
+    assert not P.masked_attention(x, e, e, B=2, Sq=3, Sk=0, n_heads=2, q_docs=ids, k_docs=ids[:0]).any()
     dq, dk, dv = P.masked_attention_backward(x, e, e, O, x, lse, B=2, Sq=3, Sk=0, n_heads=2)
     assert not dq.any() and dk.shape == (0, 256)
     assert P.masked_attention(e, x, x, B=2, Sq=0, Sk=3, n_heads=2).shape == (0, 256)

@@ -114,6 +114,8 @@ def test_nothing_to_do():
     for empty in (dict(B=0), dict(Sq=0)):
         assert infer(Q=NULL, K=NULL, V=NULL, O=NULL, ws=NULL, wsb=0, **empty) == "PARTIR_OK"
     n = {k: NULL for k in ("Q", "K", "V", "O", "dO", "lse", "dQ", "dK", "dV", "ws")}
+    assert infer(Sq=0, k_docs=A, Q=NULL, O=NULL) == "PARTIR_OK"       # the array of no queries is NULL
+    assert infer(Sk=0, q_docs=A, K=NULL, V=NULL, ws=NULL, wsb=0) == "PARTIR_E_HIP"
     assert bwd(B=0, wsb=0, **n) == "PARTIR_OK" and bwd(Sq=0, Sk=0, wsb=0, **n) == "PARTIR_OK"
 
 

@@ -45,6 +45,7 @@ def drop(**kw):
     (dict(p=nan), "PARTIR_E_UNSUPPORTED"), (dict(xd=5), "PARTIR_E_DTYPE"), (dict(yd=-1), "PARTIR_E_DTYPE"),
     (dict(ldx=36), "PARTIR_E_LAYOUT"), (dict(ldx=44), "PARTIR_E_LAYOUT"), (dict(ldy=41), "PARTIR_E_LAYOUT"),
     (dict(X=ODD), "PARTIR_E_LAYOUT"), (dict(Y=ODD), "PARTIR_E_LAYOUT"), (dict(seed=ODD), "PARTIR_E_LAYOUT"),
+    (dict(Y=A[3]), "PARTIR_E_LAYOUT"), (dict(Y=at(A[3], -16)), "PARTIR_E_LAYOUT"),   # over the seed
     (dict(Y=A[0]), "PARTIR_E_LAYOUT"),                                   # X's place, another type
     (dict(Y=A[0], xd=P.F32, ldy=44), "PARTIR_E_LAYOUT"),                 # another leading dim
     (dict(Y=at(A[1], 16)), "PARTIR_E_LAYOUT"), (dict(Y=at(A[1], 15 * 160)), "PARTIR_E_LAYOUT"),
