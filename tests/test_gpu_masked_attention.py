@@ -219,7 +219,7 @@ def test_far_positions():
 def test_many_documents():
     """As many documents as the list of runs holds, and one more."""
     for n in (4096, 4097):
-        ids = np.arange(n)[::-1]
+        ids = n - np.arange(n)
         run(1, n, n, 1, 1, dict(q_docs=ids, k_docs=ids), wid=14, backward=False)
     ids = np.arange(1500) // 2
     run(1, 1500, 1500, 1, 1, dict(q_docs=ids, k_docs=ids), wid=15)
