@@ -216,6 +216,7 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
       }
       weights(s, sl, key0);
       bf16x8 dsf[2];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int v = 0; v < 16; v += 2) {
         float x = s[v] * dp[v], y = s[v + 1] * dp[v + 1];
@@ -230,6 +231,7 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
       for (int uu = 0; uu < 2; ++uu)
 #pragma unroll
         for (int d = 0; d < 4; ++d) dq[d] = mfma(tr.read(ks, 2 * t + uu, d), dsf[uu], dq[d]);
+      __builtin_amdgcn_s_setprio(0);
     }
     WAIT_VMCNT(0);
     __syncthreads();
