@@ -646,7 +646,7 @@ typedef struct partir_attention_mask {
  * Workspace: tables of the documents, and the parts as in partir_cross_attention.
  * Errors: as partir_cross_attention; E_NULL (mask, one of q_docs and k_docs),
  * E_UNSUPPORTED (cap, prefix_lens without causal), E_LAYOUT (O or lse overlaps an
- * input: O may be Q, with its leading dim). */
+ * input or an array of the mask: O may be Q, with its leading dim). */
 int partir_masked_attention(const void* Q, const void* K, const void* V, void* O, int64_t B, int64_t Sq, int64_t Sk,
                             int64_t n_heads, int64_t n_kv_heads, int64_t d_head, int64_t ldq, int64_t ldk, int64_t ldv,
                             int64_t ldo, const partir_attention_mask* mask, float scale, void* ws, size_t ws_bytes,

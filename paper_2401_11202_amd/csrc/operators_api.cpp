@@ -382,6 +382,16 @@ int resolve_mask(MaskArgs& m, int& form, const partir_attention_mask* mask, cons
   return PARTIR_OK;
 }
 
+// An output is apart from the mask's arrays: a length that changed during a launch
+// would send a workgroup's waves different ways.
+int check_mask_apart(const Matrix& out, const partir_attention_mask& m, const CrossSizes& z) {
+  const auto ints = [&](const char* name, const void* p, int64_t n) { return Matrix{name, p, p ? 1 : 0, n, n, 4}; };
+  const Matrix slopes = ints("slopes", m.slopes, z.Hq), k = ints("k_lens", m.k_lens, z.B), q = ints("q_lens", m.q_lens, z.B);
+  const Matrix at = ints("q_starts", m.q_starts, z.B), pre = ints("prefix_lens", m.prefix_lens, z.B);
+  const Matrix qd = ints("q_docs", m.q_docs, z.B * z.Sq), kd = ints("k_docs", m.k_docs, z.B * z.Sk);
+  return check_apart(out, nullptr, {&slopes, &k, &q, &at, &pre, &qd, &kd});
+}
+
 // The intervals of documents, at the front of the workspace.
 struct DocPlan {
   int q_blocks = 0;
@@ -438,6 +448,8 @@ int run_masked(const void* Q, const void* K, const void* V, void* O, float* lse,
   if (Tq == 0) return PARTIR_OK;
   if (int st = check_apart(o, &q, {&k, &v, &l})) return st;   // a workgroup holds its rows of Q before it stores those of O
   if (int st = check_apart(l, nullptr, {&q, &k, &v})) return st;
+  for (const Matrix* out : {&o, &l})
+    if (int st = check_mask_apart(*out, *mask, z)) return st;
   const CrossPlan plan = plan_cross(z);
   const DocPlan docs = plan_docs(z, *mask);
   if (int st = check_ws(docs.ws() + plan.ws(), ws, ws_bytes)) return st;
@@ -823,6 +835,8 @@ int partir_masked_attention_backward(const void* Q, const void* K, const void* V
     if (int st = check_apart(dq, nullptr, {&q, &k, &v, &o, &g, &l, &dk, &dv})) return st;
     if (int st = check_apart(dk, nullptr, {&q, &k, &v, &o, &g, &l, &dv})) return st;
     if (int st = check_apart(dv, nullptr, {&q, &k, &v, &o, &g, &l})) return st;
+    for (const Matrix* out : {&dq, &dk, &dv})
+      if (int st = check_mask_apart(*out, *mask, z)) return st;
     if (Tq > 0 && !lse) return fail(PARTIR_E_NULL, "lse must be non-NULL");
     if (!aligned(lse, 4)) return fail(PARTIR_E_LAYOUT, "lse must be 4-byte aligned");
     if (Tq == 0 && Tk == 0) return PARTIR_OK;

@@ -110,6 +110,22 @@ def test_backward_accepts(kw):
     assert bwd(**kw) == "PARTIR_E_HIP"
 
 
+ARRAYS = ("slopes", "k_lens", "q_lens", "q_starts", "prefix_lens", "q_docs", "k_docs")
+
+
+@pytest.mark.parametrize("name", ARRAYS)
+@pytest.mark.parametrize("out", ["O", "lse", "dQ", "dK", "dV"])
+def test_outputs_are_apart_from_the_masks_arrays(name, out):
+    """Behind the last array's end, and before the first, an output may lie."""
+    m = dict({n: A for n in ARRAYS if "docs" in n} if "docs" in name else {}, causal=1)
+    size = 4 * {"slopes": 4, "q_docs": 60, "k_docs": 1000}.get(name, 2)
+    fwd = out in ("O", "lse")
+    p = dict(FWD if fwd else BWD)[out]
+    go = train if fwd else bwd
+    for off, want in ((0, "PARTIR_E_LAYOUT"), (4 - size, "PARTIR_E_LAYOUT"), (-size, "PARTIR_E_HIP")):
+        assert go(**{**m, name: at(p, off)}) == want, off
+
+
 def test_nothing_to_do():
     for empty in (dict(B=0), dict(Sq=0)):
         assert infer(Q=NULL, K=NULL, V=NULL, O=NULL, ws=NULL, wsb=0, **empty) == "PARTIR_OK"
