@@ -71,75 +71,79 @@ __global__ __launch_bounds__(kDocThreads) void doc_rows_kernel(DocRows t) {
   __shared__ int wave_sum[17];
   __shared__ int in_pieces;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int chunks = (t.Sq + kDocThreads - 1) / kDocThreads, b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
-  const int klen = clamp_len(t.k_lens, b, t.Sk), qlen = clamp_len(t.q_lens, b, t.Sq);
-  const int32_t* kd = t.k_docs + (int64_t)b * t.Sk;
-  // starts of runs among this thread's keys, and how many lie before them
-  const int per = (klen + kDocThreads - 1) / kDocThreads;
-  const int j0 = min(tid * per, klen), j1 = min(j0 + per, klen);
-  int count = 0;
-  for (int j = j0; j < j1; ++j) count += j == 0 || kd[j] != kd[j - 1];
-  int before = count;
+  const int chunks = (t.Sq + kDocThreads - 1) / kDocThreads;
+  for (int64_t job = blockIdx.x; job < (int64_t)chunks * t.B; job += gridDim.x) {
+    const int b = (int)(job / chunks), chunk = (int)(job - (int64_t)b * chunks);
+    const int klen = clamp_len(t.k_lens, b, t.Sk), qlen = clamp_len(t.q_lens, b, t.Sq);
+    const int32_t* kd = t.k_docs + (int64_t)b * t.Sk;
+    // starts of runs among this thread's keys, and how many lie before them
+    const int per = (klen + kDocThreads - 1) / kDocThreads;
+    const int j0 = min(tid * per, klen), j1 = min(j0 + per, klen);
+    int count = 0;
+    for (int j = j0; j < j1; ++j) count += j == 0 || kd[j] != kd[j - 1];
+    int before = count;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(before, o);
-    if (lane >= o) before += x;
-  }
-  if (lane == 63) wave_sum[wave] = before;
-  if (tid == 0) in_pieces = 0;
-  __syncthreads();
-  int runs = 0, base = 0;
-  for (int w = 0; w < kDocThreads / 64; ++w) {
-    if (w == wave) base = runs;
-    runs += wave_sum[w];
-  }
-  before += base - count;
-  const bool listed = runs <= kRuns;   // the same in every thread
-  if (listed) {
-    for (int j = j0; j < j1; ++j)
-      if (j == 0 || kd[j] != kd[j - 1]) {
-        id[before] = kd[j];
-        first[before++] = j;
-      }
-    if (tid == 0) first[runs] = klen;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(before, o);
+      if (lane >= o) before += x;
+    }
+    if (lane == 63) wave_sum[wave] = before;
+    if (tid == 0) in_pieces = 0;
     __syncthreads();
-    for (int r = tid; r < runs; r += kDocThreads) {
-      const int mine = id[r];
-      bool twice = false;
-      for (int k = 0; k < runs; ++k) twice |= id[k] == mine && k != r;
-      if (twice) in_pieces = 1;
+    int runs = 0, base = 0;
+    for (int w = 0; w < kDocThreads / 64; ++w) {
+      if (w == wave) base = runs;
+      runs += wave_sum[w];
     }
-  } else if (tid == 0) {
-    in_pieces = 1;
-  }
-  __syncthreads();
-  const bool by_id = in_pieces != 0;
-  if (chunk == 0 && tid == 0) t.by_id[b] = by_id;
-  const int s = chunk * kDocThreads + tid;
-  int2 e = make_int2(0, 0);
-  if (s < qlen) {
-    if (by_id) {
-      e = make_int2(0, klen);
-    } else if (runs > 0) {
-      const int mine = t.q_docs[(int64_t)b * t.Sq + s];
-      int a = 0, z = runs;             // the run that holds position s, if any does
-      while (z - a > 1) {
-        const int mid = (a + z) >> 1;
-        (first[mid] <= s ? a : z) = mid;
+    before += base - count;
+    const bool listed = runs <= kRuns;   // the same in every thread
+    if (listed) {
+      for (int j = j0; j < j1; ++j)
+        if (j == 0 || kd[j] != kd[j - 1]) {
+          id[before] = kd[j];
+          first[before++] = j;
+        }
+      if (tid == 0) first[runs] = klen;
+      __syncthreads();
+      for (int r = tid; r < runs; r += kDocThreads) {
+        const int mine = id[r];
+        bool twice = false;
+        for (int k = 0; k < runs; ++k) twice |= id[k] == mine && k != r;
+        if (twice) in_pieces = 1;
       }
-      if (id[a] != mine)
-        for (a = 0; a < runs && id[a] != mine; ++a) {}
-      if (a < runs) e = make_int2(first[a], first[a + 1]);
+    } else if (tid == 0) {
+      in_pieces = 1;
     }
-  }
-  if (s < t.Sq) t.rows[(int64_t)b * t.Sq + s] = e;
-  int lo = e.y > e.x ? e.x : kNowhere, hi = e.y;
+    __syncthreads();
+    const bool by_id = in_pieces != 0;
+    if (chunk == 0 && tid == 0) t.by_id[b] = by_id;
+    const int s = chunk * kDocThreads + tid;
+    int2 e = make_int2(0, 0);
+    if (s < qlen) {
+      if (by_id) {
+        e = make_int2(0, klen);
+      } else if (runs > 0) {
+        const int mine = t.q_docs[(int64_t)b * t.Sq + s];
+        int a = 0, z = runs;             // the run that holds position s, if any does
+        while (z - a > 1) {
+          const int mid = (a + z) >> 1;
+          (first[mid] <= s ? a : z) = mid;
+        }
+        if (id[a] != mine)
+          for (a = 0; a < runs && id[a] != mine; ++a) {}
+        if (a < runs) e = make_int2(first[a], first[a + 1]);
+      }
+    }
+    if (s < t.Sq) t.rows[(int64_t)b * t.Sq + s] = e;
+    int lo = e.y > e.x ? e.x : kNowhere, hi = e.y;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    lo = min(lo, __shfl_xor(lo, o));
-    hi = max(hi, __shfl_xor(hi, o));
+    for (int o = 32; o >= 1; o >>= 1) {
+      lo = min(lo, __shfl_xor(lo, o));
+      hi = max(hi, __shfl_xor(hi, o));
+    }
+    if (lane == 0 && s < t.Sq) t.blocks[(int64_t)b * t.q_blocks + (s >> 6)] = make_int2(lo, hi);
+    __syncthreads();                   // the next sequence takes the same memory
   }
-  if (lane == 0 && s < t.Sq) t.blocks[(int64_t)b * t.q_blocks + (s >> 6)] = make_int2(lo, hi);
 }
 
 template <int F>
@@ -177,7 +181,8 @@ hipError_t launch_masked_combine(const MaskedParams& p, hipStream_t s) {
 
 hipError_t launch_doc_rows(const DocRows& t, hipStream_t s) {
   const int64_t chunks = ((int64_t)t.Sq + kDocThreads - 1) / kDocThreads;
-  hipLaunchKernelGGL(doc_rows_kernel, dim3((unsigned)(chunks * t.B)), dim3(kDocThreads), 0, s, t);
+  const int64_t grid = std::min<int64_t>(chunks * t.B, 1 << 20);   // a launch is fewer than 2^32 threads
+  hipLaunchKernelGGL(doc_rows_kernel, dim3((unsigned)grid), dim3(kDocThreads), 0, s, t);
   return hipGetLastError();
 }
 

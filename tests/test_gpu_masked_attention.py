@@ -225,6 +225,27 @@ def test_many_documents():
     run(1, 1500, 1500, 1, 1, dict(q_docs=ids, k_docs=ids), wid=15)
 
 
+def test_very_many_sequences():
+    """More sequences than a launch has workgroups of 1024 threads.  One key: a query
+    that sees it has weight 1, so O = V and dV = dO in every bit; dS = P (dP - D) is 0
+    but for the errors of P and D, 2^-20 each of dP, and |dP| <= 128 * 6^2 with values
+    up to 6."""
+    B = 2 ** 22 + 3
+    say(f"masked_attention B={B}")
+    torch.manual_seed(0)
+    Q, K, V, dO = (torch.randn(B, DH, device="cuda", dtype=torch.bfloat16).clamp_(-6, 6) for _ in range(4))
+    kd = torch.arange(B, device="cuda", dtype=torch.int32)
+    seen = kd % 3 != 1
+    qd = torch.where(seen, kd, kd + 1)
+    kw = dict(B=B, Sq=1, Sk=1, n_heads=1, q_docs=qd, k_docs=kd)
+    O, lse = P.masked_attention_train(Q, K, V, **kw)
+    assert torch.equal(O, V * seen[:, None]) and torch.equal(lse[:, 0] == -math.inf, ~seen)
+    dq, dk, dv = P.masked_attention_backward(Q, K, V, O, dO, lse, **kw)
+    assert torch.equal(dv, dO * seen[:, None])
+    for g in (dq, dk):
+        assert not g[~seen].any() and float(g.abs().max()) <= 2 * 2.0 ** -20 * (DH * 36) * 6 * DH ** -0.5
+
+
 def test_nothing_to_do():
     e = torch.zeros(0, 256, device="cuda", dtype=torch.bfloat16)
     x = torch.randn(6, 256, device="cuda").to(torch.bfloat16)
