@@ -68,9 +68,11 @@ class PlanInfo(ctypes.Structure):
         return {f: getattr(self, f) for f, _ in self._fields_ if f != "reserved"}
 
 
+MASK_TENSORS = ("slopes", "k_lens", "q_lens", "q_starts", "prefix_lens", "q_docs", "k_docs")
+
+
 class AttentionMask(ctypes.Structure):
-    _fields_ = [("causal", ctypes.c_int), ("cap", ctypes.c_float),
-                *((n, ctypes.c_void_p) for n in ("slopes", "k_lens", "q_lens", "q_starts", "prefix_lens", "q_docs", "k_docs"))]
+    _fields_ = [("causal", ctypes.c_int), ("cap", ctypes.c_float), *((n, ctypes.c_void_p) for n in MASK_TENSORS)]
 
 
 class TraceEntry(ctypes.Structure):
@@ -1152,17 +1154,14 @@ def _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal, cap, s
                  prefix_lens, q_docs, k_docs):
     """Checked sizes of a masked attention call, its mask and the mask's tensors."""
     Hk, Tq, Tk, ldq, ldk, ldv = _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens)
-    i32 = _torch.int32
-    _opt(slopes, "slopes", (n_heads,), _torch.float32)
-    _opt(q_lens, "q_lens", (B,), i32)
-    _opt(q_starts, "q_starts", (B,), i32)
-    _opt(prefix_lens, "prefix_lens", (B,), i32)
-    _opt(q_docs, "q_docs", (Tq,), i32)
-    _opt(k_docs, "k_docs", (Tk,), i32)
-    mask = AttentionMask(bool(causal), float(cap), _ptr(slopes), _ptr(k_lens), _ptr(q_lens), _ptr(q_starts), _ptr(prefix_lens),
-                         _ptr(q_docs), _ptr(k_docs))
-    tensors = (("slopes", slopes), ("k_lens", k_lens), ("q_lens", q_lens), ("q_starts", q_starts),
-               ("prefix_lens", prefix_lens), ("q_docs", q_docs), ("k_docs", k_docs))
+    tensors = (slopes, k_lens, q_lens, q_starts, prefix_lens, q_docs, k_docs)
+    mask = AttentionMask(bool(causal), float(cap))
+    if not (slopes is k_lens is q_lens is q_starts is prefix_lens is q_docs is k_docs is None):
+        _opt(slopes, "slopes", (n_heads,), _torch.float32)
+        shapes = (B,), (B,), (B,), (Tq,), (Tk,)
+        for name, t, shape in zip(MASK_TENSORS[2:], tensors[2:], shapes):
+            _opt(t, name, shape, _torch.int32)
+        mask = AttentionMask(bool(causal), float(cap), *map(_ptr, tensors))
     return Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors
 
 
@@ -1200,7 +1199,8 @@ def _masked_forward(Q, K, V, scale, out, lse, train, workspace, stream, B, Sq, S
     if not fresh_o:
         ldo = _matrix(out, "out", Tq, n_heads * d_head, torch.bfloat16)
     _opt(lse, "lse", (Tq, n_heads), torch.float32)
-    _same_device(("Q", Q), ("K", K), ("V", V), *tensors, ("out", out), ("lse", lse))
+    if not _one_gpu(Q, K, V, out, lse, *tensors):
+        _gpu_all(Q=Q, K=K, V=V, **dict(zip(MASK_TENSORS, tensors)), out=out, lse=lse)
     dev = Q.device
     if fresh_o:
         out = Q.new_empty((Tq, n_heads * d_head))
@@ -1236,8 +1236,8 @@ def masked_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, 
         if len(out) != 3:
             _bad("PARTIR_E_SHAPE", "out must hold (dQ, dK, dV)")
         lds = (_matrix(out[0], "dQ", Tq, cq, bf), _matrix(out[1], "dK", Tk, ck, bf), _matrix(out[2], "dV", Tk, ck, bf))
-    _same_device(("Q", Q), ("K", K), ("V", V), ("O", O), ("dO", dO), ("lse", lse), *tensors,
-                 *(() if fresh else zip(("dQ", "dK", "dV"), out)))
+    if not _one_gpu(Q, K, V, O, dO, lse, *tensors, *(() if fresh else out)):
+        _gpu_all(Q=Q, K=K, V=V, O=O, dO=dO, lse=lse, **dict(zip(MASK_TENSORS, tensors)), out=out)
     dev = Q.device
     if fresh:
         out = (Q.new_empty((Tq, cq)), Q.new_empty((Tk, ck)), Q.new_empty((Tk, ck)))
@@ -1289,12 +1289,6 @@ def _pitch(cols, dtype):
     return -(-cols // 8) * 8 if dtype is _torch.bfloat16 else -(-cols // 4) * 4
 
 
-def _same_device(first, *ts):
-    """A call's tensors (None left out) on one GPU."""
-    if not _one_gpu(first[1], *(t for _, t in ts)):
-        _gpu_all(**dict((first, *ts)))
-
-
 def dropout(X, p: float, seed, *, residual=None, row0: int = 0, out_dtype=None, out=None, stream=None):
     """Dropout of X [T, D] (f32 or bf16, a view with a leading dim allowed), on top of
     `residual` if given: residual + (kept ? X / share kept : 0), of out_dtype
@@ -1315,7 +1309,8 @@ def dropout(X, p: float, seed, *, residual=None, row0: int = 0, out_dtype=None, 
     fresh = out is None
     if not fresh:
         ldo = _matrix(out, "out", T, D, out_dtype)
-    _same_device(("X", X), ("seed", seed), ("residual", residual), ("out", out))
+    if not _one_gpu(X, seed, residual, out):
+        _gpu_all(X=X, seed=seed, residual=residual, out=out)
     wide = _pitch(D, out_dtype)
     if fresh:
         out, ldo = X.new_empty((T, wide), dtype=out_dtype), wide
@@ -1366,8 +1361,8 @@ def residual_norm(X, Y, *, g_post=None, post_norm: bool = False, gate=None, gate
     fresh_h, fresh_n = out is None, next_norm and norm_out is None
     ldh = D if fresh_h else _matrix(out, "out", T, D, X.dtype)
     ldn = D if norm_out is None else _matrix(norm_out, "norm_out", T, D, Y.dtype)
-    _same_device(("Y", Y), ("X", X), ("g_post", g_post), ("gate", gate), ("g_pre", g_pre), ("seed", seed), ("out", out),
-                 ("norm_out", norm_out))
+    if not _one_gpu(Y, X, g_post, gate, g_pre, seed, out, norm_out):
+        _gpu_all(Y=Y, X=X, g_post=g_post, gate=gate, g_pre=g_pre, seed=seed, out=out, norm_out=norm_out)
     if fresh_h:
         out = X.new_empty((T, D))
     if fresh_n:
@@ -1415,9 +1410,8 @@ def residual_norm_backward(X, Y, dH, dN, *, g_post=None, post_norm: bool = False
             if t is not None and shape is None:
                 _bad("PARTIR_E_UNSUPPORTED", f"{name} without its operand")
             _opt(t, name, shape, f32)
-    _same_device(("Y", Y), ("X", X), ("dH", dH), ("dN", dN), ("g_post", g_post), ("gate", gate), ("g_pre", g_pre),
-                 ("seed", seed), *(() if fresh else (("dX", out[0]), ("dY", out[1]))),
-                 *(() if fresh_g else zip(("dg_post", "dgate", "dg_pre"), gain_out)))
+    if not _one_gpu(Y, X, dH, dN, g_post, gate, g_pre, seed, *(() if fresh else out), *(() if fresh_g else gain_out)):
+        _gpu_all(Y=Y, X=X, dH=dH, dN=dN, g_post=g_post, gate=gate, g_pre=g_pre, seed=seed, out=out, gain_out=gain_out)
     dev = Y.device
     if fresh:
         out = (X.new_empty((T, D)), Y.new_empty((T, D)))
