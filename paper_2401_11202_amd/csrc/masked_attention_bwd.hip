@@ -313,9 +313,12 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
     if (hi >= 0) tiles = min(tiles, (int)(((int64_t)64 * (hi + 1) * p.G + QT - 1) / QT));
   }
   first = min(first, tiles);
-  const int per = p.by_k_parts.quot(tiles - first + p.k_parts - 1);
-  const int it0 = min(tiles, first + part * per), it1 = min(tiles, it0 + per);
-  if (it0 < it1) {                                               // workgroup-uniform
+  // From the last rows down, the parts in turn: under a causal mask the workgroups of a
+  // key head end at different rows, but start at the same, and find them in the L2 (2 x
+  // 4096 tokens, 32 / 8 heads, capped: 686 -> 671 us; upwards, in contiguous parts, 2.1
+  // GB came from behind the L2).
+  const int it0 = tiles - 1 - part, step = p.k_parts;
+  if (it0 >= first) {                                               // workgroup-uniform
     tile_load<KW, 4>(p.V + ((int64_t)b * p.Sk + k0) * p.ldv + kvh * DH, p.ldv, m.klen - k0, smem + VT, w, lane);
     bf16x8 kf[8];
     {
@@ -373,12 +376,12 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
     // of them back from memory a tile.)
     int cur = 0, vt = VT + 32 * w * ROWB;
 #pragma unroll 1
-    for (int it = it0; it < it1; ++it) {
+    for (int it = it0; it >= first; it -= step) {
       asm volatile("" : "+s"(vt));     // V's addresses are formed here
       __builtin_amdgcn_sched_barrier(0);
       WAIT_VMCNT(0);
       lds_barrier();                   // everyone's tile has landed, and everyone is done with the stage loaded next
-      if (it + 1 < it1) gload(it + 1, cur ^ 1);
+      if (it - step >= first) gload(it - step, cur ^ 1);
       __builtin_amdgcn_sched_barrier(0);
       const char* qs = smem + cur * STAGE;
       const char* gs = qs + QT * ROWB;
@@ -471,7 +474,7 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
         __builtin_amdgcn_s_setprio(0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (it + 1 < it1) sstore(it + 1, cur ^ 1);
+      if (it - step >= first) sstore(it - step, cur ^ 1);
       cur ^= 1;
     }
     __syncthreads();                   // the tiles' memory takes the rows
