@@ -187,6 +187,14 @@ def test_grids_without_parts(B, S, Hq, Hk, f):
     run(B, S, S, Hq, Hk, dict(form(f, Hq), q_docs=ids, k_docs=ids), wid=S)
 
 
+@pytest.mark.parametrize("B,S,Hq,Hk", [(33, 130, 8, 8), (43, 97, 9, 3), (65, 161, 4, 4)])
+@pytest.mark.parametrize("f", [{}, *FORMS])
+def test_many_short_sequences(B, S, Hq, Hk, f):
+    """The kernels of many workgroups in every form, without documents, on ragged batches."""
+    lens = [S - (37 * b) % (S + 1) for b in range(B)]
+    run(B, S, S, Hq, Hk, dict(form(f, Hq), k_lens=lens, q_lens=lens), wid=S)
+
+
 @pytest.mark.parametrize("scale,qscale", [(1.0, 1.0), (0.02, 1.0), (1.0, 4.0)])
 @pytest.mark.parametrize("cap", [0.0, 30.0])
 def test_scales_from_flat_to_one_hot(scale, qscale, cap):
