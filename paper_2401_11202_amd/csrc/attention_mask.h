@@ -19,15 +19,18 @@ namespace partir {
 
 constexpr int kMasked = 1, kCap = 2, kBias = 4;
 constexpr int kNowhere = 2147483647;   // lo of a row that sees no key
+constexpr float kLog2e = 1.4426950408889634f;
 
-// What the forward kernel of form F takes.
+// What the forward and gradient kernels of form F take.
 template <int F>
 struct FormParams {
   typedef MaskedParams fwd;
+  typedef MaskedBwdParams bwd;
 };
 template <>
 struct FormParams<0> {
   typedef CrossParams fwd;
+  typedef CrossBwdParams bwd;
 };
 
 __device__ __forceinline__ int clamp_len(const int32_t* lens, int b, int most) {
@@ -76,11 +79,14 @@ struct RowMask {
   int lo0, lo1, lim0, lim1;  // least and largest of the wave's
   int pos;                   // the row's position
   template <typename P>
-  __device__ __forceinline__ RowMask(const P& p, const SeqMask& m, int64_t tq, int s) {
+  __device__ __forceinline__ RowMask(const P& p, const SeqMask& m, int64_t tq, int s)
+      : RowMask(m, p.mask.rows != nullptr, p.mask.rows ? p.mask.rows[tq] : make_int2(0, 0), s) {}
+  // e: where there are documents, the keys of the row's
+  __device__ __forceinline__ RowMask(const SeqMask& m, bool docs, int2 e, int s) {
     pos = m.start + s;
     lo = 0;
     lim = s < m.qlen ? m.lim(s) : 0;
-    if (!p.mask.rows) {      // the rows ascend, and so do their limits
+    if (!docs) {             // the rows ascend, and so do their limits
       if (lim <= 0) lo = kNowhere;
       lo0 = 0;
       lo1 = __builtin_amdgcn_readlane(lo, 0);
@@ -88,7 +94,6 @@ struct RowMask {
       lim1 = __builtin_amdgcn_readlane(lim, 31);
       return;
     }
-    const int2 e = p.mask.rows[tq];
     lo = e.x;
     lim = min(lim, e.y);
     if (lim <= lo) {
@@ -136,5 +141,50 @@ __device__ __forceinline__ float cap_small(float s, const MaskArgs& m) {
   p = __builtin_fmaf(u, p, m.cap_c[0]);
   return s * p;
 }
+
+// The weights P = 2^(z - lse) of a row, and with a cap a quarter of its derivative,
+// from its scores: the gradients' kernels that hold a row on a lane.
+template <int F>
+struct RowWeights {
+  float c, lse, top, slope;   // scale log2 e, the row's lse, cap log2 e - lse, slope log2 e
+  bool by_id;
+  // 32 keys from key0 on; element v is key 8 (v / 4) + 4 h + v % 4
+  __device__ __forceinline__ void operator()(const MaskedBwdParams& p, const RowMask& mask, int b, int64_t tq, int h, int key0,
+                                             f32x16& s, f32x16& sl) const {
+    if constexpr ((F & (kCap | kBias)) == 0) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, -lse);
+    } else {
+      const float far = (float)(mask.pos - key0 - 4 * h);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        if constexpr ((F & kCap) != 0) {
+          const float r = cap_r(s[v], p.mask.cap_rate);
+          s[v] = __builtin_fmaf(-2.0f * p.mask.cap_log2, r, top);
+          sl[v] = __builtin_fmaf(-r, r, r);
+        } else {
+          s[v] = __builtin_fmaf(s[v], c, -lse);
+        }
+        if constexpr ((F & kBias) != 0)
+          s[v] = __builtin_fmaf(-slope, __builtin_fabsf(far - (float)(8 * (v >> 2) + (v & 3))), s[v]);
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(s[v]);
+    if (by_id || !mask.all(key0, 32)) {
+      const uint32_t lo = (uint32_t)(mask.lo - key0 - 4 * h), len = (uint32_t)max(mask.lim - mask.lo, 0);
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if ((uint32_t)(8 * (v >> 2) + (v & 3)) - lo >= len) s[v] = 0.0f;
+      if (by_id) {
+        const int32_t* ids = p.mask.k_docs + (int64_t)b * p.Sk;
+        const int doc = p.mask.q_docs[tq];
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (ids[min(key0 + 8 * (v >> 2) + 4 * h + (v & 3), p.Sk - 1)] != doc) s[v] = 0.0f;
+      }
+    }
+  }
+};
 
 }  // namespace partir

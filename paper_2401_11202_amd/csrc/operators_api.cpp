@@ -475,7 +475,7 @@ int run_masked(const void* Q, const void* K, const void* V, void* O, float* lse,
 CrossBwdPlan plan_masked_bwd(const CrossSizes& z, const partir_attention_mask& mask) {
   CrossBwdPlan p;
   p.c = masked_bwd_choice(z.B, z.Sq, z.Sk, z.Hq, z.Hk, mask.causal != 0);
-  p.d_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * 4);
+  if (!p.c.one_pass) p.d_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * 4);
   if (p.c.q_parts > 1) p.q_bytes = align_up((size_t)p.c.q_parts * z.B * z.Sq * z.Hq * z.dh * 4);
   if (p.c.k_parts > 1) p.k_bytes = align_up((size_t)p.c.k_parts * z.B * z.Sk * z.Hk * z.dh * 4);
   return p;
@@ -807,7 +807,8 @@ int partir_plan_masked_attention_backward(int64_t B, int64_t Sq, int64_t Sk, int
     if (!mask || !info) return fail(PARTIR_E_NULL, "mask and info must be non-NULL");
     const CrossBwdPlan p = plan_masked_bwd(z, *mask);
     const size_t docs = plan_docs(z, *mask).ws();
-    const int launches = (docs > 0) + (B * Sq ? 1 + (p.c.q_parts > 1) : 0) + (B * Sk ? 1 + (p.c.k_parts > 1) : 0);
+    const int launches = (docs > 0) + (B * Sq && !p.c.one_pass ? 1 + (p.c.q_parts > 1) : 0) +
+                         (B * Sk ? 1 + (p.c.k_parts > 1) : 0);
     fill_info(info, std::max(p.c.q_parts, p.c.k_parts), launches, B * (Sq + Sk) ? docs + p.ws() : 0,
               10.0 * (double)B * (double)Sq * (double)Sk * (double)(n_heads * d_head));
     return PARTIR_OK;
@@ -862,7 +863,7 @@ int partir_masked_attention_backward(const void* Q, const void* K, const void* V
     if (int st = begin_launches()) return st;
     hipStream_t s = (hipStream_t)stream;
     if (int st = run_doc_rows(p.mask, docs, z, mask->k_lens, ws, s)) return st;
-    if (Tq > 0) {
+    if (Tq > 0 && !plan.c.one_pass) {
       if (int st = launched(launch_masked_backward(p, form, CROSS_DQ, s), "masked_bwd_dq")) return st;
       if (p.q_parts > 1) {
         PartSum r = part_sum(1, p.q_parts, Tq, cq);
@@ -871,12 +872,12 @@ int partir_masked_attention_backward(const void* Q, const void* K, const void* V
       }
     }
     if (Tk == 0) return PARTIR_OK;
-    if (int st = launched(launch_masked_backward(p, form, CROSS_DKV, s), "masked_bwd_dkv")) return st;
+    if (int st = launched(launch_masked_backward(p, form, plan.c.one_pass ? CROSS_ALL : CROSS_DKV, s), "masked_bwd")) return st;
     if (p.k_parts == 1) return PARTIR_OK;
     PartSum r = part_sum(2, p.k_parts, Tk, ck);
     r.part[0] = p.dKpart; r.out[0] = p.dK; r.ld[0] = lddk;
     r.part[1] = p.dVpart; r.out[1] = p.dV; r.ld[1] = lddv;
-    return launched(launch_part_sum(r, s), "masked_bwd_dkv.sum");
+    return launched(launch_part_sum(r, s), "masked_bwd.sum");
   });
 }
 

@@ -14,6 +14,13 @@
 // A row is one wave's up to 512 columns, else a workgroup's of as many waves as
 // it takes at 8 columns a lane (16 from 8192 columns on).  In the gradients a
 // workgroup keeps its columns' sums over all of its rows in registers.
+//
+// What bounds it: HBM.  8192 x 5120, float32 stream, bf16 block, dropout: forward 97 to
+// 102 us (503 MB, 5.0 TB/s), gradients 153 (761 MB, 5.0) and 5 for the sum of the parts.
+// 4084 x 1000 in bf16 with post norm and gates: 12.4, 21 and 4 us, chains of a row's
+// loads, its two sums and its stores (34 and 53 MB).  The forward loads its gains behind
+// the sums: in front of them they take 12.4 -> 11.9 us there, but registers from the
+// waves that hide the loads of the first (96 -> 102).
 #include <algorithm>
 #include <type_traits>
 

@@ -181,18 +181,34 @@ def test_axes_in_parts(B, Sq, Sk, Hq, Hk, f):
 @pytest.mark.parametrize("B,S,Hq,Hk", [(9, 500, 8, 8), (7, 450, 20, 4)])
 @pytest.mark.parametrize("f", [{}, FORMS[3]])
 def test_grids_without_parts(B, S, Hq, Hk, f):
-    """Enough workgroups that every kernel takes whole axes, in both mappings to the compute units."""
+    """Enough workgroups that the forward takes whole axes, with heads of whole rounds of the XCDs and without."""
     assert P.plan_masked_attention(B, S, S, Hq, Hk)["n_virtual_shards"] == 1
     ids = packed(B, S, 150)
     run(B, S, S, Hq, Hk, dict(form(f, Hq), q_docs=ids, k_docs=ids), wid=S)
 
 
-@pytest.mark.parametrize("B,S,Hq,Hk", [(33, 130, 8, 8), (43, 97, 9, 3), (65, 161, 4, 4)])
+@pytest.mark.parametrize("B,S,Hq,Hk", [(33, 130, 8, 8), (43, 97, 9, 3), (65, 161, 4, 4), (67, 143, 6, 2)])
 @pytest.mark.parametrize("f", [{}, *FORMS])
 def test_many_short_sequences(B, S, Hq, Hk, f):
     """The kernels of many workgroups in every form, without documents, on ragged batches."""
     lens = [S - (37 * b) % (S + 1) for b in range(B)]
     run(B, S, S, Hq, Hk, dict(form(f, Hq), k_lens=lens, q_lens=lens), wid=S)
+
+
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk", [(3, 64, 64, 4, 2), (2, 128, 128, 8, 1), (260, 20, 20, 1, 1), (130, 45, 33, 6, 2), (1, 300, 127, 6, 1),
+                                           (270, 90, 100, 3, 1), (2, 5, 97, 12, 4), (3, 400, 1, 2, 1)])
+@pytest.mark.parametrize("f", [{}, *FORMS])
+def test_up_to_128_keys(B, Sq, Sk, Hq, Hk, f):
+    """All gradients in one launch: ragged queries and keys, prefixes; then documents, in one piece each and not."""
+    if Sq == Sk:
+        lens = [S - (7 * b) % (S + 1) for b, S in enumerate([Sk] * B)]
+        run(B, Sq, Sk, Hq, Hk, dict(form(f, Hq), k_lens=lens, q_lens=lens, prefix_lens=[n // 3 for n in lens]), wid=Sk)
+    else:
+        run(B, Sq, Sk, Hq, Hk, dict(form(f, Hq), q_lens=[Sq - (11 * b) % (Sq + 1) for b in range(B)], q_starts=[(5 * b) % 9 - 3 for b in range(B)]),
+            wid=Sk)
+    q, k = packed(B, Sq, 9), packed(B, Sk, 9)
+    run(B, Sq, Sk, Hq, Hk, dict(form(f, Hq), q_docs=q, k_docs=k), wid=Sk + 1)
+    run(B, Sq, Sk, Hq, Hk, dict(form(f, Hq), causal=False, q_docs=q % 3, k_docs=k % 3), wid=Sk + 1)
 
 
 @pytest.mark.parametrize("scale,qscale", [(1.0, 1.0), (0.02, 1.0), (1.0, 4.0)])

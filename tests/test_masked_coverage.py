@@ -57,6 +57,6 @@ def test_the_gradients_run_in_every_form_with_even_and_other_groups_with_and_wit
             shapes = [s for s in shapes if s[1] < 5]        # the others run no gradients
         for s in shapes:
             parts = P.plan_masked_attention_backward(*s)["n_virtual_shards"] > 1
-            got |= {(16 % (s[3] // s[4]) == 0, form, parts) for form in forms}
-    assert {k[:2] for k in got} == {(even, form) for even in (True, False) for form in range(4)}
-    assert {(True, 0, True), (True, 0, False), (True, 3, True), (True, 3, False), (False, 0, False), (False, 3, False)} <= got
+            got |= {(s[2] <= 128, 16 % (s[3] // s[4]) == 0, form, parts) for form in forms}
+    assert {k[:3] for k in got} == {(short, even, form) for short in (True, False) for even in (True, False) for form in range(4)}
+    assert {(short, even, form, parts) for short in (True, False) for even in (True, False) for form in (0, 3) for parts in (True, False)} <= got
