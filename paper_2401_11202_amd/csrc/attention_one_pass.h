@@ -51,7 +51,8 @@ __global__ __launch_bounds__(2 * NT, 2) void attention_one_pass_kernel(typename 
   constexpr int EP = KT + 128 * ROWB;                // P and dS of a tile, [64 rows][128 keys] as tiles
   constexpr int ES = EP + TILE;
   constexpr int DSUM = ES + TILE;                    // [key group][row]: shares of D
-  constexpr int ROWS = DSUM + 4 * TR * 4;            // the waves' row areas
+  constexpr int PSUM = DSUM + 4 * TR * 4;            // and of the sum of the weights
+  constexpr int ROWS = PSUM + (F != 0 ? 4 * TR * 4 : 0);   // the waves' row areas
   __shared__ __attribute__((aligned(1024))) char smem[ROWS + 8 * row_area<1, __bf16>()];
   static_assert(8 * row_area<2, float>() <= EP, "the end goes through the stages and K");
   const int lane = threadIdx.x & 63;
@@ -160,6 +161,13 @@ __global__ __launch_bounds__(2 * NT, 2) void attention_one_pass_kernel(typename 
 #pragma unroll
     for (int v = 0; v < 16; ++v) d = __builtin_fmaf(s[v], dp[v], d);
     d += __shfl_xor(d, 32);
+    if constexpr (F != 0) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum += s[v];
+      sum += __shfl_xor(sum, 32);
+      if (h == 0) lds_write(smem + PSUM + (kg * TR + erow) * 4, sum);
+    }
     auto put = [&](char* e, f32x16 x) {   // four consecutive keys a lane and write
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -178,6 +186,12 @@ __global__ __launch_bounds__(2 * NT, 2) void attention_one_pass_kernel(typename 
     float D = 0.0f;
 #pragma unroll
     for (int g = 0; g < 4; ++g) D += lds_read<float>(smem + DSUM + (g * TR + erow) * 4);
+    if constexpr (F != 0) {   // over the sum of the weights, which is 1 up to the error of z
+      float sum = 0.0f;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) sum += lds_read<float>(smem + PSUM + (g * TR + erow) * 4);
+      D = sum > 0.0f ? D / sum : 0.0f;
+    }
 #pragma unroll
     for (int v = 0; v < 16; ++v) dp[v] = s[v] * (dp[v] - D);
     put(smem + es, dp);

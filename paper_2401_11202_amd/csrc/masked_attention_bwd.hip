@@ -128,6 +128,7 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
     tile_load<TR, 4>(p.K + tk * p.ldk + kvh * DH, p.ldk, rows, t, w, lane);
     tile_load<TR, 4>(p.V + tk * p.ldv + kvh * DH, p.ldv, rows, t + TILE, w, lane);
   };
+  float psum = 0.0f;
   if (few0 < few1) {
     if (few) dsum = 0.0f;
     int buf = (few1 - few0 + TR - 1) / TR & 1;       // so that the first tile of the loop below is in stage 0
@@ -154,13 +155,20 @@ void masked_bwd_dq_kernel(MaskedBwdParams p) {
         }
         weights(s, sl, key + 32 * t);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) dsum = __builtin_fmaf(s[v], dp[v], dsum);
+        for (int v = 0; v < 16; ++v) {
+          dsum = __builtin_fmaf(s[v], dp[v], dsum);
+          psum += s[v];
+        }
       }
     }
   } else if (nkb > 0) {
     gload(range.begin, 0);
   }
-  const float Dq = dsum + __shfl_xor(dsum, 32);
+  float Dq = dsum + __shfl_xor(dsum, 32);
+  if (few) {   // over the sum of the weights, which is 1 up to the error of z: what all weights are off by leaves dP - D alone
+    psum += __shfl_xor(psum, 32);
+    Dq = psum > 0.0f ? Dq / psum : 0.0f;
+  }
 
   f32x16 dq[4], nD;   // dP starts at -D: its first product reads it, where a subtraction would follow
 #pragma unroll

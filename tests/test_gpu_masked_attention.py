@@ -249,6 +249,26 @@ def test_many_documents():
     run(1, 1500, 1500, 1, 1, dict(q_docs=ids, k_docs=ids), wid=15)
 
 
+@pytest.mark.parametrize("S", [1, 60, 130, 300])
+@pytest.mark.parametrize("f", [dict(cap=1000.0), dict(cap=1000.0, slopes=True), {}])
+def test_rows_of_one_key_have_no_gradient(S, f):
+    """dS = P (dP - D) is 0 with one key, whatever P: D = P dP / P.  dP and D are
+    float32 sums of the same 128 products, a product and a division, below 2^-20 of
+    |dO| |V|^T; that P is off by 2^-20 of the cap must not show."""
+    say(f"masked_attention S={S} {f}")
+    B, H = 3, 2
+    (Q, K, V, dO), (q, k, v, g) = make(B, S, S, H, H, {}, 50 + S)
+    ids = torch.arange(B * S, device="cuda", dtype=torch.int32)
+    kw = dict(B=B, Sq=S, Sk=S, n_heads=H, q_docs=ids, k_docs=ids, **device_mask(form(f, H)))
+    O, lse = P.masked_attention_train(Q, K, V, **kw)
+    dq, dk, _ = P.masked_attention_backward(Q, K, V, O, dO, lse, **kw)
+    ds = 2.0 ** -20 * np.repeat((np.abs(g) * np.abs(v)).reshape(B * S, H, DH).sum(-1), DH, axis=1) * DH ** -0.5
+    for name, got, x in (("dQ", dq, k), ("dK", dk, q)):
+        past = np.abs(host(got)) - 1.01 * ds * np.abs(x)
+        say(f"    {name}: largest error past its bound {past.max():.2e}")
+        assert past.max() <= 0, name
+
+
 def test_very_many_sequences():
     """More sequences than a launch has workgroups of 1024 threads.  One key: a query
     that sees it has weight 1, so O = V and dV = dO in every bit; dS = P (dP - D) is 0
