@@ -18,16 +18,17 @@
 // of the other errors.  The dq pass starts from it, and adds the sum over its keys of
 // P (dP - D), which is what it was off by (the weights sum to 1), so that dkv takes D
 // with float32's error; where a wave's rows see 256 keys at most, some blocks' time
-// more give the dq pass itself that D, as the sum of P dP over that of P.  (Error of dQ at 4 x 2048 tokens of documents of
-// 400 on average, of its size: 2.69e-3 with rowsum(dO * O) alone.)
+// more give the dq pass itself that D, as the sum of P dP over that of P.  (Error of dQ
+// at 4 x 2048 tokens of documents of 400 on average, of its size: 2.45e-3, and 2.69e-3
+// with rowsum(dO * O) alone.)
 //
 // What bounds it.  Many rows: matrix and vector units, two waves a SIMD, behind one
 // another's time in part only.  2 x 4096 tokens, 32 / 8 heads, causal, capped: dq 447 to
 // 482 us (0.41 TFLOP, 0.9 PFLOP/s; matrix units busy 45 % of the time, vector units 62),
 // dkv 640 to 671 (0.55 TFLOP, 0.84 PFLOP/s; 37 and 50 %), 26 for the sum of two parts.
 // Without a cap and a mask they take 743 and 1092 us for twice the pairs (attention to
-// another sequence 727 and 992, whose dkv pass holds 256 keys).  Documents of 400 tokens on average, 4 x 2048, 32 heads: 157 and
-// 167 us, with 640 and 576 MB read and written (4.1 and 3.5 TB/s) in chains of few
+// another sequence 727 and 992, whose dkv pass holds 256 keys).  Documents of 400
+// tokens on average, 4 x 2048, 32 heads: 157 and 167 us, with 640 and 576 MB read and written (4.1 and 3.5 TB/s) in chains of few
 // tiles.  3 x 333 tokens, 12 / 4 heads, bias: 23 and 19, one workgroup's chain.
 #include <algorithm>
 #include <type_traits>

@@ -343,6 +343,66 @@ def test_a_captured_step_reads_its_masks_at_every_replay():
             assert torch.equal(a, b)
 
 
+def test_a_captured_step_of_short_sequences():
+    """The one launch for all gradients, which must leave the gradients of rows that a shorter batch no longer has at 0."""
+    B, S, Hq, Hk = 3, 120, 4, 1
+    (Q, K, V, dO), _ = make(B, S, S, Hq, Hk, {}, 44)
+    ids = torch.tensor(packed(B, S, 30), dtype=torch.int32, device="cuda")
+    lens = torch.tensor([120, 100, 3], dtype=torch.int32, device="cuda")
+    kw = dict(B=B, Sq=S, Sk=S, n_heads=Hq, n_kv_heads=Hk, cap=20.0, q_docs=ids, k_docs=ids, k_lens=lens, q_lens=lens)
+
+    def step():
+        O, lse = P.masked_attention_train(Q, K, V, **kw)
+        return [O, lse, *P.masked_attention_backward(Q, K, V, O, dO, lse, **kw)]
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for r in range(4):
+        lens.copy_(torch.tensor([120 - 40 * r, 30 * r, 7 + r], dtype=torch.int32))
+        ids.copy_(torch.tensor(packed(B, S, 5 + 20 * r, r), dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, step()):
+            assert torch.equal(a, b)
+        assert not outs[2].reshape(B, S, -1)[1, 30 * r:].any()
+
+
+@pytest.mark.parametrize("S", [110, 700])
+def test_two_graphs_share_a_workspace(S):
+    """Each call writes what it reads of a workspace."""
+    Hq, Hk = 4, 1
+    ws = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    graphs, steps = [], []
+    for i, mean in enumerate((20, 90)):
+        (Q, K, V, dO), _ = make(2, S, S, Hq, Hk, {}, 46 + i)
+        ids = torch.tensor(packed(2, S, mean, i), dtype=torch.int32, device="cuda")
+        kw = dict(B=2, Sq=S, Sk=S, n_heads=Hq, n_kv_heads=Hk, q_docs=ids, k_docs=ids)
+
+        def step(Q=Q, K=K, V=V, dO=dO, kw=kw, ws=ws):
+            O, lse = P.masked_attention_train(Q, K, V, workspace=ws, **kw)
+            return [O, lse, *P.masked_attention_backward(Q, K, V, O, dO, lse, workspace=ws, **kw)]
+
+        steps.append(step)
+        step()
+        torch.cuda.synchronize()
+        graphs.append((torch.cuda.CUDAGraph(), []))
+        with torch.cuda.graph(graphs[-1][0]):
+            graphs[-1][1].extend(step())
+    want = [[x.clone() for x in s(ws=None)] for s in steps]
+    for _ in range(3):
+        for graph, outs in graphs:
+            for x in outs:
+                x.fill_(7)
+            ws.fill_(255)
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, outs), w in zip(graphs, want):
+            assert all(torch.equal(a, b) for a, b in zip(outs, w))
+
+
 def test_two_streams_at_once():
     ids = torch.tensor(packed(2, 500, 100), dtype=torch.int32, device="cuda")
     cases = []
