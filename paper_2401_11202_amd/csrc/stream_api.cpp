@@ -52,9 +52,12 @@ int validate_join(const JoinArgs& a) {
   return PARTIR_OK;
 }
 
-Matrix gate_matrix(const JoinArgs& a) {
-  return {"gate", a.gate, a.gate && a.T ? cdiv(a.T, a.gate_rows) : 0, a.D, a.ldgate, 4};
-}
+// Rows of the stream that take one row of the gate.  More than T are T: gate_rows may be
+// any count, and sums with it would pass 64 bits.
+int64_t gate_span(const JoinArgs& a) { return std::min(a.gate_rows, std::max<int64_t>(a.T, 1)); }
+int64_t gate_groups(const JoinArgs& a) { return a.gate && a.T ? cdiv(a.T, gate_span(a)) : 0; }
+
+Matrix gate_matrix(const JoinArgs& a) { return {"gate", a.gate, gate_groups(a), a.D, a.ldgate, 4}; }
 
 // The parameters that forward and backward share.
 int fill_join(JoinParams& p, const JoinArgs& a) {
@@ -67,7 +70,7 @@ int fill_join(JoinParams& p, const JoinArgs& a) {
   if (int st = resolve_dropout(p.drop, a.p, a.seed, a.row0, a.T)) return st;
   p.g_post = a.g_post; p.g_pre = a.g_pre; p.gate = a.gate;
   p.ldgate = a.ldgate;
-  p.gate_rows = a.gate ? a.gate_rows : std::max<int64_t>(a.T, 1);
+  p.gate_rows = a.gate ? gate_span(a) : std::max<int64_t>(a.T, 1);
   p.T = a.T; p.D = (int)a.D; p.post = a.post != 0;
   p.scale = a.scale * p.drop.factor;
   p.eps = a.eps;
@@ -175,7 +178,7 @@ int partir_residual_norm_backward(const void* X, const void* Y, const void* dH, 
     for (const float* g : {dg_post, dgate, dg_pre})
       if (!aligned(g, 16)) return fail(PARTIR_E_LAYOUT, "gradients of gains and gates must be 16-byte aligned");
     if (D == 0) return PARTIR_OK;
-    const int64_t groups = gate && T ? cdiv(T, gate_rows) : 0;
+    const int64_t groups = gate_groups(a);
     const Matrix g = gate_matrix(a), gp{"g_post", g_post, 1, D, D, 4}, gn{"g_pre", g_pre, 1, D, D, 4}, sd{"seed", seed, 1, 2, 2, 8};
     const Matrix o1{"dg_post", dg_post, 1, D, D, 4}, o2{"dgate", dgate, groups, D, D, 4}, o3{"dg_pre", dg_pre, 1, D, D, 4};
     if (int st = check_apart(dx, &dh, {&x, &y, &dn, &dy, &g, &gp, &gn, &sd, &o1, &o2, &o3})) return st;

@@ -1340,6 +1340,7 @@ def _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed):
             gate_rows = max(T, 1)
         if gate_rows < 1:
             _bad("PARTIR_E_SHAPE", f"gate_rows = {gate_rows}")
+        gate_rows = min(gate_rows, max(T, 1))    # all rows; a count past 64 bits would arrive as another
         ldg = _matrix(gate, "gate", -(-T // gate_rows), D, torch.float32)
     _seed(seed)
     return T, D, gate_rows if gate is not None else 0, ldx, ldy, ldg, xd, yd
