@@ -21,7 +21,7 @@ int resolve_dropout(Dropout& d, double p, const uint64_t* seed, int64_t row0, in
   if (!(p >= 0.0 && p <= 1.0)) return fail(PARTIR_E_UNSUPPORTED, "p must be within 0..1");
   if (!seed && p != 0.0) return fail(PARTIR_E_NULL, "seed must be non-NULL where p is not 0");
   if (!aligned(seed, 8)) return fail(PARTIR_E_LAYOUT, "seed must be 8-byte aligned");
-  if (row0 < 0 || row0 + T > ((int64_t)1 << 32)) return fail(PARTIR_E_SHAPE, "row0 = %lld: rows are numbered below 2^32", (long long)row0);
+  if (row0 < 0 || row0 > ((int64_t)1 << 32) - T) return fail(PARTIR_E_SHAPE, "row0 = %lld: rows are numbered below 2^32", (long long)row0);
   d.kept = (uint32_t)std::floor((1.0 - p) * 65536.0 + 0.5);
   d.seed = d.kept == 65536 ? nullptr : seed;
   d.row0 = (uint32_t)row0;

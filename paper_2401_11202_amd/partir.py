@@ -1274,7 +1274,9 @@ def _rows(t, name, rows, cols):
     return _dt(t), _matrix(t, name, rows, cols, t.dtype)
 
 
-def _seed(seed):
+def _seed(seed, row0):
+    if not 0 <= row0 <= 2 ** 32:             # past 64 bits it would arrive as another number
+        _bad("PARTIR_E_SHAPE", f"row0 = {row0}: rows are numbered below 2^32")
     if seed is not None:
         torch = _th()
         if not isinstance(seed, torch.Tensor):
@@ -1302,7 +1304,7 @@ def dropout(X, p: float, seed, *, residual=None, row0: int = 0, out_dtype=None, 
     xd, ldx = _rows(X, "X", T, D)
     if seed is None:
         _bad("PARTIR_E_NULL", "seed must be a tensor")
-    _seed(seed)
+    _seed(seed, row0)
     if out_dtype is None:
         out_dtype = (X if out is None and residual is None else residual if out is None else out).dtype
     ldr = 0 if residual is None else _matrix(residual, "residual", T, D, out_dtype)
@@ -1324,7 +1326,7 @@ def dropout(X, p: float, seed, *, residual=None, row0: int = 0, out_dtype=None, 
     return out
 
 
-def _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed):
+def _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed, row0):
     """Checked sizes of a join: (T, D, gate_rows, ldx, ldy, ldgate, x_dtype, y_dtype)."""
     torch = _th()
     if not isinstance(Y, torch.Tensor) or Y.dim() != 2:
@@ -1342,7 +1344,7 @@ def _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed):
             _bad("PARTIR_E_SHAPE", f"gate_rows = {gate_rows}")
         gate_rows = min(gate_rows, max(T, 1))    # all rows; a count past 64 bits would arrive as another
         ldg = _matrix(gate, "gate", -(-T // gate_rows), D, torch.float32)
-    _seed(seed)
+    _seed(seed, row0)
     return T, D, gate_rows if gate is not None else 0, ldx, ldy, ldg, xd, yd
 
 
@@ -1356,7 +1358,7 @@ def residual_norm(X, Y, *, g_post=None, post_norm: bool = False, gate=None, gate
     gate [ceil(T / gate_rows), D] f32: row t takes gate row t // gate_rows (None: one
     row for all).  p, seed, row0: as dropout.  out, norm_out: where to write H (X
     allowed) and N (Y allowed).  Returns (H, N), N None without next_norm."""
-    T, D, rows, ldx, ldy, ldg, xd, yd = _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed)
+    T, D, rows, ldx, ldy, ldg, xd, yd = _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed, row0)
     if norm_out is not None and not next_norm:
         _bad("PARTIR_E_UNSUPPORTED", "norm_out without next_norm")
     fresh_h, fresh_n = out is None, next_norm and norm_out is None
@@ -1384,7 +1386,7 @@ def residual_norm_backward(X, Y, dH, dN, *, g_post=None, post_norm: bool = False
     dgate and dg_pre are f32, None without their operand.  out: (dX, dY) to write
     into, dH and dN themselves allowed; gain_out: (dg_post, dgate, dg_pre)."""
     torch = _th()
-    T, D, rows, ldx, ldy, ldg, xd, yd = _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed)
+    T, D, rows, ldx, ldy, ldg, xd, yd = _join_args(X, Y, g_post, gate, gate_rows, g_pre, seed, row0)
     if (dN is None) == bool(next_norm):
         _bad("PARTIR_E_NULL", "dN must be given exactly with next_norm")
     if dH is None and dN is None:

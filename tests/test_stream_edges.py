@@ -1,9 +1,10 @@
 """Arguments of dropout and of the join with the residual stream at the ends of
 their ranges (no GPU needed)."""
 import pytest
+import torch
 
 from paper_2401_11202_amd import partir as P
-from tests.test_stream_checks import A, _never_launch, bwd, join  # noqa: F401
+from tests.test_stream_checks import A, _never_launch, bwd, drop, join, status  # noqa: F401
 
 MOST = 2 ** 63 - 1
 
@@ -17,3 +18,16 @@ def test_a_gate_row_for_any_count_of_rows(rows):
     assert bwd(rows=rows, dgpost=A[11]) == "PARTIR_E_LAYOUT"
     ws = P.lib().partir_residual_norm_backward_workspace
     assert ws(16, 40, rows) == ws(16, 40, 16)
+
+
+@pytest.mark.parametrize("row0", [2 ** 32 - 15, 2 ** 32, MOST - 16, MOST - 15, MOST])
+def test_rows_numbered_past_their_range(row0):
+    assert drop(row0=row0) == join(row0=row0) == bwd(row0=row0) == "PARTIR_E_SHAPE"
+
+
+@pytest.mark.parametrize("row0", [-1, 2 ** 32 + 1, 2 ** 64, 2 ** 64 + 1, -2 ** 64 + 5])
+def test_the_binding_passes_no_other_row_on(row0):
+    x, y, s = torch.zeros(16, 40), torch.zeros(16, 40, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int64)
+    for call in (lambda: P.dropout(x, 0.5, s, row0=row0), lambda: P.residual_norm(x, y, p=0.5, seed=s, row0=row0),
+                 lambda: P.residual_norm_backward(x, y, x, y, p=0.5, seed=s, row0=row0)):
+        assert status(call) == "PARTIR_E_SHAPE"
