@@ -172,9 +172,11 @@ int partir_residual_norm_backward(const void* X, const void* Y, const void* dH, 
     for (const Matrix* m : {&x, &y, &dh, &dn, &dx, &dy})
       if (int st = check(*m)) return st;
     if (T > 0 && D > 0 && !dH && !dN) return fail(PARTIR_E_NULL, "dH or dN must be non-NULL");
-    if (dg_post && !post_norm) return fail(PARTIR_E_UNSUPPORTED, "dg_post without the block's norm");
+    // gains of 1 have no gradient; without columns all of these may be NULL
+    if (dg_post && !g_post) return fail(PARTIR_E_UNSUPPORTED, "dg_post without g_post");
+    if (dg_pre && !g_pre) return fail(PARTIR_E_UNSUPPORTED, "dg_pre without g_pre");
     if (dgate && !gate) return fail(PARTIR_E_UNSUPPORTED, "dgate without a gate");
-    if ((g_pre || dg_pre) && !dN && T > 0) return fail(PARTIR_E_UNSUPPORTED, "g_pre or dg_pre without dN");
+    if (g_pre && !dN && T > 0) return fail(PARTIR_E_UNSUPPORTED, "g_pre without dN");
     for (const float* g : {dg_post, dgate, dg_pre})
       if (!aligned(g, 16)) return fail(PARTIR_E_LAYOUT, "gradients of gains and gates must be 16-byte aligned");
     if (D == 0) return PARTIR_OK;

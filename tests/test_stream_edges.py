@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2401_11202_amd import partir as P
-from tests.test_stream_checks import A, _never_launch, bwd, drop, join, status  # noqa: F401
+from tests.test_stream_checks import A, NULL, _never_launch, bwd, drop, join, status  # noqa: F401
 
 MOST = 2 ** 63 - 1
 
@@ -31,3 +31,12 @@ def test_the_binding_passes_no_other_row_on(row0):
     for call in (lambda: P.dropout(x, 0.5, s, row0=row0), lambda: P.residual_norm(x, y, p=0.5, seed=s, row0=row0),
                  lambda: P.residual_norm_backward(x, y, x, y, p=0.5, seed=s, row0=row0)):
         assert status(call) == "PARTIR_E_SHAPE"
+
+
+@pytest.mark.parametrize("T", [16, 0])
+@pytest.mark.parametrize("gain", ["post", "pre"])
+def test_a_gain_of_1_has_no_gradient(gain, T):
+    none = {"g" + gain: NULL}
+    assert bwd(T=T, **none) == "PARTIR_E_UNSUPPORTED"
+    assert bwd(T=T, **none, **{"dg" + gain: NULL}) == "PARTIR_E_HIP"
+    assert bwd(T=T, **{"dg" + gain: NULL}) == "PARTIR_E_HIP"
