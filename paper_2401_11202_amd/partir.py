@@ -1150,18 +1150,26 @@ def _plan_sizes(fn, *args):
     return info.as_dict()
 
 
+def _nonzero(x, name):
+    """x, which float32 holds: where it is rounded to 0 it would select what 0 does."""
+    x = float(x)
+    if x and not F(x).value:
+        _bad("PARTIR_E_UNSUPPORTED", f"{name} = {x} is below float32's least number")
+    return x
+
+
 def _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal, cap, slopes, k_lens, q_lens, q_starts,
                  prefix_lens, q_docs, k_docs):
     """Checked sizes of a masked attention call, its mask and the mask's tensors."""
     Hk, Tq, Tk, ldq, ldk, ldv = _cross_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, k_lens)
     tensors = (slopes, k_lens, q_lens, q_starts, prefix_lens, q_docs, k_docs)
-    mask = AttentionMask(bool(causal), float(cap))
+    mask = AttentionMask(bool(causal), _nonzero(cap, "cap"))
     if not (slopes is k_lens is q_lens is q_starts is prefix_lens is q_docs is k_docs is None):
         _opt(slopes, "slopes", (n_heads,), _torch.float32)
         shapes = (B,), (B,), (B,), (Tq,), (Tk,)
         for name, t, shape in zip(MASK_TENSORS[2:], tensors[2:], shapes):
             _opt(t, name, shape, _torch.int32)
-        mask = AttentionMask(bool(causal), float(cap), *map(_ptr, tensors))
+        mask = AttentionMask(mask.causal, mask.cap, *map(_ptr, tensors))
     return Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors
 
 
@@ -1193,6 +1201,7 @@ def masked_attention_train(Q, K, V, *, B: int, Sq: int, Sk: int, n_heads: int, n
 
 def _masked_forward(Q, K, V, scale, out, lse, train, workspace, stream, B, Sq, Sk, n_heads, n_kv_heads, d_head, *mask_args):
     torch = _th()
+    scale = _nonzero(max(scale, 0.0), "scale")
     Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors = _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, *mask_args)
     ldo = n_heads * d_head
     fresh_o, fresh_l = out is None, train and lse is None
@@ -1208,7 +1217,7 @@ def _masked_forward(Q, K, V, scale, out, lse, train, workspace, stream, B, Sq, S
         lse = torch.empty((Tq, n_heads), dtype=torch.float32, device=dev)
     ws, wsb = _workspace(dev, workspace, lib().partir_masked_attention_workspace, B, Sq, Sk, n_heads, Hk, d_head, mask)
     _on_stream(stream, ws if workspace is None else None, out if fresh_o else None, lse if fresh_l else None)
-    sizes = (B, Sq, Sk, n_heads, Hk, d_head, ldq, ldk, ldv, ldo, mask, float(scale), _ptr(ws), wsb)
+    sizes = (B, Sq, Sk, n_heads, Hk, d_head, ldq, ldk, ldv, ldo, mask, scale, _ptr(ws), wsb)
     if train:
         _launch(dev, lib().partir_masked_attention_train, _ptr(Q), _ptr(K), _ptr(V), _ptr(out), _ptr(lse), *sizes, stream=stream)
         return out, lse
@@ -1225,6 +1234,7 @@ def masked_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, 
     slopes have none.  out: (dQ, dK, dV) to write into."""
     torch = _th()
     bf = torch.bfloat16
+    scale = _nonzero(max(scale, 0.0), "scale")
     Hk, Tq, Tk, ldq, ldk, ldv, mask, tensors = _masked_args(Q, K, V, B, Sq, Sk, n_heads, n_kv_heads, d_head, causal, cap, slopes,
                                                             k_lens, q_lens, q_starts, prefix_lens, q_docs, k_docs)
     cq, ck = n_heads * d_head, Hk * d_head
@@ -1245,7 +1255,7 @@ def masked_attention_backward(Q, K, V, O, dO, lse, *, B: int, Sq: int, Sk: int, 
     _on_stream(stream, ws if workspace is None else None, *(out if fresh else ()))
     _launch(dev, lib().partir_masked_attention_backward, _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(lse),
             _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), B, Sq, Sk, n_heads, Hk, d_head, ldq, ldk, ldv, ldo, lddo, *lds, mask,
-            float(scale), _ptr(ws), wsb, stream=stream)
+            scale, _ptr(ws), wsb, stream=stream)
     return out
 
 
