@@ -106,7 +106,8 @@ int partir_dropout(const void* X, const void* R, void* Y, int64_t T, int64_t D, 
     if (int st = check_apart(y, &x, {&sd})) return st;
     if (int st = check_apart(y, &r, {})) return st;
     q.cols8 = (int)cdiv(D, 8);
-    if (T * q.cols8 >= (int64_t)1 << 34) return fail(PARTIR_E_SHAPE, "more than 2^32 threads of a launch");
+    // workgroups of 256 threads for 1024 groups of columns, fewer than 2^32 threads in all
+    if (cdiv(T * q.cols8, 1024) >= (int64_t)1 << 24) return fail(PARTIR_E_SHAPE, "2^32 threads of a launch or more");
     q.x = X; q.r = R; q.y = Y;
     q.ldx = ldx; q.ldr = ldr; q.ldy = ldy;
     q.T = T; q.D = (int)D;

@@ -1,5 +1,7 @@
 """Arguments of dropout and of the join with the residual stream at the ends of
 their ranges (no GPU needed)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -40,3 +42,10 @@ def test_a_gain_of_1_has_no_gradient(gain, T):
     assert bwd(T=T, **none) == "PARTIR_E_UNSUPPORTED"
     assert bwd(T=T, **none, **{"dg" + gain: NULL}) == "PARTIR_E_HIP"
     assert bwd(T=T, **{"dg" + gain: NULL}) == "PARTIR_E_HIP"
+
+
+@pytest.mark.parametrize("T,D,want", [(2 ** 30 - 64, 128, "PARTIR_E_HIP"), (2 ** 30 - 63, 128, "PARTIR_E_SHAPE"), (2 ** 30 - 1, 128, "PARTIR_E_SHAPE"),
+                                      (8191, 2 ** 24, "PARTIR_E_HIP"), (8192, 2 ** 24, "PARTIR_E_SHAPE")])
+def test_the_largest_launch_of_dropout(T, D, want):
+    """A launch is fewer than 2^32 threads: at most 2^24 - 1 workgroups of 256, each for 1024 groups of eight columns."""
+    assert drop(T=T, D=D, ldx=D, ldy=D, R=NULL, ldr=0, Y=ctypes.c_void_p(1 << 50)) == want
