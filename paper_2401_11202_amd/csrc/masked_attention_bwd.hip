@@ -298,7 +298,7 @@ void masked_bwd_dkv_kernel(MaskedBwdParams p) {
   // GB came from behind the L2).
   const int it0 = tiles - 1 - part, step = p.k_parts;
   if (it0 >= first) {                                               // workgroup-uniform
-    tile_load<KW, 4>(p.V + ((int64_t)b * p.Sk + k0) * p.ldv + kvh * DH, p.ldv, m.klen - k0, smem + VT, w, lane);
+    tile_load<KW, 4>(p.V + ((int64_t)b * p.Sk + k0) * p.ldv + kvh * DH, p.ldv, min(KW, m.klen - k0), smem + VT, w, lane);
     bf16x8 kf[8];
     {
       const uint16_t* krow = p.K + ((int64_t)b * p.Sk + min(kj, m.klen - 1)) * p.ldk + kvh * DH + 8 * h;
