@@ -1,22 +1,7 @@
 // Attention to another sequence, forward: O = softmax(scale Q K^T) V over the
 // first len_b keys of each sequence, d_head = 128, bf16 in and out, any number
-// of queries and keys, key heads shared by G query heads.
-//
-// A workgroup takes 32 QW rows of the G Sq query rows of one (sequence, key
-// head); its QW x KG waves hold 32 rows each, and the KG key groups take every
-// KG-th block of BKV keys through a ring of LDS stages of their own.  A
-// wave computes
-//     S^T[BKV keys x 32 rows] = K_blk Q^T      (v_mfma_f32_32x32x16_bf16)
-// so that a lane owns one row: maximum and sum of the running softmax are lane
-// registers, and exp2(S^T - m), rounded to bf16 (within 2^-8 of its value, as
-// the weights of partir_attention), is the B operand of
-//     O^T[128 x 32 rows] += V_blk^T P^T
-// with V^T from transposed LDS reads.  Where rows are few the matrix units wait
-// for K and V, and what that rounding leaves is a second operand (the weights
-// are within 2^-16 then), so that O's error is its own rounding: 1.66e-3 of its
-// size, 2.34e-3 with one (64 x 8192 keys, 363 us either way; the smallest calls
-// take 0.2 to 0.6 us more).  Sums and O are float32; groups and key parts join by
-// (m, l, O) (+) (m', l', O'), in a fixed order.
+// of queries and keys, key heads shared by G query heads.  The kernel and how it
+// computes: cross_attention_kernel.h.
 //
 // Keys at and behind len_b are never read: their tile rows are zeros (the
 // descriptor ends before them), so what the padding holds, NaN included, does

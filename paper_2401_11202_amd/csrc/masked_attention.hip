@@ -8,9 +8,11 @@
 //
 // What bounds it.  A token a sequence: reading K and V; 65537 keys of 16 heads, bias
 // (537 MB): 98 us, 5.5 TB/s, and 4.6 for the join of the parts; 16 sequences of up to
-// 4099 keys, 8 key heads, capped (161 MB): 35 to 40, ragged lengths on equal parts.  Many
+// 4099 keys, 8 key heads, capped (161 MB): 39 to 41, ragged lengths on equal parts.  Many
 // rows: without a cap or documents the times are those of attention to another
-// sequence (2 x 4096 tokens, 32 / 8 heads, no mask: 505 and 501 us).  A cap costs vector work, with the matrix units' behind it in part only:
+// sequence (2 x 4096 tokens, 32 / 8 heads, no mask: 505 and 501 us; causal, 0.27 TFLOP:
+// 276, and 447 with a bias, whose six instructions a score are vector work too).  A cap
+// costs vector work, with the matrix units' behind it in part only:
 // 2 x 4096 tokens, 32 / 8 heads, causal (0.27 TFLOP): 355 to 377 us, vector units busy 66
 // % of the time, matrix units 37; 509 queries over 8192 keys: 95, in 54 and 32 %, and
 // 5.7 for the join.  Documents of 400 tokens on average, 4 x 2048, 32 heads: 94 us for
@@ -74,8 +76,10 @@ __global__ __launch_bounds__(256) void masked_combine_kernel(MaskedParams p) {
 // it lists the runs of equal numbers of the sequence's valid keys, and where no
 // number has two runs, and there are at most kRuns, a query's keys are the run of
 // its number.  The run at the query's own position is looked at first, which is the
-// one where queries and keys are the same tokens.  4 x 2048 tokens: 5.5 us, a launch and
-// a chain of loads and barriers.
+// one where queries and keys are the same tokens.  4 x 2048 tokens of some five
+// documents each: 5.5 us, a launch and a chain of loads and barriers.  Many documents:
+// the comparison of every two runs, in each workgroup again.  1 x 8192 tokens: 9 us
+// with 32 documents, 14 with 128, 34 with 512, 320 with 2048, 1270 with 4096.
 constexpr int kRuns = 4096, kDocThreads = 1024;
 __global__ __launch_bounds__(kDocThreads) void doc_rows_kernel(DocRows t) {
   __shared__ __attribute__((aligned(16))) int id[kRuns];

@@ -26,10 +26,12 @@
 // another's time in part only.  2 x 4096 tokens, 32 / 8 heads, causal, capped: dq 447 to
 // 482 us (0.41 TFLOP, 0.9 PFLOP/s; matrix units busy 45 % of the time, vector units 62),
 // dkv 640 to 671 (0.55 TFLOP, 0.84 PFLOP/s; 37 and 50 %), 26 for the sum of two parts.
-// Without a cap and a mask they take 743 and 1092 us for twice the pairs (attention to
-// another sequence 727 and 992, whose dkv pass holds 256 keys).  Documents of 400
-// tokens on average, 4 x 2048, 32 heads: 157 and 167 us, with 640 and 576 MB read and written (4.1 and 3.5 TB/s) in chains of few
-// tiles.  3 x 333 tokens, 12 / 4 heads, bias: 23 and 19, one workgroup's chain.
+// Causal without a cap: 410 and 639 (0.96 TFLOP, 0.92 PFLOP/s),
+// with a bias 409 and 657; without a mask, for twice the pairs, 743 and 1092 us
+// (attention to another sequence 727 and 992, whose dkv pass holds 256 keys).
+// Documents of 400 tokens on average, 4 x 2048, 32 heads: 157 and 167 us, with 640 and
+// 576 MB read and written (4.1 and 3.5 TB/s) in chains of few tiles.  3 x 333 tokens,
+// 12 / 4 heads, bias: 23 and 19, one workgroup's chain.
 #include <algorithm>
 #include <type_traits>
 
@@ -506,7 +508,10 @@ void launch_form(const MaskedBwdParams& p, CrossBwdPass pass, hipStream_t s) {
 // Parts of an axis whose `grid` workgroups take up to `steps` steps each, and `share`
 // of those on average: the longest workgroup, or all of them on the chip's two a compute
 // unit, whichever lasts longer; from two parts on a launch that adds them (5 us) and
-// part_us for the float32 rows of each, written and read.
+// part_us for the float32 rows of each, written and read.  Documents are not looked at:
+// their chains are shorter than `steps`, and parts are cost alone where they are short
+// (1 x 8192 tokens, 8 heads, documents of 256: 58 and 48 us in two parts each, and 13
+// and 25 for their sums).
 static int masked_parts(int64_t grid, int64_t steps, double share, double step_us, double part_us) {
   if (grid <= 0 || steps <= 0) return 1;
   const double all = (double)grid * (double)steps * share / (2.0 * kCUs);
@@ -526,6 +531,9 @@ CrossBwdChoice masked_bwd_choice(int64_t B, int64_t Sq, int64_t Sk, int64_t Hq, 
   const int64_t R = Hq / Hk * Sq, rows = (R + QT - 1) / QT, keys = (Sk + TR - 1) / TR;
   // a causal mask leaves half of the pairs where the queries are as many as the keys
   const double share = causal && Sk > 0 ? 1.0 - 0.5 * (double)std::min(Sq, Sk) / (double)Sk : 1.0;
+  // As cross_bwd_choice says, whose tiles these are: 1000 rows of a part cost 0.15 us
+  // (k_us: of two matrices); a tile of 64 keys takes a workgroup 1.45 us in dq, one of 32
+  // rows half of 3 us in dkv, one of 64 rows 2.8 us in the one pass.
   const double q_us = 1.5e-4 * (double)(B * Sq * Hq), k_us = 2 * 1.5e-4 * (double)(B * Sk * Hk);
   // One pass, as of attention to another sequence.  Forward and gradients of 4 x 51
   // tokens, 8 heads, replayed from a graph: 15.7 us, 24.6 with two passes; 2 x 128, 8 / 2

@@ -246,7 +246,10 @@ int validate_cross(const CrossSizes& z) {
   if (z.Sq * G > kMaxSize || z.B * z.Sq > kMaxSize || z.B * z.Sk > kMaxSize)
     return fail(PARTIR_E_SHAPE, "more than 2^30 query rows of a key head, queries or keys");
   // A launch is a grid of fewer than 2^32 threads: 256 for 128 query rows of a key
-  // head, 512 for 256 keys (parts are asked for only below one workgroup a CU).
+  // head, 512 for 256 keys.  Parts, at most 64 (256 in the gradients of attention to
+  // another sequence), are asked for only below one workgroup a CU; in the gradients of
+  // masked attention below 1024 workgroups (masked_parts: where the longest outlasts
+  // all of them on 512 places, with half of its steps on average at the least).
   if (z.B * z.Hk * std::max(cdiv(z.Sq * G, 128), 2 * cdiv(z.Sk, 256)) >= ((int64_t)1 << 24) || z.B * z.Sq * z.Hq > ((int64_t)1 << 33))
     return fail(PARTIR_E_SHAPE, "more than 2^32 threads of a launch");
   return PARTIR_OK;

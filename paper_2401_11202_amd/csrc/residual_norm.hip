@@ -21,6 +21,19 @@
 // loads, its two sums and its stores (34 and 53 MB).  The forward loads its gains behind
 // the sums: in front of them they take 12.4 -> 11.9 us there, but registers from the
 // waves that hide the loads of the first (96 -> 102).
+//
+// Above 4096 columns the gradients' workgroups have 9 to 16 waves, so 128 registers a
+// lane, and with a post norm or a gate that is not enough: 4 to 52 registers lie in
+// scratch memory, and above 8192 columns, with 16 columns a lane, 45 to 348 in every form.
+// These forms are bound by that.  Gradients in us, float32 stream, bf16 block, dropout,
+// a gate's row for 2048 rows; the bytes at 5.06 TB/s:
+//                  bytes   plain   post norm   gate   both
+//   8192 x 4096      119     119         143    131    148
+//   8192 x 5120      149     155         242    190    402
+//   8192 x 8192      239     246         318    263    558
+//   3000 x 12288     131     354         572    657   1212
+//   3000 x 16384     175     409         726    870   1543
+// The forward has no such limit: 95 to 114 us at 8192 x 5120, 92 to 108 at 3000 x 12288.
 #include <algorithm>
 #include <type_traits>
 
@@ -437,7 +450,8 @@ hipError_t launch_join_backward(const JoinParams& p, bool x_bf16, bool y_bf16, h
     auto go = [&](auto post, auto gate) {
       constexpr int C = decltype(c)::value;
       constexpr bool P = decltype(post)::value, G = decltype(gate)::value;
-      // up to 8 waves may take twice the registers that 16 may
+      // up to 8 waves may take twice the registers that 16 may, which are too few for
+      // most forms (the figures at the top)
       if (C == 1 && p.waves * p.teams <= 8)
         hipLaunchKernelGGL((join_bwd_kernel<decltype(x), decltype(y), 1, 512, P, G>), grid, block, 0, s, p);
       else
