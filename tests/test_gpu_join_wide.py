@@ -67,3 +67,19 @@ def test_offsets_past_32_bits(T, D, ld):
     want = P.residual_norm_backward(*dense, **kw)
     got = P.residual_norm_backward(X, Y, dH, dN, out=(h, n), **kw)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("T,D", [(3, 24), (700, 512), (1501, 1000), (90, 5120), (60, 9000)])
+def test_gradients_repeat_whatever_workspace_and_outputs_held(T, D, form):
+    """Sums of a workgroup's rows, of a team's gate rows and of the parts: each is written before it is read."""
+    say(f"residual_norm_backward T={T} D={D} {form}")
+    dev, ref, kw, j = make(T, D, form)
+    args = dev["X"], dev["Y"], dev["dH"], dev["dN"]
+    first = P.residual_norm_backward(*args, **kw)
+    ws = torch.empty(P.lib().partir_residual_norm_backward_workspace(T, D, kw["gate_rows"] or 0), dtype=torch.uint8, device="cuda")
+    for fill in (255, 0, 127):                     # NaN, 0, 3e38
+        outs = [None if t is None else torch.full_like(t, float("nan")) for t in first]
+        ws.fill_(fill)
+        P.residual_norm_backward(*args, out=outs[:2], gain_out=outs[2:], workspace=ws, **kw)
+        assert all(a is b is None or torch.equal(a, b) for a, b in zip(outs, first))
