@@ -26,8 +26,8 @@
 // another's time in part only.  2 x 4096 tokens, 32 / 8 heads, causal, capped: dq 447 to
 // 482 us (0.41 TFLOP, 0.9 PFLOP/s; matrix units busy 45 % of the time, vector units 62),
 // dkv 640 to 671 (0.55 TFLOP, 0.84 PFLOP/s; 37 and 50 %), 26 for the sum of two parts.
-// Causal without a cap: 410 and 639 (0.96 TFLOP, 0.92 PFLOP/s),
-// with a bias 409 and 657; without a mask, for twice the pairs, 743 and 1092 us
+// Causal without a cap: 410 and 639 (0.96 TFLOP, 0.92 PFLOP/s), with a bias 409 and
+// 657; without a mask, for twice the pairs, 743 and 1092 us
 // (attention to another sequence 727 and 992, whose dkv pass holds 256 keys).
 // Documents of 400 tokens on average, 4 x 2048, 32 heads: 157 and 167 us, with 640 and
 // 576 MB read and written (4.1 and 3.5 TB/s) in chains of few tiles.  3 x 333 tokens,
